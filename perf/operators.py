@@ -147,7 +147,8 @@ def work(case):
 def _quantized(x):
     """Codes and scales of an 8-bit cache: s = max|x| / 127 per token and head, codes round(x * (1 / s)), ties to even."""
     x = x.float()
-    s = x.abs().amax(-1) / 127
+    s = x.abs().amax(-1)
+    s = s / torch.full_like(s, 127)                      # (divided by a number, torch would multiply by its reciprocal)
     r = torch.where(s > 0, 1 / s, torch.zeros_like(s))
     return torch.round(x * r[..., None]).to(torch.int8), s
 
