@@ -336,6 +336,124 @@ int sage_attn_int8_bwd_ws(const void* q, const void* k, const void* v, const flo
                           int B, int H, int N, int D, int causal, unsigned flags,
                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ======================================================================== */
+/* Attention of language models: a causal sliding window with sinks         */
+/* (forward and backward), a paged cache of keys and values, attention of   */
+/* one new token per sequence over it, and shortening it.                   */
+/*                                                                          */
+/* Query i of a sequence of n tokens sees key j iff                         */
+/*     j <= i,  j < n,  and  (j > i - window  or  j < sinks)                */
+/* (window >= 1 counts the query's own token; a window of n or more is      */
+/* plain causal attention).  Heads are grouped: Hq is a multiple of Hkv and */
+/* query head h reads key head h * Hkv / Hq.  Softmax scale 1/sqrt(D).  A   */
+/* row that sees no key has o = 0 and L = -infinity.  What lies in keys and */
+/* values that a row does not see -- behind a sequence's end, in unused     */
+/* cache slots -- does not change it, infinities and NaN included.          */
+/* Everything is 16-bit in the type that flags give (SAGE_IN_FP16 or        */
+/* SAGE_IN_BF16, the only accepted bits), o and gradients too; scores,      */
+/* softmax and sums are fp32.  Probabilities are rounded to 16 bits for     */
+/* their product with V.  D is 64 or 128.  `stream` must belong to the      */
+/* current device.  Results are the same bits from call to call.            */
+/* ======================================================================== */
+
+/* Element strides of a [B, H, N, D] tensor; its channels are contiguous and
+ * every stride is a multiple of 16 bytes.  A null pointer means contiguous.  */
+typedef struct {
+  int64_t b, h, n;
+} sage_strides;
+
+/*
+ * sage_attn_window_fwd -- forward.
+ *  q      : [B, Hq, N, D], k, v: [B, Hkv, N, D], any strides (n at most 2^22; 0
+ *           broadcasts), 16-byte aligned
+ *  o      : [B, Hq, N, D], rows may not overlap
+ *  lse    : fp32 [B, Hq, N] or NULL: the natural-log log-sum-exp
+ *  lens   : int32 [B] or NULL: tokens of each sequence of a padded batch (on the
+ *           device; clamped to [0, N]).  Rows behind it are o = 0, L = -infinity
+ * Shape limits as above, with Hq heads (at most 65535).  No workspace.
+ */
+int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* lens,
+                         int B, int Hq, int Hkv, int N, int D, int window, int sinks, unsigned flags,
+                         const sage_strides* q_strides, const sage_strides* k_strides, const sage_strides* v_strides,
+                         const sage_strides* o_strides, hipStream_t stream);
+
+/*
+ * A paged cache: `pages` pages of `page_size` tokens (any size) for Hkv heads.
+ * Row (page, head, slot) of k starts at element page * k_strides.b + head *
+ * k_strides.h + slot * k_strides.n; [pages, Hkv, page_size, D] and [pages,
+ * page_size, Hkv, D] are both views of this form.  Rows hold D values of the
+ * 16-bit type, or, if k_scale and v_scale are given, D int8 codes:
+ *     s = max|x| / 127 per row,  code = rint(x * fl32(1/s)) (ties to even),
+ * with s in the fp32 arrays [pages, Hkv, page_size] (a row whose s is below
+ * 2^-126 has s = 0 and zero codes).
+ * A sequence's pages are a row of `table`, int32 [S, max_pages] on the device:
+ * its token j lies in page table[s][j / page_size], slot j % page_size.  Only
+ * entries of tokens that the sequence has are read; a token whose entry is not
+ * in [0, pages) is not stored, seen or moved.  Sequence lengths above max_pages *
+ * page_size (at most 2^30) count as that, negative ones as 0.  S is at most 65535.
+ */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  sage_strides k_strides, v_strides;   /* b: from page to page */
+  int pages, page_size, Hkv, D;
+} sage_kv_cache;
+
+/*
+ * sage_kv_append -- store new tokens: token t < counts[s] of sequence s at
+ * position pos[s] + t (positions that the table does not hold are skipped).
+ *  k, v   : [S, Hkv, N, D] 16-bit, any strides, 16-byte aligned
+ *  pos    : int32 [S], cached tokens before the call; counts: int32 [S] or NULL (N)
+ *  weights: fp32 [S, Hkv, weights_stride] or NULL: set to 0 for the new tokens
+ * Two tokens of one call stored in the same slot leave either.
+ */
+int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
+                   const sage_strides* v_strides, const int32_t* table, int max_pages, const int32_t* pos,
+                   const int32_t* counts, float* weights, int64_t weights_stride, int S, int N, unsigned flags,
+                   hipStream_t stream);
+
+/* Workspace bytes for sage_attn_paged_decode; 0 for invalid arguments.  Host only. */
+size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int max_pages, int page_size, int with_weights);
+
+/*
+ * sage_attn_paged_decode -- attention of one token per sequence, its last one
+ * (position lens[s] - 1, cached already), over the cache.  The work is split
+ * over the sequences' lengths, which are read on the device: a captured graph
+ * follows them.  Sequences may share pages.
+ *  q      : [S, Hq, D], element strides q_stride_s, q_stride_h, 16-byte aligned
+ *  o      : [S, Hq, D] contiguous; lse: fp32 [S, Hq] or NULL
+ *  lens   : int32 [S], cached tokens (0: o = 0, L = -infinity)
+ *  weights: fp32 [S, Hkv, weights_stride] or NULL: the attention weight of cached
+ *           token j, summed over the group's query heads, is added to
+ *           weights[s][head][j]; weights_stride >= max_pages * page_size
+ *  workspace: at least sage_attn_paged_decode_workspace_size() bytes, 256-byte
+ *           aligned; calls that may overlap need one each
+ */
+int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
+                           float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,
+                           int sinks, float* weights, int64_t weights_stride, unsigned flags, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * sage_kv_evict -- shorten cached sequences to `budget` tokens.  Per sequence of
+ * more than that, and per head: its first keep_first and last keep_last tokens
+ * stay, and of those between the ones with the largest weights (equal weights:
+ * the lowest index; NaN is lowest).  The kept tokens are copied, in their order,
+ * to positions 0, 1, ... of the pages in new_table.  Shorter sequences are copied
+ * whole (a token whose new place is its old one stays there).
+ *  weights    : fp32 [S, Hkv, weights_stride], weights_stride >= max_pages * page_size
+ *  new_table  : int32 [S, new_max_pages], new_max_pages * page_size >= budget.  Its
+ *               pages may not hold other tokens that this call moves
+ *  new_lens   : int32 [S]; kept: int32 [S, Hkv, budget], the kept tokens' old
+ *               positions, -1 behind the last; new_weights: fp32 [S, Hkv,
+ *               new_max_pages * page_size], their weights, 0 behind the last.
+ *               None of them overlaps an input
+ * keep_first + keep_last <= budget.  Source pages are left as they were.
+ */
+int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
+                  int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
+                  int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, hipStream_t stream);
+
 /* Human-readable status name; never NULL. */
 const char* sage_status_string(int status);
 

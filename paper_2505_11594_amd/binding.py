@@ -31,6 +31,16 @@ SAGE_ROLE_Q, SAGE_ROLE_K, SAGE_ROLE_V = 0, 1, 2
 _lib = None
 
 
+class _Strides(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("n", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("k_strides", _Strides), ("v_strides", _Strides),
+                ("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int)]
+
+
 class SageError(RuntimeError):
     def __init__(self, fn: str, status: int):
         super().__init__("%s failed: %s" % (fn, status_string(status)))
@@ -77,13 +87,21 @@ def lib():
         L.sage_attn_int8_bwd_workspace_size.restype = sz
         L.sage_attn_int8_bwd_min_workspace_size.argtypes = [i, i, i, i, u]
         L.sage_attn_int8_bwd_min_workspace_size.restype = sz
+        i64, st, ca = ctypes.c_int64, ctypes.POINTER(_Strides), ctypes.POINTER(_Cache)
+        L.sage_attn_window_fwd.argtypes = [vp] * 6 + [i] * 7 + [u] + [st] * 4 + [vp]
+        L.sage_kv_append.argtypes = [ca, vp, vp, st, st, vp, i, vp, vp, vp, i64, i, i, u, vp]
+        L.sage_attn_paged_decode_workspace_size.argtypes = [i] * 7
+        L.sage_attn_paged_decode_workspace_size.restype = sz
+        L.sage_attn_paged_decode.argtypes = [ca, vp, i64, i64, vp, vp, vp, i, vp, i, i, i, i, vp, i64, u, vp, sz, vp]
+        L.sage_kv_evict.argtypes = [ca, vp, i, vp, vp, i64, vp, i, i, i, i, vp, vp, vp, i, vp]
         L.sage_status_string.argtypes = [i]
         L.sage_status_string.restype = ctypes.c_char_p
         L.sage_version.restype = ctypes.c_char_p
         for name in ("sage_quant_sizes", "sage_quant_fp4", "sage_attn_fp4_fwd", "sage_attn_fp4_fwd_ws",
                      "sage_attn_fp4_fwd_noalloc", "sage_attn_fp4_fwd_prequant", "sage_attn_bf16_fwd", "sage_quant_int8_sizes",
                      "sage_quant_int8", "sage_attn_int8_fwd", "sage_attn_int8_fwd_ws",
-                     "sage_attn_int8_fwd_prequant", "sage_attn_int8_bwd", "sage_attn_int8_bwd_ws"):
+                     "sage_attn_int8_fwd_prequant", "sage_attn_int8_bwd", "sage_attn_int8_bwd_ws",
+                     "sage_attn_window_fwd", "sage_kv_append", "sage_attn_paged_decode", "sage_kv_evict"):
             getattr(L, name).restype = i
         _lib = L
     return _lib
@@ -383,6 +401,205 @@ def sage_attn_int8_bwd(q, k, v, o, lse, dout, causal: bool = False, flags: int =
         _check("sage_attn_int8_bwd_ws", lib().sage_attn_int8_bwd_ws(*ptrs, B, H, N, D, int(bool(causal)), flags,
                                                                   _ptr(workspace), workspace.numel(), _stream()))
     return dq, dk, dv
+
+
+# ------------------------------------------------- sliding window, paged cache, one-token attention
+_NO_WINDOW = 2 ** 31 - 1
+
+
+def _call(fn: str, device, *args):
+    """The C call on ``device`` and its current stream."""
+    import torch
+    stream = ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    if torch.cuda.current_device() == device.index:
+        rc = getattr(lib(), fn)(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(lib(), fn)(*args, stream)
+    _check(fn, rc)
+
+
+def _rows(t, what: str, ndim: int = 4):
+    """A strided tensor with contiguous channels whose rows start on 16 bytes: its strides but the last."""
+    if t.dim() != ndim or not t.is_cuda or t.numel() == 0:
+        raise ValueError("%s must be a non-empty %d-d device tensor, got shape %s on %s"
+                         % (what, ndim, tuple(t.shape), t.device))
+    # the stride of a dimension of size 1 is never used
+    s = tuple(x if n > 1 else n * 0 for x, n in zip(t.stride(), t.shape))
+    if (t.shape[-1] > 1 and s[-1] != 1) or any(x * t.element_size() % 16 for x in s[:-1]) or t.data_ptr() % 16:
+        raise ValueError("%s must have contiguous channels and rows on 16-byte addresses, got strides %s"
+                         % (what, tuple(t.stride())))
+    return s[:-1]
+
+
+def _same(t, like, what: str, shape):
+    if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be a %s tensor of shape %s on %s, got %s %s on %s"
+                         % (what, like.dtype, tuple(shape), like.device, t.dtype, tuple(t.shape), t.device))
+
+
+def _window_of(window, sinks: int):
+    window = _NO_WINDOW if window is None else int(window)
+    if window < 1 or sinks < 0:
+        raise ValueError("window must be at least 1 (None: no window) and sinks at least 0")
+    return min(window, _NO_WINDOW), min(int(sinks), _NO_WINDOW)
+
+
+def _check_window_args(q, k, v, lens):
+    import torch
+    qs, ks, vs = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    B, Hq, N, D = q.shape
+    Hkv = k.shape[1]
+    if Hq % Hkv:
+        raise ValueError("q's %d heads are no multiple of k's %d" % (Hq, Hkv))
+    for t, what in ((k, "k"), (v, "v")):
+        _same(t, q, what, (B, Hkv, N, D))
+    if lens is not None:
+        _check_tensor(lens, "lens", (B,), torch.int32, q.device)
+    return (B, Hq, Hkv, N, D), [_Strides(*x) for x in (qs, ks, vs)]
+
+
+def sage_attn_window_fwd(q, k, v, window=None, sinks: int = 0, lens=None, lse: bool = True, out=None, lse_out=None):
+    """Causal attention in which a query sees the last ``window`` keys (its own among them; None:
+    all) and the first ``sinks``.  q [B, Hq, N, D], k and v [B, Hkv, N, D] 16-bit, any strides with
+    contiguous channels; Hq a multiple of Hkv.  ``lens``: int32 [B], the tokens of a padded batch's
+    sequences.  Returns (O, L): O like q (``out`` may have other strides), L fp32 [B, Hq, N] (None
+    when ``lse`` is False); rows behind a sequence's end are 0 and -inf."""
+    import torch
+    flags = _in_flag(q)
+    (B, Hq, Hkv, N, D), st = _check_window_args(q, k, v, lens)
+    window, sinks = _window_of(window, sinks)
+    o = torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device) if out is None else out
+    _same(o, q, "out", (B, Hq, N, D))
+    st.append(_Strides(*_rows(o, "out")))
+    L = None
+    if lse:
+        L = torch.empty((B, Hq, N), dtype=torch.float32, device=q.device) if lse_out is None else lse_out
+        _check_tensor(L, "lse_out", (B, Hq, N), torch.float32, q.device)
+    _call("sage_attn_window_fwd", q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(L), _ptr(lens), B, Hq, Hkv, N, D,
+          window, sinks, flags, *st)
+    return o, L
+
+
+def _check_cache(k_cache, v_cache, k_scale, v_scale, table):
+    """The C description of a paged cache, and the table's shape."""
+    import torch
+    ks, vs = _rows(k_cache, "k_cache"), _rows(v_cache, "v_cache")
+    P, Hkv, page, D = k_cache.shape
+    _same(v_cache, k_cache, "v_cache", k_cache.shape)
+    dev = k_cache.device
+    if (k_scale is None) != (v_scale is None) or (k_cache.dtype == torch.int8) != (k_scale is not None):
+        raise ValueError("an int8 cache has k_scale and v_scale, a 16-bit one has neither")
+    if k_scale is not None:
+        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+            _check_tensor(t, what, (P, Hkv, page), torch.float32, dev)
+    else:
+        _in_flag(k_cache)
+    if table.dim() != 2 or table.numel() == 0:
+        raise ValueError("table must be a non-empty [S, max_pages] tensor")
+    _check_tensor(table, "table", table.shape, torch.int32, dev)
+    ptr = lambda t: t.data_ptr() if t is not None else None
+    c = _Cache(ptr(k_cache), ptr(v_cache), ptr(k_scale), ptr(v_scale), _Strides(*ks), _Strides(*vs), P, page, Hkv, D)
+    return c, int(table.shape[0]), int(table.shape[1])
+
+
+def _check_weights(w, what: str, S: int, Hkv: int, capacity: int, device):
+    import torch
+    if w.dim() != 3 or w.shape[2] < capacity:
+        raise ValueError("%s must be [S, Hkv, at least %d]" % (what, capacity))
+    _check_tensor(w, what, (S, Hkv, w.shape[2]), torch.float32, device)
+
+
+def sage_kv_append(k, v, k_cache, v_cache, table, pos, counts=None, k_scale=None, v_scale=None, weights=None):
+    """Store new tokens in a paged cache: token t < counts[s] (None: all) of k, v [S, Hkv, N, D] at
+    position pos[s] + t of sequence s.  The cache is [pages, Hkv, page_size, D] of any strides with
+    contiguous channels, of k's type or int8 with fp32 scales [pages, Hkv, page_size]; ``table`` int32
+    [S, max_pages] holds the sequences' pages.  ``weights`` [S, Hkv, >= max_pages * page_size] is set
+    to 0 at the new tokens."""
+    import torch
+    c, S, M = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    flags = _in_flag(k)
+    ks, vs = _rows(k, "k"), _rows(v, "v")
+    N, dev = int(k.shape[2]), k_cache.device
+    _same(v, k, "v", (S, c.Hkv, N, c.D))
+    _same(k, v, "k", (S, c.Hkv, N, c.D))
+    if k.device != dev or (k_scale is None and k.dtype != k_cache.dtype):
+        raise ValueError("k and v must be on %s and of the cache's type" % dev)
+    _check_tensor(pos, "pos", (S,), torch.int32, dev)
+    if counts is not None:
+        _check_tensor(counts, "counts", (S,), torch.int32, dev)
+    if weights is not None:
+        _check_weights(weights, "weights", S, c.Hkv, M * c.page_size, dev)
+    _call("sage_kv_append", dev, ctypes.byref(c), _ptr(k), _ptr(v), _Strides(*ks), _Strides(*vs), _ptr(table), M, _ptr(pos),
+          _ptr(counts), _ptr(weights), weights.shape[2] if weights is not None else 0, S, N, flags)
+
+
+def attn_paged_decode_workspace_size(S: int, Hq: int, Hkv: int, D: int, max_pages: int, page_size: int,
+                                     weights: bool = False) -> int:
+    return int(lib().sage_attn_paged_decode_workspace_size(S, Hq, Hkv, D, max_pages, page_size, int(bool(weights))))
+
+
+def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks: int = 0, k_scale=None, v_scale=None,
+                           weights=None, lse: bool = True, out=None, lse_out=None, workspace=None):
+    """Attention of each sequence's last token, q [S, Hq, D], over its lens[s] cached tokens (its own
+    among them); the cache as in sage_kv_append.  ``weights`` fp32 [S, Hkv, >= max_pages * page_size]:
+    the attention weights, summed over a group's query heads, are added to it.  Returns (O, L), L fp32
+    [S, Hq] (None when ``lse`` is False).  With ``workspace`` (uint8, at least
+    attn_paged_decode_workspace_size bytes) and ``out``, ``lse_out`` nothing is allocated inside."""
+    import torch
+    c, S, M = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    flags, dev = _in_flag(q), k_cache.device
+    qs = _rows(q, "q", 3)
+    Hq = int(q.shape[1])
+    if tuple(q.shape) != (S, Hq, c.D) or q.device != dev or (k_scale is None and q.dtype != k_cache.dtype):
+        raise ValueError("q must be [%d, Hq, %d] of the cache's type on %s, got %s %s on %s"
+                         % (S, c.D, dev, q.dtype, tuple(q.shape), q.device))
+    if Hq % c.Hkv:
+        raise ValueError("q's %d heads are no multiple of the cache's %d" % (Hq, c.Hkv))
+    window, sinks = _window_of(window, sinks)
+    _check_tensor(lens, "lens", (S,), torch.int32, dev)
+    if weights is not None:
+        _check_weights(weights, "weights", S, c.Hkv, M * c.page_size, dev)
+    o = torch.empty((S, Hq, c.D), dtype=q.dtype, device=dev) if out is None else out
+    _check_tensor(o, "out", (S, Hq, c.D), q.dtype, dev)
+    L = None
+    if lse:
+        L = torch.empty((S, Hq), dtype=torch.float32, device=dev) if lse_out is None else lse_out
+        _check_tensor(L, "lse_out", (S, Hq), torch.float32, dev)
+    if workspace is None:
+        n = attn_paged_decode_workspace_size(S, Hq, c.Hkv, c.D, M, c.page_size, weights is not None)
+        workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev)
+    _call("sage_attn_paged_decode", dev, ctypes.byref(c), _ptr(q), qs[0], qs[1], _ptr(o), _ptr(L), _ptr(table), M, _ptr(lens),
+          S, Hq, window, sinks, _ptr(weights), weights.shape[2] if weights is not None else 0, flags, _ptr(workspace),
+          workspace.numel())
+    return o, L
+
+
+def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int, keep_first: int = 0, keep_last: int = 0,
+                  k_scale=None, v_scale=None):
+    """Shorten cached sequences to ``budget`` tokens: the first keep_first, the last keep_last and the
+    heaviest of those between by ``weights`` [S, Hkv, >= max_pages * page_size], per head, in their
+    order; copied to the pages of ``new_table`` (int32 [S, new_max_pages]), which hold nothing else
+    that the call moves.  Returns (new_lens [S], new_weights [S, Hkv, new_max_pages * page_size],
+    kept [S, Hkv, budget]: the old positions, -1 behind the last)."""
+    import torch
+    c, S, M = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    dev = k_cache.device
+    _check_tensor(lens, "lens", (S,), torch.int32, dev)
+    _check_weights(weights, "weights", S, c.Hkv, M * c.page_size, dev)
+    if new_table.dim() != 2 or new_table.numel() == 0:
+        raise ValueError("new_table must be a non-empty [S, new_max_pages] tensor")
+    M2 = int(new_table.shape[1])
+    _check_tensor(new_table, "new_table", (S, M2), torch.int32, dev)
+    if not (1 <= budget <= M2 * c.page_size) or keep_first < 0 or keep_last < 0 or keep_first + keep_last > budget:
+        raise ValueError("budget must be at least 1, keep_first + keep_last and at most new_table's capacity")
+    new_lens = torch.empty((S,), dtype=torch.int32, device=dev)
+    new_weights = torch.empty((S, c.Hkv, M2 * c.page_size), dtype=torch.float32, device=dev)
+    kept = torch.empty((S, c.Hkv, budget), dtype=torch.int32, device=dev)
+    _call("sage_kv_evict", dev, ctypes.byref(c), _ptr(table), M, _ptr(lens), _ptr(weights), weights.shape[2], _ptr(new_table),
+          M2, budget, keep_first, keep_last, _ptr(new_lens), _ptr(new_weights), _ptr(kept), S)
+    return new_lens, new_weights, kept
 
 
 def version() -> str:

@@ -1,0 +1,485 @@
+// Attention of one new token per sequence over a paged cache, for gfx950.  The
+// token is the last one of its sequence (length n, itself cached already); it
+// sees key j iff j >= n - window or j < sinks.  Per key head and up to 16 query
+// heads of its group:
+//   S^T (keys x heads) = K . q^T,  online softmax in fp32,  O^T += V^T . P^T
+// on v_mfma_f32_16x16x32: each cached row is read once for all heads of the
+// group, 2 operations per byte and head, so the cache's bytes bound it and the
+// unused columns of a small group cost nothing.
+//
+// Every wave walks its own 32-key tiles: K goes from memory straight into the
+// A operand's registers (lane l: key l % 16, channels 8 (l / 16) on), V through
+// a wave-private LDS tile that is transposed as it is read; there is no barrier in
+// the loop.  The next tile's rows are in flight while one is computed.
+//
+// The split: the visible tiles of all sequences, in steps of 4 tiles (one per
+// wave), form one line that the workgroups of a key head cut into equal shares.
+// A workgroup's share may span several short sequences, and a long sequence
+// several workgroups: it is balanced whatever the lengths are, which only the
+// device knows.  A part that is a whole sequence is final; others leave their
+// (maximum, sum, O) for join_kernel.  A share has at most two of them: one that
+// began before it (slot 0) and one that goes on behind it (slot 1).
+#include "bf16_tile.h"
+#include "lm_args.h"
+#include "mma16.h"
+#include "window.h"
+
+namespace sage {
+
+constexpr int DT = 32;                  // keys per tile
+constexpr int DW = 4;                   // waves per workgroup
+constexpr int DG = 16;                  // query heads per workgroup
+
+__device__ __forceinline__ float max_over_groups(float x) {      // over the lanes l % 16 equal
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = smax(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return smax(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// Steps of a sequence.
+__device__ __forceinline__ TileList seq_tiles(const Decode& a, int s, int* n) {
+  *n = cached_len(a.lens[s], a.c.max_pages * a.c.page_size);
+  return decode_tiles(*n, a.window, a.sinks, DT);
+}
+
+// Where a share begins on the line of all sequences' steps: every wave adds up
+// the steps of 64 sequences at a time.
+struct Line {
+  long long total, share;               // steps in all, and per workgroup
+};
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+__device__ __forceinline__ Line steps_line(const Decode& a) {
+  const int lane = threadIdx.x & 63;
+  long long total = 0;
+  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
+    int n, c = 0;
+    if (s0 + lane < a.c.S) c = cdiv(seq_tiles(a, s0 + lane, &n).count, DW);
+    total += wave_sum(c);
+  }
+  Line l;
+  l.total = total;
+  l.share = (total + a.nw - 1) / a.nw;
+  return l;
+}
+// The sequence that holds step r (r < total) and the steps before it.
+__device__ __forceinline__ int find_step(const Decode& a, long long r, long long* before) {
+  const int lane = threadIdx.x & 63;
+  long long base = 0;
+  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
+    int n, c = 0;
+    if (s0 + lane < a.c.S) c = cdiv(seq_tiles(a, s0 + lane, &n).count, DW);
+    int inc = c;                                             // inclusive sum over the lanes
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(inc, o, 64);
+      if (lane >= o) inc += y;
+    }
+    const unsigned long long past = __builtin_amdgcn_ballot_w64(base + inc > r);
+    if (past) {
+      const int first = __builtin_ctzll(past);
+      *before = base + __shfl(inc - c, first, 64);
+      return s0 + first;
+    }
+    base += __shfl(inc, 63, 64);
+  }
+  *before = base;
+  return a.c.S;
+}
+
+// 16 int8 codes as 16 values of the type (exact).
+template <bool BF16>
+__device__ __forceinline__ void widen16(const v4i c, v4i& lo, v4i& hi) {
+  uint32_t w[8];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int x = c[d];
+    w[2 * d] = pack16<BF16>((float)(int8_t)x, (float)(int8_t)(x >> 8));
+    w[2 * d + 1] = pack16<BF16>((float)(int8_t)(x >> 16), (float)(x >> 24));
+  }
+  lo = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+  hi = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
+}
+
+// The A operands of 4 channel blocks for 32 keys: two transposing reads each, 16 keys apart.
+template <int D>
+__device__ __forceinline__ void v_read4(uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, v4i* r) {
+  v2u x0, x1, x2, x3, x4, x5, x6, x7;
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3), "=&v"(x4), "=&v"(x5), "=&v"(x6), "=&v"(x7)
+      : "v"(b0), "v"(b1), "v"(b2), "v"(b3), "n"(16 * D * 2)
+      : "memory");
+  r[0] = __builtin_bit_cast(v4i, __builtin_shufflevector(x0, x1, 0, 1, 2, 3));
+  r[1] = __builtin_bit_cast(v4i, __builtin_shufflevector(x2, x3, 0, 1, 2, 3));
+  r[2] = __builtin_bit_cast(v4i, __builtin_shufflevector(x4, x5, 0, 1, 2, 3));
+  r[3] = __builtin_bit_cast(v4i, __builtin_shufflevector(x6, x7, 0, 1, 2, 3));
+}
+
+// BF16: the type of q and o.  I8: 8-bit cache; its codes are exact in either type,
+// and P times V's scale, whose size nothing bounds, is rounded to bf16.
+template <int D, bool BF16, bool I8>
+__global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a) {
+  constexpr bool PB = BF16 || I8;                        // type of P and V in the second product
+  constexpr int EB = I8 ? 1 : 2, ROW = D * 2;
+  constexpr int KL = D * EB / 64;                        // 16-byte K loads per lane and 16-key subtile
+  constexpr int RC = D * EB / 16, VR = 64 / RC, VL = DT / VR;   // V: chunks per row, rows per load, loads
+  constexpr int NKS = D / 32, NDB = D / 16;
+  constexpr int PADQ = D + 4;                            // floats per head in the waves' join
+  constexpr int REG = DG * PADQ * 4;                     // LDS bytes per wave: V tile, then its O
+  static_assert(REG >= DT * ROW, "a V tile fits");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[DW * REG + DW * DG * 8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15, grp = lane >> 4;
+  const int hk = blockIdx.y, G = a.Hq / a.c.Hkv, g0 = blockIdx.z * DG, gn = min(DG, G - g0);
+  const int h0 = hk * G + g0;                            // first query head
+  uint8_t* const vt = lds + wave * REG;
+  const uint32_t vbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)vt;
+  uint32_t va[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+    va[db] = vbase + (4 * grp + c16 / 4) * ROW + vswz<D>(4 * grp + c16 / 4, 2 * db + (c16 & 3) / 2) * 16 + 8 * (c16 & 1);
+
+  long long r0 = 0, r1 = 0, before = 0;
+  int s = blockIdx.x;
+  if (a.nw > 0) {
+    const Line line = steps_line(a);
+    r0 = min(line.total, blockIdx.x * line.share);
+    r1 = min(line.total, r0 + line.share);
+    if (r0 >= r1) return;
+    s = find_step(a, r0, &before);
+  }
+  const int ps = a.c.page_size;
+  for (;;) {
+    // one sequence (or the share's part of it)
+    s = __builtin_amdgcn_readfirstlane(s);
+    int n;
+    const TileList tl = seq_tiles(a, s, &n);
+    const int steps = cdiv(tl.count, DW);
+    const int off = a.nw > 0 ? (int)(r0 - before) : 0;
+    const int cnt = a.nw > 0 ? (int)min((long long)(steps - off), r1 - r0) : steps;
+    const int tend = min(tl.count, DW * (off + cnt));
+    const int32_t* const table = a.c.table + (size_t)s * a.c.max_pages;
+
+    v4i qreg[NKS];
+    {
+      const uint16_t* q = (const uint16_t*)a.q + s * a.q_s + (h0 + min(c16, gn - 1)) * a.q_h;
+#pragma unroll
+      for (int i = 0; i < NKS; ++i)                      // channels in the order in which K's lie in its registers
+        qreg[i] = *reinterpret_cast<const v4i*>(q + (I8 ? 64 * (i / 2) + 16 * grp + 8 * (i & 1) : 32 * i + 8 * grp));
+    }
+    v4f oacc[NDB];
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) oacc[db] = v4f{};
+    float m = -INFINITY, l = 0.0f;                       // m in log2 units
+
+    // the page of this lane's key (key l % 32 of a tile), -1 where it has none
+    auto page_of = [&](int i) -> int {
+      const int key = tl.tile(i) * DT + (lane & 31);
+      if (i >= tend || !decode_sees(key, n, a.window, a.sinks)) return -1;
+      const int id = table[key / ps];
+      return page_ok(id, a.c.pages) ? id : -1;
+    };
+    struct Rows {
+      v4i k[2][KL], v[VL];
+      float ks[2], vs;
+    };
+    auto load = [&](int i, int id, Rows& r) {
+      const int kb = tl.tile(i) * DT;
+      const int slot = max(id, 0) == id ? (kb + (lane & 31)) % ps : 0;      // rows without a page: the cache's first one
+      const int pid = max(id, 0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int p = __shfl(pid, 16 * t + c16, 64), sl = __shfl(slot, 16 * t + c16, 64);
+        const uint8_t* k = (const uint8_t*)a.c.k + EB * (p * a.c.ks.b + hk * a.c.ks.h + sl * a.c.ks.n);
+#pragma unroll
+        for (int j = 0; j < KL; ++j) r.k[t][j] = *reinterpret_cast<const v4i*>(k + 64 * j + 16 * grp);
+      }
+#pragma unroll
+      for (int j = 0; j < VL; ++j) {
+        const int row = VR * j + lane / RC;
+        const int p = __shfl(pid, row, 64), sl = __shfl(slot, row, 64);
+        const uint8_t* v = (const uint8_t*)a.c.v + EB * (p * a.c.vs.b + hk * a.c.vs.h + sl * a.c.vs.n);
+        r.v[j] = *reinterpret_cast<const v4i*>(v + 16 * (lane % RC));
+      }
+      if constexpr (I8) {
+        const size_t x = ((size_t)pid * a.c.Hkv + hk) * ps + slot;
+        r.ks[0] = a.c.k_scale[x];
+        r.vs = id >= 0 ? a.c.v_scale[x] : 0.0f;          // a key that is not seen adds nothing, whatever lies there
+      }
+    };
+
+    int i = DW * off + wave;
+    int id = page_of(i), id1 = page_of(i + DW);
+    Rows cur, nxt;
+    if (i < tend) load(i, id, cur);
+    for (; i < tend; i += DW) {
+      const int id2 = page_of(i + 2 * DW);
+      if (i + DW < tend) load(i + DW, id1, nxt);
+      const unsigned ok = (unsigned)__builtin_amdgcn_ballot_w64(id >= 0);    // bit: key of the tile (both halves alike)
+
+      // scores of keys 16 t + 4 grp + e
+      v4f sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        v4f acc = v4f{};
+        if constexpr (I8) {
+#pragma unroll
+          for (int j = 0; j < KL; ++j) {
+            v4i lo, hi;
+            widen16<BF16>(cur.k[t][j], lo, hi);
+            acc = mma16<BF16>(lo, qreg[2 * j], acc);
+            acc = mma16<BF16>(hi, qreg[2 * j + 1], acc);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < KL; ++j) acc = mma16<BF16>(cur.k[t][j], qreg[j], acc);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = acc[e] * a.c2;
+          const int key = 16 * t + 4 * grp + e;
+          if constexpr (I8) x *= __shfl(cur.ks[0], key, 64);
+          sc[t][e] = (ok >> key) & 1u ? x : -INFINITY;
+        }
+      }
+      if (a.scores && c16 < gn) {
+        float* row = a.scores + ((size_t)s * a.Hq + h0 + c16) * a.score_stride + tl.tile(i) * DT;
+        *reinterpret_cast<v4f*>(row + 4 * grp) = sc[0];
+        *reinterpret_cast<v4f*>(row + 16 + 4 * grp) = sc[1];
+      }
+      float x = sc[0][0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) x = smax(x, sc[e >> 2][e & 3]);
+      const float m_new = smax(m, max_over_groups(x));
+      const float mc = m_new == -INFINITY ? 0.0f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - mc);
+      m = m_new;
+      const float mp = mc - kPShift<PB>;
+      float sum = 0.0f;
+      v4i pk;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        float p0 = __builtin_amdgcn_exp2f(sc[e >> 2][e & 3] - mp), p1 = __builtin_amdgcn_exp2f(sc[e >> 2][(e & 3) + 1] - mp);
+        sum += p0 + p1;
+        if constexpr (I8) {
+          const int key = 16 * (e >> 2) + 4 * grp + (e & 3);
+          p0 *= __shfl(cur.vs, key, 64);
+          p1 *= __shfl(cur.vs, key + 1, 64);
+        }
+        pk[e / 2] = (int)pack16<PB>(p0, p1);
+      }
+      l = l * alpha + sum;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) oacc[db][e] *= alpha;
+      }
+      // V into the wave's tile; rows that are not seen are zero, whatever lies in the cache
+#pragma unroll
+      for (int j = 0; j < VL; ++j) {
+        const int row = VR * j + lane / RC, ch = lane % RC;
+        v4i v = cur.v[j];
+        if (!((ok >> row) & 1u)) v = v4i{};
+        if constexpr (I8) {
+          v4i lo, hi;
+          widen16<true>(v, lo, hi);
+          *reinterpret_cast<v4i*>(vt + row * ROW + vswz<D>(row, 2 * ch) * 16) = lo;
+          *reinterpret_cast<v4i*>(vt + row * ROW + vswz<D>(row, 2 * ch + 1) * 16) = hi;
+        } else {
+          *reinterpret_cast<v4i*>(vt + row * ROW + vswz<D>(row, ch) * 16) = v;
+        }
+      }
+      static_for<NDB / 4>([&](auto B_) {
+        constexpr int b4 = 4 * decltype(B_)::value;
+        v4i vv[4];
+        v_read4<D>(va[b4], va[b4 + 1], va[b4 + 2], va[b4 + 3], vv);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) oacc[b4 + d] = mma16<PB>(vv[d], pk, oacc[b4 + d]);
+      });
+      id = id1;
+      id1 = id2;
+      cur = nxt;
+    }
+
+    // join the 4 waves
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    float* const ml = reinterpret_cast<float*>(lds + DW * REG);
+    if (grp == 0) {
+      ml[(wave * DG + c16) * 2] = m;
+      ml[(wave * DG + c16) * 2 + 1] = l;
+    }
+    __syncthreads();                                     // also: every wave is past its last V tile
+    float mm = -INFINITY, ll = 0.0f;
+#pragma unroll
+    for (int w = 0; w < DW; ++w) mm = smax(mm, ml[(w * DG + c16) * 2]);
+    const float mc = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll
+    for (int w = 0; w < DW; ++w) ll += ml[(w * DG + c16) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * DG + c16) * 2] - mc);
+    const float f = __builtin_amdgcn_exp2f(m - mc);
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+      *reinterpret_cast<v4f*>(vt + (c16 * PADQ + 16 * db + 4 * grp) * 4) = oacc[db] * v4f{f, f, f, f};
+    __syncthreads();
+
+    const bool whole = off == 0 && cnt == steps;
+    const size_t slot = (size_t)blockIdx.x * 2 + (off == 0 ? 1 : 0);
+    if (wave == 0 && grp == 0 && c16 < gn) {
+      const float l2 = ll > 0.0f || ll != ll ? mm + (__builtin_log2f(ll) - kPShift<PB>) : -INFINITY;
+      if (whole) {
+        if (a.lse) a.lse[(size_t)s * a.Hq + h0 + c16] = l2 * 0.69314718055994530942f;
+        if (a.lse2) a.lse2[(size_t)s * a.Hq + h0 + c16] = l2;
+      } else {
+        float* p = a.part + (size_t)a.nw * 2 * a.Hq * D + (slot * a.Hq + h0 + c16) * 2;
+        p[0] = mm;
+        p[1] = ll;
+      }
+    }
+    // thread: head tid / 16, 4 channels at a time
+    const int qh = tid >> 4;
+    const float lq = __shfl(ll, qh, 64);                 // lane qh (< 16) holds head qh's sum
+    if (qh < gn) {
+      const float inv = lq > 0.0f || lq != lq ? 1.0f / lq : 0.0f;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        const int d = 64 * c + 4 * (tid & 15);
+        v4f x = v4f{};
+#pragma unroll
+        for (int w = 0; w < DW; ++w) x += *reinterpret_cast<const v4f*>(lds + w * REG + (qh * PADQ + d) * 4);
+        if (whole) {
+          const v2u o = {pack16<BF16>(x[0] * inv, x[1] * inv), pack16<BF16>(x[2] * inv, x[3] * inv)};
+          *reinterpret_cast<v2u*>((uint16_t*)a.o + ((size_t)s * a.Hq + h0 + qh) * D + d) = o;
+        } else {
+          *reinterpret_cast<v4f*>(a.part + (slot * a.Hq + h0 + qh) * D + d) = x;
+        }
+      }
+    }
+    if (a.nw == 0) return;
+    r0 += cnt;
+    before += steps;
+    if (r0 >= r1) return;
+    ++s;
+    // sequences that have no steps hold no place on the line
+    for (int nn; s < a.c.S && seq_tiles(a, s, &nn).count == 0; ++s) {}
+    __syncthreads();                                     // the next sequence's V tiles overwrite the join's LDS
+  }
+}
+
+// Sequences whose steps several workgroups shared: O = sum O_w 2^(m_w - m) / l.
+// One workgroup per (sequence, query head).
+template <int D, bool BF16>
+__global__ __launch_bounds__(64) void join_kernel(const Decode a, float shift) {
+  const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
+  const Line line = steps_line(a);
+  int n;
+  const int steps = cdiv(seq_tiles(a, s, &n).count, DW);
+  long long before = 0;
+  for (int s0 = 0; s0 < s; s0 += 64) {
+    int nn, c = 0;
+    if (s0 + lane < s) c = cdiv(seq_tiles(a, s0 + lane, &nn).count, DW);
+    before += wave_sum(c);
+  }
+  uint16_t* o = (uint16_t*)a.o + ((size_t)s * a.Hq + h) * D + lane * (D / 64);
+  float l2 = -INFINITY, x[D / 64] = {};
+  if (steps > 0) {
+    const int w0 = (int)(before / line.share), w1 = (int)((before + steps - 1) / line.share);
+    if (w0 == w1) return;                                // final already
+    const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
+    // a share's slot 1 if the sequence begins in it, slot 0 if it began before
+    auto at = [&](int w) { return ((size_t)w * 2 + (w == w0 ? 1 : 0)) * a.Hq + h; };
+    float m = -INFINITY, l = 0.0f;
+    for (int w = w0 + lane; w <= w1; w += 64) m = smax(m, ml[at(w) * 2]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) m = smax(m, __shfl_xor(m, d, 64));
+    const float mc = m == -INFINITY ? 0.0f : m;
+    for (int w = w0; w <= w1; ++w) {
+      const float f = __builtin_amdgcn_exp2f(ml[at(w) * 2] - mc);
+      l += ml[at(w) * 2 + 1] * f;
+      const float* p = a.part + at(w) * D + lane * (D / 64);
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) x[i] += p[i] * f;
+    }
+    if (l > 0.0f || l != l) {
+      l2 = m + (__builtin_log2f(l) - shift);
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) x[i] /= l;
+    }
+  }
+  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(o) = pack16<BF16>(x[0], x[1]);
+  else *o = (uint16_t)pack16<BF16>(x[0], 0.0f);
+  if (lane == 0) {
+    if (a.lse) a.lse[(size_t)s * a.Hq + h] = l2 * 0.69314718055994530942f;
+    if (a.lse2) a.lse2[(size_t)s * a.Hq + h] = l2;
+  }
+}
+
+// weights[j] += sum over the group's heads of exp(S - L), one thread per cached token.
+__global__ __launch_bounds__(256) void add_weights_kernel(const Decode a) {
+  const int s = blockIdx.z, hk = blockIdx.y, G = a.Hq / a.c.Hkv;
+  const int n = cached_len(a.lens[s], a.c.max_pages * a.c.page_size);
+  float* w = a.weights + ((size_t)s * a.c.Hkv + hk) * a.wstride;
+  const float* sc = a.scores + ((size_t)s * a.Hq + (size_t)hk * G) * a.score_stride;
+  const float* l2 = a.lse2 + (size_t)s * a.Hq + hk * G;
+  for (int j = blockIdx.x * 256 + threadIdx.x; j < n; j += gridDim.x * 256) {
+    if (!decode_sees(j, n, a.window, a.sinks)) continue;
+    float x = 0.0f;
+    for (int g = 0; g < G; ++g) {
+      const float y = sc[g * a.score_stride + j];
+      if (y != -INFINITY) x += __builtin_amdgcn_exp2f(y - l2[g]);
+    }
+    w[j] += x;
+  }
+}
+
+// Workgroups per group of 16 query heads of a key head.  Two fit a CU, so 512 in
+// all keep every CU busy; a batch has no use for more than its steps.  Sequences of
+// up to 4 steps (512 cached tokens) get a workgroup each instead, and no join.
+int decode_workgroups(int S, int Hq, int Hkv, int capacity) {
+  const long long steps = cdiv(capacity, DT * DW) + 1;   // the sinks' tiles may add a step
+  if (steps <= 5) return 0;
+  const int heads = Hkv * cdiv(Hq / Hkv, DG);
+  const long long want = imax(1, 512 / heads), most = (long long)S * steps;
+  return (int)(want < most ? want : most);
+}
+size_t decode_part_floats(int S, int Hq, int Hkv, int D, int capacity) {
+  return (size_t)decode_workgroups(S, Hq, Hkv, capacity) * 2 * Hq * (D + 2);
+}
+
+template <int D, bool BF16>
+static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
+  const int G = a.Hq / a.c.Hkv;
+  const dim3 grid((unsigned)(a.nw > 0 ? a.nw : a.c.S), (unsigned)a.c.Hkv, (unsigned)cdiv(G, DG)), block(64 * DW);
+  if (a.c.k_scale) hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false>), grid, block, 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && a.nw > 0) {
+    const float shift = a.c.k_scale ? 0.0f : kPShift<BF16>;
+    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(64), 0, st, a, shift);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && a.weights) {
+    const int capacity = a.c.max_pages * a.c.page_size;
+    const int want = imax(1, 2048 / imax(1, imin(2048, a.c.S * a.c.Hkv)));
+    hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)imin(cdiv(capacity, 256), want), (unsigned)a.c.Hkv, (unsigned)a.c.S),
+                       dim3(256), 0, st, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+hipError_t launch_paged_decode(const Decode& a, int D, bool bf16, hipStream_t st) {
+  if (D == 128) return bf16 ? launch_decode_t<128, true>(a, st) : launch_decode_t<128, false>(a, st);
+  return bf16 ? launch_decode_t<64, true>(a, st) : launch_decode_t<64, false>(a, st);
+}
+
+}  // namespace sage
