@@ -377,6 +377,28 @@ int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, f
                          const sage_strides* q_strides, const sage_strides* k_strides, const sage_strides* v_strides,
                          const sage_strides* o_strides, hipStream_t stream);
 
+/* Workspace bytes for sage_attn_window_bwd (two fp32 values per query row, and
+ * parts of the sinks' gradients); 0 for invalid arguments.  Host only. */
+size_t sage_attn_window_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D, int window, int sinks);
+
+/*
+ * sage_attn_window_bwd -- backward: the gradients of q, k, v for dout, that of o.
+ *  q, k, v, o, lse, lens, window, sinks: as given to the forward, and its outputs
+ *  dout    : [B, Hq, N, D], any strides; rows behind a sequence's end are not read
+ *  dq      : [B, Hq, N, D], dk, dv: [B, Hkv, N, D] (summed over the group's query
+ *            heads), contiguous, 16-byte aligned; 0 behind a sequence's end
+ *  workspace: at least sage_attn_window_bwd_workspace_size() bytes, 256-byte aligned
+ * P and dS are rounded to 16 bits for their products with dO, Q and K (in fp16
+ * scaled by powers of two that keep them in range).  B * (Hq + Hkv) is at most
+ * 65535.  A NaN or infinity in q, k, v or dout of a token may spread to the
+ * gradients of all tokens of its sequence and key head (not to others').
+ */
+int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout,
+                         const int32_t* lens, void* dq, void* dk, void* dv, int B, int Hq, int Hkv, int N, int D,
+                         int window, int sinks, unsigned flags, const sage_strides* q_strides,
+                         const sage_strides* k_strides, const sage_strides* v_strides, const sage_strides* o_strides,
+                         const sage_strides* dout_strides, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /*
  * A paged cache: `pages` pages of `page_size` tokens (any size) for Hkv heads.
  * Row (page, head, slot) of k starts at element page * k_strides.b + head *

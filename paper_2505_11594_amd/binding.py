@@ -89,6 +89,9 @@ def lib():
         L.sage_attn_int8_bwd_min_workspace_size.restype = sz
         i64, st, ca = ctypes.c_int64, ctypes.POINTER(_Strides), ctypes.POINTER(_Cache)
         L.sage_attn_window_fwd.argtypes = [vp] * 6 + [i] * 7 + [u] + [st] * 4 + [vp]
+        L.sage_attn_window_bwd_workspace_size.argtypes = [i] * 7
+        L.sage_attn_window_bwd_workspace_size.restype = sz
+        L.sage_attn_window_bwd.argtypes = [vp] * 10 + [i] * 7 + [u] + [st] * 5 + [vp, sz, vp]
         L.sage_kv_append.argtypes = [ca, vp, vp, st, st, vp, i, vp, vp, vp, i64, i, i, u, vp]
         L.sage_attn_paged_decode_workspace_size.argtypes = [i] * 7
         L.sage_attn_paged_decode_workspace_size.restype = sz
@@ -101,7 +104,7 @@ def lib():
                      "sage_attn_fp4_fwd_noalloc", "sage_attn_fp4_fwd_prequant", "sage_attn_bf16_fwd", "sage_quant_int8_sizes",
                      "sage_quant_int8", "sage_attn_int8_fwd", "sage_attn_int8_fwd_ws",
                      "sage_attn_int8_fwd_prequant", "sage_attn_int8_bwd", "sage_attn_int8_bwd_ws",
-                     "sage_attn_window_fwd", "sage_kv_append", "sage_attn_paged_decode", "sage_kv_evict"):
+                     "sage_attn_window_fwd", "sage_attn_window_bwd", "sage_kv_append", "sage_attn_paged_decode", "sage_kv_evict"):
             getattr(L, name).restype = i
         _lib = L
     return _lib
@@ -479,6 +482,37 @@ def sage_attn_window_fwd(q, k, v, window=None, sinks: int = 0, lens=None, lse: b
     _call("sage_attn_window_fwd", q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(L), _ptr(lens), B, Hq, Hkv, N, D,
           window, sinks, flags, *st)
     return o, L
+
+
+def attn_window_bwd_workspace_size(B: int, Hq: int, Hkv: int, N: int, D: int, window=None, sinks: int = 0) -> int:
+    return int(lib().sage_attn_window_bwd_workspace_size(B, Hq, Hkv, N, D, *_window_of(window, sinks)))
+
+
+def sage_attn_window_bwd(q, k, v, o, lse, dout, window=None, sinks: int = 0, lens=None, workspace=None, out=None):
+    """The gradients (dQ, dK, dV) of sage_attn_window_fwd for dout, the gradient of its O; o and lse
+    are its outputs, window, sinks and lens as given to it.  q, k, v, o, dout of any strides with
+    contiguous channels; the gradients are contiguous, of q's type, dK and dV summed over a group's
+    query heads.  ``out``: three preallocated tensors; with ``workspace`` (uint8, at least
+    attn_window_bwd_workspace_size bytes) too nothing is allocated inside."""
+    import torch
+    flags = _in_flag(q)
+    (B, Hq, Hkv, N, D), st = _check_window_args(q, k, v, lens)
+    window, sinks = _window_of(window, sinks)
+    for t, what in ((o, "o"), (dout, "dout")):
+        _same(t, q, what, (B, Hq, N, D))
+        st.append(_Strides(*_rows(t, what)))
+    _check_tensor(lse, "lse", (B, Hq, N), torch.float32, q.device)
+    shapes = ((B, Hq, N, D), (B, Hkv, N, D), (B, Hkv, N, D))
+    dq, dk, dv = out if out is not None else [torch.empty(s, dtype=q.dtype, device=q.device) for s in shapes]
+    for t, s, what in zip((dq, dk, dv), shapes, ("dq", "dk", "dv")):
+        _check_tensor(t, what, s, q.dtype, q.device)
+    if workspace is None:
+        n = attn_window_bwd_workspace_size(B, Hq, Hkv, N, D, window, sinks)
+        workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=q.device)
+    _check_workspace(workspace, q.device)
+    _call("sage_attn_window_bwd", q.device, *[_ptr(t) for t in (q, k, v, o, lse, dout, lens, dq, dk, dv)], B, Hq, Hkv, N, D,
+          window, sinks, flags, *st, _ptr(workspace), workspace.numel())
+    return dq, dk, dv
 
 
 def _check_cache(k_cache, v_cache, k_scale, v_scale, table):

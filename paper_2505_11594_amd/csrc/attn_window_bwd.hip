@@ -1,0 +1,554 @@
+// Backward pass of the window attention (attn_window.hip) for gfx950.  With
+// P = exp(S / sqrt(D) - L), delta_i = sum_d dO_i O_i and dS = P o (dO V^T - delta):
+//   dV_j = sum_i P_ij dO_i,   dK_j = sum_i dS_ij Q_i / sqrt(D),   dQ_i = sum_j dS_ij K_j / sqrt(D)
+// summed over the query heads of a group for dK and dV, in fp32 and in a fixed order.
+//
+// Two passes over the visible pairs, each recomputing S and dP: dkv_kernel (4
+// products; a wave holds 32 keys' K, V, dK^T and dV^T in registers and walks the
+// queries that see them, all heads of the group) and dq_kernel (3 products; a wave
+// holds 32 queries and walks their keys).  One pass would need dQ added up across
+// workgroups: atomics whose order changes the result, or a stored dS, whose 4 bytes
+// per pair (written and read) take longer than the two products they save.
+//
+// A query tile (or key tile) lies in LDS once, in a layout that serves both the row
+// reads of S and dP and the transposing reads of the second products (vswz); P and dS
+// stay in registers, as in the forward.  MFMA issue and LDS reads (32 KiB per 32
+// products of 32 x 32 x 16) bound both kernels.
+//
+// Sink keys are seen by every later query, 32768 / 1152 times as many as others of a
+// long sequence: dkv_kernel leaves them out, sink_kernel takes them in chunks of
+// queries and join_sinks_kernel adds the chunks.
+//
+// P and dS are rounded to the input's type for the second products.  In fp16 both
+// carry a power of two that keeps them normal numbers: P 2^15, and dS the largest
+// with which 2 max|dO_i| max|V_j| (a bound of |dP - delta|, over the group's heads)
+// stays below 2^15.
+#include "bf16_tile.h"
+#include "lm_args.h"
+#include "mma16.h"
+#include "window.h"
+
+namespace sage {
+
+constexpr int BT = 64;                  // rows of a tile in LDS
+constexpr int PR = 64;                  // rows per workgroup of the row pass
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ int seq_len(const WindowBwd& a, int b) { return a.lens ? cached_len(a.lens[b], a.N) : a.N; }
+// Rows of a sequence's lb and delta arrays.
+__device__ __forceinline__ int row_pad(int N) { return (N + BT - 1) / BT * BT; }
+
+// lb = L log2(e) (+inf behind the sequence's end: P = 0 there) and delta per query
+// row; in fp16 also the largest |dO_i| (and, from blockIdx.y >= B Hq on, |V_j|) of
+// every PR rows.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void rows_kernel(const WindowBwd a) {
+  constexpr int LPR = D / 8, RPP = 256 / LPR;            // lanes per row, rows per pass
+  __shared__ float red[4];
+  const int tid = threadIdx.x, ch = tid % LPR;
+  const int nb = cdiv(a.N, PR);
+  const bool vrows = (int)blockIdx.y >= a.B * a.Hq;
+  const int bh = vrows ? blockIdx.y - a.B * a.Hq : blockIdx.y, H = vrows ? a.Hkv : a.Hq;
+  const int b = bh / H, h = bh - b * H, n = seq_len(a, b);
+  const Strides& xs = vrows ? a.vs : a.gs;
+  const uint16_t* x = (const uint16_t*)(vrows ? a.v : a.dout) + b * xs.b + h * xs.h + 8 * ch;
+  const uint16_t* o = (const uint16_t*)a.o + b * a.os.b + h * a.os.h + 8 * ch;
+  float most = 0.0f;
+#pragma unroll
+  for (int r0 = 0; r0 < PR; r0 += RPP) {
+    const int i = blockIdx.x * PR + r0 + tid / LPR;
+    float dot = 0.0f, sq = 0.0f;
+    if (i < n) {
+      const v4i g = *reinterpret_cast<const v4i*>(x + i * xs.n);
+      v4i y = g;
+      if (!vrows) y = *reinterpret_cast<const v4i*>(o + i * a.os.n);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float gv = widen<BF16>((uint16_t)((uint32_t)g[e / 2] >> (16 * (e & 1))));
+        dot = __builtin_fmaf(gv, widen<BF16>((uint16_t)((uint32_t)y[e / 2] >> (16 * (e & 1)))), dot);
+        if constexpr (!BF16) sq = __builtin_fmaf(gv, gv, sq);
+      }
+    }
+#pragma unroll
+    for (int s = LPR / 2; s >= 1; s >>= 1) {
+      dot += __shfl_xor(dot, s, 64);
+      if constexpr (!BF16) sq += __shfl_xor(sq, s, 64);
+    }
+    if (!vrows && ch == 0) {                             // (the arrays hold whole tiles of rows)
+      const size_t at = (size_t)bh * row_pad(a.N) + i;
+      a.delta[at] = dot;
+      a.lb[at] = i < n ? a.lse[(size_t)bh * a.N + i] * kLog2e : INFINITY;
+    }
+    most = __builtin_fmaxf(most, sq);
+  }
+  if constexpr (!BF16) {
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) most = __builtin_fmaxf(most, __shfl_xor(most, s, 64));
+    if ((tid & 63) == 0) red[tid >> 6] = most;
+    __syncthreads();
+    if (tid == 0)
+      a.norms[(size_t)blockIdx.y * nb + blockIdx.x] =
+          __builtin_sqrtf(__builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3])));
+  }
+}
+static_assert(PR == BT, "the row pass fills whole tiles of rows");
+
+// The power of two that dS of a (sequence, key head) carries in fp16.  Every lane
+// gets it.
+template <bool BF16>
+__device__ __forceinline__ float ds_scale(const WindowBwd& a, int b, int hk) {
+  if constexpr (BF16) return 1.0f;
+  const int lane = threadIdx.x & 63, nb = cdiv(a.N, PR), G = a.Hq / a.Hkv;
+  const float* g = a.norms + ((size_t)b * a.Hq + hk * G) * nb;
+  const float* v = a.norms + ((size_t)a.B * a.Hq + b * a.Hkv + hk) * nb;
+  float gm = 0.0f, vm = 0.0f;
+  for (int i = lane; i < G * nb; i += 64) gm = __builtin_fmaxf(gm, g[i]);
+  for (int i = lane; i < nb; i += 64) vm = __builtin_fmaxf(vm, v[i]);
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) {
+    gm = __builtin_fmaxf(gm, __shfl_xor(gm, s, 64));
+    vm = __builtin_fmaxf(vm, __shfl_xor(vm, s, 64));
+  }
+  const float bound = 2.0f * gm * vm;
+  if (!(bound > 0.0f) || bound == INFINITY) return 1.0f;
+  int e;
+  __builtin_frexpf(bound, &e);                           // bound < 2^e
+  return __builtin_ldexpf(1.0f, imax(-100, imin(100, 15 - e)));
+}
+
+// Address pieces of the transposing reads of a tile at LDS offset 0 (see attn_window.hip).
+template <int D>
+__device__ __forceinline__ void tr_offsets(uint32_t* vo) {
+  constexpr int ROW = D * 2;
+  const int lane = threadIdx.x & 63, hi = lane >> 5;
+  const int r = 4 * hi + (lane & 15) / 4, c0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) vo[db] = r * ROW + vswz<D>(r, 4 * db + c0) * 16 + 8 * (lane & 1);
+}
+template <int D, int OFF>
+__device__ __forceinline__ void tr_read(const uint32_t* va, v4i* r) {
+  v8bf t[D / 32];
+  if constexpr (D == 128) vt_read4<OFF, OFF + 8 * D * 2>(va[0], va[1], va[2], va[3], t[0], t[1], t[2], t[3]);
+  else vt_read2<OFF, OFF + 8 * D * 2>(va[0], va[1], t[0], t[1]);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) r[db] = __builtin_bit_cast(v4i, t[db]);
+}
+
+// One 32 x 32 block of (query, key) pairs for a wave that holds 32 keys (kreg, vreg;
+// lane: key l % 32): adds to dv and dk (dims x keys).  The block's queries are rows
+// [32 t, +32) of the tile at L (Q, then dO, then lb and delta).
+template <int D, bool BF16, bool MASK>
+__device__ __forceinline__ void dkv_block(const uint8_t* L, uint32_t lbase, const uint32_t* vo, int t, const v4i* kreg,
+                                          const v4i* vreg, v16f* dk, v16f* dv, float c2, float f15, int first, int past) {
+  constexpr int ROW = D * 2, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
+  const int lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
+  const int row = 32 * t + col;
+  v16f s = v16f{}, g = v16f{};
+#pragma unroll
+  for (int i = 0; i < NKS; ++i) s = mma32<BF16>(*reinterpret_cast<const v4i*>(L + row * ROW + vswz<D>(row, 2 * i + hi) * 16), kreg[i], s);
+#pragma unroll
+  for (int i = 0; i < NKS; ++i) g = mma32<BF16>(*reinterpret_cast<const v4i*>(L + TB + row * ROW + vswz<D>(row, 2 * i + hi) * 16), vreg[i], g);
+  // element e is query 32 t + 8 (e >> 2) + 4 hi + (e & 3) of the tile, visible iff first <= it < past
+  uint32_t pw[8], dw[8];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int at = 32 * t + 8 * q + 4 * hi;
+    const v4f lb = *reinterpret_cast<const v4f*>(L + 2 * TB + 4 * at), dl = *reinterpret_cast<const v4f*>(L + 2 * TB + 4 * BT + 4 * at);
+    float p[4], d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * q + e], c2, kPShift<BF16> - lb[e]));
+      if constexpr (MASK) {
+        const uint32_t keep = (uint32_t)((~(at + e - first) & (at + e - past)) >> 31);
+        p[e] = __uint_as_float(__float_as_uint(p[e]) & keep);
+      }
+      const float x = g[4 * q + e] - dl[e];
+      d[e] = p[e] * (BF16 ? x : x * f15);
+    }
+    pw[2 * q] = pack16<BF16>(p[0], p[1]); pw[2 * q + 1] = pack16<BF16>(p[2], p[3]);
+    dw[2 * q] = pack16<BF16>(d[0], d[1]); dw[2 * q + 1] = pack16<BF16>(d[2], d[3]);
+  }
+  uint32_t va[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) va[db] = vo[db] + lbase + (uint32_t)t * 32 * ROW;
+  static_for<2>([&](auto U_) {
+    constexpr int u = decltype(U_)::value;
+    const v4i pk = {(int)pw[4 * u], (int)pw[4 * u + 1], (int)pw[4 * u + 2], (int)pw[4 * u + 3]};
+    const v4i dsk = {(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]};
+    v4i x[NDB];
+    tr_read<D, TB + 16 * u * ROW>(va, x);
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) dv[db] = mma32<BF16>(x[db], pk, dv[db]);
+    tr_read<D, 16 * u * ROW>(va, x);
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) dk[db] = mma32<BF16>(x[db], dsk, dk[db]);
+  });
+}
+
+// dK and dV.  SINK: 2 waves share 32 sink keys and take one half of each query tile;
+// else 4 waves x 32 keys.  Grid x: (sequence, key head) times the key blocks (times
+// the chunks of the sinks' query tiles).
+template <int D, bool BF16, bool SINK>
+__global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dkv_kernel(const WindowBwd a) {
+  constexpr int W = SINK ? 2 : 4;                        // waves
+  constexpr int KB = SINK ? 32 : 128;                    // keys per workgroup
+  constexpr int ROW = D * 2, CH = ROW / 16, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
+  constexpr int STAGE = 2 * TB + 2 * BT * 4;             // Q, dO, lb, delta
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hi = lane >> 5;
+  const int nkb = SINK ? cdiv(a.sinks, KB) : cdiv(a.N, KB);
+  const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
+  unsigned lin = xcd * (total >> 3) + min(xcd, total & 7u) + (blockIdx.x >> 3);
+  int chunk = 0;
+  if constexpr (SINK) { chunk = lin % a.chunks; lin /= a.chunks; }
+  const int bh = (int)(lin / nkb), b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.Hq / a.Hkv;
+  const int k0 = (int)(lin % nkb) * KB, kw = SINK ? k0 : k0 + 32 * wave, key = kw + col;
+  const int n = seq_len(a, b), Np = row_pad(a.N);
+
+  // query tiles that see some of the keys, once per head of the group
+  int t0 = k0 / BT, t1 = 0;                              // tiles [t0, t1)
+  if (k0 < n) t1 = cdiv(SINK ? n : imin(n, imin(a.N, k0 + KB - 1 + a.window)), BT);
+  if (!SINK && k0 + KB <= a.sinks) t1 = 0;               // sink keys alone
+  const int nt = imax(0, t1 - t0), all = nt * G;
+  int it0 = 0, it1 = all;
+  if constexpr (SINK) {
+    const int share = cdiv(all, a.chunks);
+    it0 = imin(all, chunk * share);
+    it1 = imin(all, it0 + share);
+  }
+
+  v4i kreg[NKS], vreg[NKS];
+  {
+    const int kr = imax(0, imin(key, n - 1));
+    const uint16_t* k = (const uint16_t*)a.k + (b * a.ks.b + hk * a.ks.h + (long long)kr * a.ks.n);
+    const uint16_t* v = (const uint16_t*)a.v + (b * a.vs.b + hk * a.vs.h + (long long)kr * a.vs.n);
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) {
+      kreg[s] = *reinterpret_cast<const v4i*>(k + 16 * s + 8 * hi);
+      vreg[s] = *reinterpret_cast<const v4i*>(v + 16 * s + 8 * hi);
+    }
+  }
+  const float f = ds_scale<BF16>(a, b, hk), f15 = f * 0x1p-15f;
+
+  constexpr int JR = 1024 / ROW, NJ = BT / JR, JW = NJ / W;
+  uint32_t qlo[JW], glo[JW];
+  const uint32_t qst = (uint32_t)(a.qs.n * 2), gst = (uint32_t)(a.gs.n * 2);
+#pragma unroll
+  for (int i = 0; i < JW; ++i) {
+    const int r = (wave + W * i) * JR + lane / CH, c = vswz<D>(r, lane % CH) * 16;
+    qlo[i] = r * qst + c;
+    glo[i] = r * gst + c;
+  }
+  auto issue = [&](int g, int tile, int stage) {
+    uint8_t* L = lds + stage * STAGE;
+    const int h = hk * G + g, qb = tile * BT;
+    const uint32_t rows = (uint32_t)imin(n - qb, BT);
+    const uint8_t* q = (const uint8_t*)a.q + 2 * (b * a.qs.b + h * a.qs.h) + (size_t)qb * qst;
+    const uint8_t* o = (const uint8_t*)a.dout + 2 * (b * a.gs.b + h * a.gs.h) + (size_t)qb * gst;
+    const __amdgpu_buffer_rsrc_t rq = make_rsrc(q, (rows - 1) * qst + ROW), rg = make_rsrc(o, (rows - 1) * gst + ROW);
+#pragma unroll
+    for (int i = 0; i < JW; ++i) {
+      buf_load16(rq, qlo[i], 0u, L + (wave + W * i) * 1024);
+      buf_load16(rg, glo[i], 0u, L + TB + (wave + W * i) * 1024);
+    }
+    const size_t at = ((size_t)b * a.Hq + h) * Np + qb;
+    if (wave == 0) buf_load4(make_rsrc(a.lb + at, BT * 4), 4 * lane, 0u, L + 2 * TB);
+    if (wave == 1) buf_load4(make_rsrc(a.delta + at, BT * 4), 4 * lane, 0u, L + 2 * TB + BT * 4);
+  };
+  uint32_t vo[NDB];
+  tr_offsets<D>(vo);
+  const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+
+  v16f dk[NDB], dv[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = v16f{};
+  int g = nt > 0 ? it0 / nt : 0, tile = nt > 0 ? t0 + it0 % nt : 0;
+  if (it0 < it1) issue(g, tile, 0);
+  for (int it = it0; it < it1; ++it) {
+    const int qb = tile * BT;
+    if (++tile == t1) { tile = t0; ++g; }
+    __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): this wave's loads of the tile have landed
+    __syncthreads();                                     // everyone's; every wave is past the tile before
+    const int st = (it - it0) & 1;
+    if (it + 1 < it1) issue(g, tile, st ^ 1);
+    const uint8_t* L = lds + st * STAGE;
+    const uint32_t lb = l0 + st * STAGE;
+    // queries [first, past) of the tile see this lane's key
+    const int first = key - qb, past = SINK ? BT : key + a.window - qb;
+    if constexpr (SINK) {
+      if (qb + 32 * wave + 31 < kw) continue;
+      if (qb + 32 * wave >= kw + 31) dkv_block<D, BF16, false>(L, lb, vo, wave, kreg, vreg, dk, dv, a.c2, f15, first, past);
+      else dkv_block<D, BF16, true>(L, lb, vo, wave, kreg, vreg, dk, dv, a.c2, f15, first, past);
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        const int q0 = qb + 32 * t;
+        if (q0 + 31 < kw || q0 >= kw + 31 + a.window) continue;
+        if (q0 >= kw + 31 && q0 + 31 < kw + a.window) dkv_block<D, BF16, false>(L, lb, vo, t, kreg, vreg, dk, dv, a.c2, f15, first, past);
+        else dkv_block<D, BF16, true>(L, lb, vo, t, kreg, vreg, dk, dv, a.c2, f15, first, past);
+      }
+    }
+  }
+
+  const float sv = BF16 ? 1.0f : 0x1p-15f, sk = a.rsd / f;
+  if constexpr (SINK) {
+    // add the two waves' sums; the chunk's part goes to the workspace
+    __syncthreads();
+    float* x = reinterpret_cast<float*>(lds);            // [2 D][32 keys] of wave 1
+    if (wave == 1) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          x[((db * 16 + e) * 2) * 64 + lane] = dk[db][e];
+          x[((db * 16 + e) * 2 + 1) * 64 + lane] = dv[db][e];
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+      float* part = a.part + ((((size_t)bh * nkb + k0 / KB) * a.chunks + chunk) * 2 * 32 + col) * D;
+      const bool live = key < n;                         // keys behind the end were read as copies of the last
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v4f y, z;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = (db * 16 + 4 * q + e) * 2;
+            y[e] = live ? (dk[db][4 * q + e] + x[r * 64 + lane]) * sk : 0.0f;
+            z[e] = live ? (dv[db][4 * q + e] + x[(r + 1) * 64 + lane]) * sv : 0.0f;
+          }
+          *reinterpret_cast<v4f*>(part + 32 * db + 8 * q + 4 * hi) = y;
+          *reinterpret_cast<v4f*>(part + 32 * D + 32 * db + 8 * q + 4 * hi) = z;
+        }
+    }
+  } else {
+    if (key >= a.N || key < a.sinks) return;             // the sinks' rows are join_sinks_kernel's
+    const bool live = key < n;
+    uint16_t* kr = (uint16_t*)a.dk + ((size_t)bh * a.N + key) * D;
+    uint16_t* vr = (uint16_t*)a.dv + ((size_t)bh * a.N + key) * D;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const v2u y = {pack16<BF16>(dk[db][4 * q] * sk, dk[db][4 * q + 1] * sk), pack16<BF16>(dk[db][4 * q + 2] * sk, dk[db][4 * q + 3] * sk)};
+        const v2u z = {pack16<BF16>(dv[db][4 * q] * sv, dv[db][4 * q + 1] * sv), pack16<BF16>(dv[db][4 * q + 2] * sv, dv[db][4 * q + 3] * sv)};
+        *reinterpret_cast<v2u*>(kr + 32 * db + 8 * q + 4 * hi) = live ? y : v2u{0u, 0u};
+        *reinterpret_cast<v2u*>(vr + 32 * db + 8 * q + 4 * hi) = live ? z : v2u{0u, 0u};
+      }
+  }
+}
+
+// Sink keys' dK and dV from the chunks' parts, in their order.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void join_sinks_kernel(const WindowBwd a) {
+  const int bh = blockIdx.y, nkb = cdiv(a.sinks, 32);
+  const int at = (blockIdx.x * 256 + threadIdx.x) * 2, key = at / D, d = at % D;
+  if (key >= a.sinks) return;
+  const float* p = a.part + (((size_t)bh * nkb + key / 32) * a.chunks * 2 * 32 + key % 32) * D + d;
+  float k0 = 0.0f, k1 = 0.0f, v0 = 0.0f, v1 = 0.0f;
+  for (int c = 0; c < a.chunks; ++c, p += 2 * 32 * D) {
+    k0 += p[0]; k1 += p[1];
+    v0 += p[32 * D]; v1 += p[32 * D + 1];
+  }
+  const size_t o = ((size_t)bh * a.N + key) * D + d;
+  *reinterpret_cast<uint32_t*>((uint16_t*)a.dk + o) = pack16<BF16>(k0, k1);
+  *reinterpret_cast<uint32_t*>((uint16_t*)a.dv + o) = pack16<BF16>(v0, v1);
+}
+
+// dQ: 4 waves x 32 queries, the forward's walk over the key tiles.
+//
+// delta comes from O in 16 bits, so it is off by d_i = sum_d dO_i (O rounded - O), and
+// every dS_ij by P_ij d_i: dQ would be off by d_i times the average key, which is
+// large where keys share an offset, as trained models' do.  But sum_j dS_ij = 0, so
+// any vector c may be taken off the keys: dQ_i = sum_j dS_ij K_j - c sum_j dS_ij,
+// where the second sum holds the rounded dS that the product took.  c is the mean
+// of the workgroup's last key tile.  (Error of dQ for keys N(0,1) with an N(0,1)
+// offset per channel, 8192 tokens, window 1024, bf16: 3.7e-3 without c.)
+template <int D, bool BF16>
+__global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
+  constexpr int W = 4, ROW = D * 2, CH = ROW / 16, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TB];   // two stages of a K tile and a V tile
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hi = lane >> 5;
+  const int nqt = cdiv(a.N, 32 * W);
+  const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
+  const unsigned lin = xcd * (total >> 3) + min(xcd, total & 7u) + (blockIdx.x >> 3);
+  const int bh = (int)(lin / nqt), b = bh / a.Hq, h = bh - b * a.Hq, hk = h / (a.Hq / a.Hkv);
+  const int qt = nqt - 1 - (int)(lin % nqt), q0 = qt * (32 * W), qw = q0 + wave * 32, qi = qw + col;
+  const int n = seq_len(a, b), win = a.window, sinks = a.sinks;
+  const TileList tl = q0 < n ? tile_list(q0 - win + 1, imin(q0 + 32 * W, n), sinks, BT) : TileList{0, 0, 0};
+
+  v4i qreg[NKS], greg[NKS];
+  const int qr = imax(0, imin(qi, n - 1));
+  {
+    const uint16_t* q = (const uint16_t*)a.q + (b * a.qs.b + h * a.qs.h + (long long)qr * a.qs.n);
+    const uint16_t* g = (const uint16_t*)a.dout + (b * a.gs.b + h * a.gs.h + (long long)qr * a.gs.n);
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) {
+      qreg[s] = *reinterpret_cast<const v4i*>(q + 16 * s + 8 * hi);
+      greg[s] = *reinterpret_cast<const v4i*>(g + 16 * s + 8 * hi);
+    }
+  }
+  const size_t at = ((size_t)b * a.Hq + h) * row_pad(a.N) + qr;
+  const float lb = a.lb[at] - kPShift<BF16>, dl = a.delta[at];
+  const float f = ds_scale<BF16>(a, b, hk), f15 = f * 0x1p-15f;
+
+  constexpr int JR = 1024 / ROW, NJ = BT / JR, JW = NJ / W;
+  uint32_t klo[JW], vlo[JW];
+  const uint32_t kst = (uint32_t)(a.ks.n * 2), vst = (uint32_t)(a.vs.n * 2);
+#pragma unroll
+  for (int i = 0; i < JW; ++i) {
+    const int r = (wave + W * i) * JR + lane / CH, c = vswz<D>(r, lane % CH) * 16;
+    klo[i] = r * kst + c;
+    vlo[i] = r * vst + c;
+  }
+  const uint8_t* kbase = (const uint8_t*)a.k + 2 * (b * a.ks.b + hk * a.ks.h);
+  const uint8_t* vbase = (const uint8_t*)a.v + 2 * (b * a.vs.b + hk * a.vs.h);
+  auto issue = [&](int kb, int stage) {
+    uint8_t* L = lds + stage * 2 * TB;
+    const uint32_t rows = (uint32_t)imin(n - kb, BT);
+    const __amdgpu_buffer_rsrc_t rk = make_rsrc(kbase + (size_t)kb * kst, (rows - 1) * kst + ROW);
+    const __amdgpu_buffer_rsrc_t rv = make_rsrc(vbase + (size_t)kb * vst, (rows - 1) * vst + ROW);
+#pragma unroll
+    for (int i = 0; i < JW; ++i) {
+      buf_load16(rk, klo[i], 0u, L + (wave + W * i) * 1024);
+      buf_load16(rv, vlo[i], 0u, L + TB + (wave + W * i) * 1024);
+    }
+  };
+  uint32_t vo[NDB];
+  tr_offsets<D>(vo);
+  const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  v16f dq[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dq[db] = v16f{};
+  float dsum = 0.0f;
+
+  if (tl.count > 0) issue(tl.tile(0) * BT, 0);
+  for (int j = 0; j < tl.count; ++j) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+    if (j + 1 < tl.count) issue(tl.tile(j + 1) * BT, (j + 1) & 1);
+    const uint8_t* L = lds + (j & 1) * 2 * TB;
+    const int kb = tl.tile(j) * BT;
+    static_for<2>([&](auto T_) {
+      constexpr int t = decltype(T_)::value;
+      const int kt = kb + 32 * t;
+      if (kt > qw + 31 || (kt + 32 <= qw - win + 1 && kt >= sinks)) return;
+      const int row = 32 * t + col;
+      v16f s = v16f{}, g = v16f{};
+#pragma unroll
+      for (int i = 0; i < NKS; ++i) s = mma32<BF16>(*reinterpret_cast<const v4i*>(L + row * ROW + vswz<D>(row, 2 * i + hi) * 16), qreg[i], s);
+#pragma unroll
+      for (int i = 0; i < NKS; ++i) g = mma32<BF16>(*reinterpret_cast<const v4i*>(L + TB + row * ROW + vswz<D>(row, 2 * i + hi) * 16), greg[i], g);
+      uint32_t dw[8];
+      const bool mask = kt + 31 > qw || kt + 32 > n || (kt <= qw + 31 - win && kt + 32 > sinks);
+      const int base = kt + 4 * hi, rem = imin(n, qi + 1) - base, low = qi - win + 1 - base, sk = sinks - base;
+      float d[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c2, -lb)), x = g[e] - dl;
+        d[e] = p * (BF16 ? x : x * f15);
+      }
+      if (mask) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int c = 8 * (e >> 2) + (e & 3);
+          d[e] = __uint_as_float(__float_as_uint(d[e]) & (uint32_t)(((c - rem) & ~((c - low) & ~(c - sk))) >> 31));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dw[e] = pack16<BF16>(d[2 * e], d[2 * e + 1]);
+        dsum = add_pair<BF16>(dw[e], dsum);
+      }
+      uint32_t va[NDB];
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) va[db] = vo[db] + l0 + (uint32_t)((j & 1) * 2 * TB);
+      static_for<2>([&](auto U_) {
+        constexpr int u = decltype(U_)::value;
+        const v4i dsk = {(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]};
+        v4i x[NDB];
+        tr_read<D, (32 * t + 16 * u) * ROW>(va, x);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) dq[db] = mma32<BF16>(x[db], dsk, dq[db]);
+      });
+    });
+  }
+  // c: the mean of the last tile's keys, summed in 256 / (D / 2) groups of rows
+  constexpr int NG = 512 / D;
+  float* const sums = reinterpret_cast<float*>(lds + (tl.count & 1) * 2 * TB);   // the stage that the last tile does not use
+  const int kl = tl.count > 0 ? tl.tile(tl.count - 1) * BT : 0;
+  if (tl.count > 0) {
+    const uint8_t* L = lds + ((tl.count - 1) & 1) * 2 * TB;
+    const int ch = tid % (D / 2), g = tid / (D / 2);
+    float x = 0.0f, y = 0.0f;
+    for (int r = g; r < imin(n - kl, BT); r += NG) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(L + r * ROW + vswz<D>(r, ch / 4) * 16 + 4 * (ch % 4));
+      x += widen<BF16>((uint16_t)w);
+      y += widen<BF16>((uint16_t)(w >> 16));
+    }
+    sums[g * D + 2 * ch] = x;
+    sums[g * D + 2 * ch + 1] = y;
+  }
+  __syncthreads();
+  if (qi >= a.N) return;
+  dsum += __shfl_xor(dsum, 32, 64);
+  dsum *= 1.0f / (float)imax(1, imin(n - kl, BT));
+  const float sq = a.rsd / f;
+  uint16_t* o = (uint16_t*)a.dq + (((size_t)b * a.Hq + h) * a.N + qi) * D;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      v4f c = v4f{};
+      if (tl.count > 0)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) c += *reinterpret_cast<const v4f*>(sums + g * D + 32 * db + 8 * q + 4 * hi);
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (dq[db][4 * q + e] - dsum * c[e]) * sq;
+      *reinterpret_cast<v2u*>(o + 32 * db + 8 * q + 4 * hi) = qi < n ? v2u{pack16<BF16>(x[0], x[1]), pack16<BF16>(x[2], x[3])} : v2u{0u, 0u};
+    }
+}
+
+// Chunks of the sinks' queries: enough workgroups for two per CU, at least 4 query
+// tiles each.
+int window_bwd_chunks(int B, int Hq, int Hkv, int N, int sinks) {
+  const long long blocks = (long long)B * Hkv * cdiv(sinks, 32), tiles = (long long)cdiv(N, BT) * (Hq / Hkv);
+  const long long want = 512 / (blocks > 0 ? blocks : 1), most = (tiles + 3) / 4;
+  return (int)imax(1, (int)(want < most ? want : most));
+}
+size_t window_bwd_row_floats(int B, int Hq, int N) { return (size_t)B * Hq * ((N + BT - 1) / BT * BT); }
+size_t window_bwd_norm_floats(int B, int Hq, int Hkv, int N) { return (size_t)B * (Hq + Hkv) * cdiv(N, PR); }
+size_t window_bwd_part_floats(int B, int Hq, int Hkv, int N, int D, int sinks) {
+  return (size_t)B * Hkv * cdiv(sinks, 32) * window_bwd_chunks(B, Hq, Hkv, N, sinks) * 2 * 32 * D;
+}
+
+template <int D, bool BF16>
+static hipError_t launch_window_bwd_t(const WindowBwd& a, hipStream_t st) {
+  hipLaunchKernelGGL((rows_kernel<D, BF16>), dim3((unsigned)cdiv(a.N, PR), (unsigned)(a.B * (a.Hq + (BF16 ? 0 : a.Hkv)))), dim3(256), 0,
+                     st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const unsigned heads = (unsigned)(a.B * a.Hkv);
+  hipLaunchKernelGGL((dkv_kernel<D, BF16, false>), dim3(heads * cdiv(a.N, 128)), dim3(256), 0, st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.sinks > 0) {
+    hipLaunchKernelGGL((dkv_kernel<D, BF16, true>), dim3(heads * cdiv(a.sinks, 32) * a.chunks), dim3(128), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL((join_sinks_kernel<D, BF16>), dim3((unsigned)cdiv(a.sinks * (D / 2), 256), heads), dim3(256), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((dq_kernel<D, BF16>), dim3((unsigned)(a.B * a.Hq) * cdiv(a.N, 128)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_window_bwd(const WindowBwd& a, int D, bool bf16, hipStream_t st) {
+  if (D == 128) return bf16 ? launch_window_bwd_t<128, true>(a, st) : launch_window_bwd_t<128, false>(a, st);
+  return bf16 ? launch_window_bwd_t<64, true>(a, st) : launch_window_bwd_t<64, false>(a, st);
+}
+
+}  // namespace sage

@@ -20,6 +20,22 @@ struct WindowFwd {
 };
 hipError_t launch_window_fwd(const WindowFwd& a, int D, bool bf16, hipStream_t st);
 
+struct WindowBwd {
+  const void *q, *k, *v, *o, *dout;
+  const float* lse;
+  const int32_t* lens;     // may be null
+  void *dq, *dk, *dv;      // contiguous
+  int B, Hq, Hkv, N, window, sinks, chunks;
+  Strides qs, ks, vs, os, gs;            // gs: dout
+  float c2, rsd;           // rsd = 1 / sqrt(D)
+  float *lb, *delta, *norms, *part;      // workspace
+};
+int window_bwd_chunks(int B, int Hq, int Hkv, int N, int sinks);
+size_t window_bwd_row_floats(int B, int Hq, int N);
+size_t window_bwd_norm_floats(int B, int Hq, int Hkv, int N);
+size_t window_bwd_part_floats(int B, int Hq, int Hkv, int N, int D, int sinks);
+hipError_t launch_window_bwd(const WindowBwd& a, int D, bool bf16, hipStream_t st);
+
 // A paged cache: pages of page_size tokens, strides in elements; int8 codes with
 // one fp32 scale per token and head ([pages, Hkv, page_size], contiguous) or 16-bit.
 struct Cache {

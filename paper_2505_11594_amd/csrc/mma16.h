@@ -29,6 +29,13 @@ __device__ __forceinline__ uint32_t pack16(float a, float b) {
   else return __builtin_bit_cast(uint32_t, v2h{(_Float16)a, (_Float16)b});
 }
 
+// c + the sum of a register's two 16-bit values.
+template <bool BF16>
+__device__ __forceinline__ float add_pair(uint32_t x, float c) {
+  if constexpr (BF16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, x), __builtin_bit_cast(v2bf, 0x3F803F80u), c, false);
+  else return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, x), __builtin_bit_cast(v2h, 0x3C003C00u), c, false);
+}
+
 // Probabilities enter the second product in 16 bits.  In fp16 they are carried
 // 2^15 larger: probabilities down to 2^-29 of the row's maximum stay normal
 // numbers instead of those above 2^-14 only, and the largest is 2^15 < 65504.  The

@@ -92,6 +92,21 @@ sage::Cache cache_of(const sage_kv_cache* c, const int32_t* table, int max_pages
   return r;
 }
 
+struct BwdWs {
+  size_t lb, delta, norms, part, total;
+};
+BwdWs bwd_ws(int B, int Hq, int Hkv, int N, int D, int sinks) {
+  BwdWs w;
+  size_t off = 0;
+  const size_t rows = up256(sage::window_bwd_row_floats(B, Hq, N) * sizeof(float));
+  w.lb = off; off += rows;
+  w.delta = off; off += rows;
+  w.norms = off; off += up256(sage::window_bwd_norm_floats(B, Hq, Hkv, N) * sizeof(float));
+  w.part = off; off += up256(sage::window_bwd_part_floats(B, Hq, Hkv, N, D, sinks) * sizeof(float));
+  w.total = off;
+  return w;
+}
+
 struct DecodeWs {
   size_t part, lse2, scores, total;
   long long score_stride;
@@ -133,6 +148,47 @@ int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, f
   a.c2 = softmax_c2(D);
   clamp_window(N, &a.window, &a.sinks);
   return hip_status(sage::launch_window_fwd(a, D, (flags & SAGE_IN_BF16) != 0, stream));
+}
+
+size_t sage_attn_window_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
+  if (check_window(B, Hq, Hkv, N, D, window, sinks) != SAGE_OK) return 0;
+  clamp_window(N, &window, &sinks);
+  return bwd_ws(B, Hq, Hkv, N, D, sinks).total;
+}
+
+int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout,
+                         const int32_t* lens, void* dq, void* dk, void* dv, int B, int Hq, int Hkv, int N, int D,
+                         int window, int sinks, unsigned flags, const sage_strides* q_strides,
+                         const sage_strides* k_strides, const sage_strides* v_strides, const sage_strides* o_strides,
+                         const sage_strides* dout_strides, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (flags & ~(unsigned)SAGE_IN_BF16) return SAGE_ERR_INVALID_ARG;
+  const int rc = check_window(B, Hq, Hkv, N, D, window, sinks);
+  if (rc != SAGE_OK) return rc;
+  if (!lse || !aligned(lse, 4) || !aligned(lens, 4)) return SAGE_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, o, dout, (const void*)dq, (const void*)dk, (const void*)dv})
+    if (!p || !aligned(p, 16)) return SAGE_ERR_INVALID_ARG;
+  if ((long long)B * (Hq + Hkv) > 65535) return SAGE_ERR_INVALID_ARG;
+  sage::WindowBwd a;
+  a.q = q; a.k = k; a.v = v; a.o = o; a.dout = dout; a.lse = lse; a.lens = lens; a.dq = dq; a.dk = dk; a.dv = dv;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.N = N; a.window = window; a.sinks = sinks;
+  a.qs = strides_or(q_strides, Hq, N, D); a.ks = strides_or(k_strides, Hkv, N, D);
+  a.vs = strides_or(v_strides, Hkv, N, D); a.os = strides_or(o_strides, Hq, N, D);
+  a.gs = strides_or(dout_strides, Hq, N, D);
+  for (const Strides& s : {a.qs, a.ks, a.vs, a.os, a.gs})
+    if (!strides_ok(s, 8, kMaxRowStride)) return SAGE_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
+  clamp_window(N, &a.window, &a.sinks);
+  const BwdWs w = bwd_ws(B, Hq, Hkv, N, D, a.sinks);
+  if (workspace_bytes < w.total) return SAGE_ERR_WORKSPACE;
+  uint8_t* base = static_cast<uint8_t*>(workspace);
+  a.lb = reinterpret_cast<float*>(base + w.lb);
+  a.delta = reinterpret_cast<float*>(base + w.delta);
+  a.norms = reinterpret_cast<float*>(base + w.norms);
+  a.part = reinterpret_cast<float*>(base + w.part);
+  a.chunks = sage::window_bwd_chunks(B, Hq, Hkv, N, a.sinks);
+  a.c2 = softmax_c2(D);
+  a.rsd = (float)(1.0 / std::sqrt((double)D));
+  return hip_status(sage::launch_window_bwd(a, D, (flags & SAGE_IN_BF16) != 0, stream));
 }
 
 int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,

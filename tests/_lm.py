@@ -18,22 +18,52 @@ def visible(i, j, n, window, sinks):
     return w if window is None else w & ((j > i - window) | (j < sinks))
 
 
-def window_attention(q, k, v, window, sinks, n, dout=None):
+def window_attention(q, k, v, window, sinks, n, dout=None, u=0.0):
     """One sequence and head: q, k, v [N, D] in 64 bits.  Returns a dict with o, lse, p,
-    the score's error bound e and, with dout, dq, dk, dv and the terms of their bounds."""
+    the score's error bound e and, with dout, the gradients and bounds of their errors
+    before the last rounding (u: the 16-bit type's)."""
     import torch
     N, D = q.shape
     at = torch.arange(N, device=q.device)
     see = visible(at[:, None], at[None, :], n, window, sinks) & (at[:, None] < n)
-    k, v = k.clone(), v.clone()
-    k[n:], v[n:] = 0, 0
+    q, k, v = q.clone(), k.clone(), v.clone()
+    q[n:], k[n:], v[n:] = 0, 0, 0
     s = torch.where(see, q @ k.T / math.sqrt(D), -math.inf)
     m = s.amax(-1, keepdim=True).clamp_min(-1e300)
     x = torch.exp(s - m)
     l = x.sum(-1, keepdim=True)
     p = x / torch.where(l > 0, l, 1.0)
     e = (D + 4) * 2.0 ** -24 * torch.where(see, q.abs() @ k.abs().T, 0.0).amax(-1, keepdim=True) / math.sqrt(D)
-    return {"o": p @ v, "lse": (m + torch.log(l))[:, 0], "p": p, "e": e, "av": p @ v.abs(), "see": see}
+    r = {"o": p @ v, "lse": (m + torch.log(l))[:, 0], "p": p, "e": e, "av": p @ v.abs(), "see": see}
+    if dout is None:
+        return r
+    # Gradients and their bounds.  P: relative rho (as for O), and u where it meets dO.  dP: D exact
+    # products.  delta: O is off by o_bound.  dS = P (dP - delta): both errors, and u for its rounding
+    # (in fp16 its power of two leaves at most 2^-38 max|dO| max|V| of underflow).  Sums of N terms.
+    g = dout.clone()
+    g[n:] = 0
+    f, rd = 2.0 ** -24, 1 / math.sqrt(D)
+    rho = 2 * e + 2 * (N + 64) * f
+    dp, delta = g @ v.T, (g * r["o"]).sum(-1, keepdim=True)
+    ds = p * (dp - delta)
+    e_dp = (D + 4) * f * (g.abs() @ v.abs().T)
+    e_delta = (g.abs() * o_bound(r, n, u)).sum(-1, keepdim=True) + (D + 4) * f * (g.abs() * r["o"].abs()).sum(-1, keepdim=True)
+    low = 2.0 ** -38 * float(g.norm(dim=-1).max() * v.norm(dim=-1).max()) if n else 0.0
+    e_ds = (rho + u) * ds.abs() + (1 + u) * p * (e_dp + e_delta) + torch.where(see, low, 0.0)
+    r["dq"], r["dk"], r["dv"] = ds @ k * rd, ds.T @ q * rd, p.T @ g
+    # dQ_i = sum_j dS_ij (K_j - c) for any c, as sum_j dS_ij = 0: the kernel's is the sum over its
+    # rounded dS, off by sum_j e_ij |K_j - c|.  Its c is the mean of the last 64-key tile that the
+    # workgroup of 128 queries reads.
+    edq = torch.zeros_like(r["dq"])
+    for q0 in range(0, n, 128):
+        last = min(q0 + 128, n)
+        tile = k[(last - 1) // 64 * 64:min(n, (last - 1) // 64 * 64 + 64)]
+        c, rows = tile.mean(0, keepdim=True), slice(q0, last)
+        edq[rows] = e_ds[rows] @ (k - c).abs() + (N + 64) * f * (ds[rows].abs() @ (k.abs() + c.abs()))
+    r["edq"] = edq * rd
+    r["edk"] = (e_ds + N * f * ds.abs()).T @ q.abs() * rd
+    r["edv"] = ((rho + u + N * f) * p).T @ g.abs()
+    return r
 
 
 def unit(dtype):

@@ -86,6 +86,154 @@ def test_window_forward(case):
     check_window(q, k, v, o, lse, window, sinks, lens, "window %s" % (case,))
 
 
+def check_grads(q, k, v, dout, grads, window, sinks, lens, label):
+    """dQ, dK, dV within their bounds; returns the references and bounds for other uses."""
+    import torch
+    B, Hq, N, D = q.shape
+    Hkv = k.shape[1]
+    G, u = Hq // Hkv, _lm.unit(q.dtype)
+    want = [torch.zeros(x.shape, dtype=torch.float64, device=x.device) for x in (q, k, v)]
+    bound = [torch.zeros_like(x) for x in want]
+    for b in range(B):
+        n = N if lens is None else max(0, min(N, int(lens[b])))
+        for h in range(Hq):
+            r = _lm.window_attention(q[b, h].double(), k[b, h // G].double(), v[b, h // G].double(), window, sinks, n,
+                                     dout[b, h].double(), u)
+            for i, (x, hh) in enumerate((("dq", h), ("dk", h // G), ("dv", h // G))):
+                want[i][b, hh] += r[x]
+                bound[i][b, hh] += r["e" + x]
+    worst = []
+    for x, w, t in zip(grads, want, bound):
+        t = t + u * (w.abs() + t) + torch.finfo(x.dtype).smallest_normal * 2.0 ** -10
+        worst.append(float(((x.double() - w).abs() / t).max()))
+        for b in range(B):
+            n = N if lens is None else max(0, min(N, int(lens[b])))
+            assert bool((x[b, :, n:] == 0).all()), label
+    say("%s: dQ at %.3f of its bound, dK %.3f, dV %.3f" % (label, *worst))
+    assert max(worst) <= 1, label
+    return want, bound
+
+
+@pytest.mark.parametrize("case", WINDOWS)
+def test_window_backward(case):
+    import torch
+    B, Hq, Hkv, N, D, dtype, window, sinks, lens = case
+    q, k, v = qkv(12 + N + D, B, Hq, Hkv, N, D, dtype)
+    dout = randn(gen(N), B, Hq, N, D).to(q.dtype)
+    ln = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    say("backward %s" % (case,))
+    o, lse = bd.sage_attn_window_fwd(q, k, v, window=window, sinks=sinks, lens=ln)
+    grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=window, sinks=sinks, lens=ln)
+    torch.cuda.synchronize()
+    want, bound = check_grads(q, k, v, dout, grads, window, sinks, lens, "backward %s" % (case,))
+    again = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=window, sinks=sinks, lens=ln)
+    assert all(torch.equal(a, b) for a, b in zip(grads, again))
+    # against differences of the definition in 64 bits, along one direction
+    d = [randn(gen(N + i), *x.shape).double() for i, x in enumerate((q, k, v))]
+
+    def loss(t):
+        x, y, z = (a.double() + t * b for a, b in zip((q, k, v), d))
+        s = 0.0
+        for b in range(B):
+            n = N if lens is None else max(0, min(N, int(lens[b])))
+            for h in range(Hq):
+                kv = h * Hkv // Hq
+                s += float((_lm.window_attention(x[b, h], y[b, kv], z[b, kv], window, sinks, n)["o"] * dout[b, h].double())[:n].sum())
+        return s
+
+    t = 1e-4
+    slope = (loss(t) - loss(-t)) / (2 * t)
+    got = sum(float((g.double() * x).sum()) for g, x in zip(grads, d))
+    u = _lm.unit(q.dtype)
+    tol = sum(float(((e + u * (w.abs() + e)) * x.abs()).sum()) for e, w, x in zip(bound, want, d))
+    # a difference of second order in t, whose third derivative the scores bound loosely; rounding of the losses
+    scale = sum(float((w.abs() * x.abs()).sum()) for w, x in zip(want, d))
+    assert abs(got - slope) <= tol + 1e-3 * scale + 1e-6, (got, slope, tol)
+
+
+@pytest.mark.parametrize("dtype,scale", [("fp16", 1e-4), ("fp16", 3e2), ("bf16", 1e-6), ("bf16", 1e6)])
+def test_window_backward_small_and_large_gradients(dtype, scale):
+    """dO far from 1, its rows of very different size: fp16's dS keeps its precision."""
+    import torch
+    q, k, v = qkv(60, 1, 4, 2, 333, 64, dtype)
+    dout = (randn(gen(61), 1, 4, 333, 64) * scale * torch.exp(randn(gen(62), 1, 4, 333, 1))).to(q.dtype)
+    o, lse = bd.sage_attn_window_fwd(q, k, v, window=100, sinks=5)
+    grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=100, sinks=5)
+    torch.cuda.synchronize()
+    check_grads(q, k, v, dout, grads, 100, 5, None, "dO x %g" % scale)
+    zero = bd.sage_attn_window_bwd(q, k, v, o, lse, torch.zeros_like(dout), window=100, sinks=5)
+    assert all(bool((x == 0).all()) for x in zero)
+
+
+def test_window_backward_strides_padding_and_buffers():
+    """[B, N, H, D] tensors and given buffers: the bits of contiguous copies; what lies behind a
+    sequence's end (NaN here) is not read; gradients of broadcast heads add up to the group's."""
+    import torch
+    B, Hq, Hkv, N, D = 2, 4, 2, 200, 128
+    q, k, v = qkv(70, B, Hq, Hkv, N, D, "bf16")
+    dout = randn(gen(71), B, Hq, N, D).to(q.dtype)
+    lens = torch.tensor([200, 77], dtype=torch.int32, device="cuda")
+    kw = dict(window=50, sinks=40, lens=lens)
+    o, lse = bd.sage_attn_window_fwd(q, k, v, **kw)
+    ref = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, **kw)
+    tr = [x.transpose(1, 2).contiguous().transpose(1, 2) for x in (q, k, v, o, dout)]
+    bad = [x.clone() for x in tr]
+    for x in bad:
+        x[1, :, 77:] = float("nan")
+    lb = lse.clone()
+    lb[1, :, 77:] = float("nan")
+    ws = torch.full((bd.attn_window_bwd_workspace_size(B, Hq, Hkv, N, D, 50, 40),), 255, dtype=torch.uint8, device="cuda")
+    out = [torch.full_like(x, 3.0) for x in ref]
+    for t, l in ((tr, lse), (bad, lb)):
+        got = bd.sage_attn_window_bwd(t[0], t[1], t[2], t[3], l, t[4], workspace=ws, out=out, **kw)
+        torch.cuda.synchronize()
+        assert all(a is b for a, b in zip(got, out)) and all(torch.equal(a, b) for a, b in zip(got, ref))
+        for x in out:
+            x.fill_(5.0)
+    wide = [x.repeat_interleave(2, 1) for x in (k, v)]
+    o2, lse2 = bd.sage_attn_window_fwd(q, *wide, **kw)
+    assert torch.equal(o2, o) and torch.equal(lse2, lse)
+    g2 = bd.sage_attn_window_bwd(q, *wide, o, lse, dout, **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(g2[0], ref[0])
+    for a, b in zip(g2[1:], ref[1:]):
+        a = a.float().view(B, Hkv, 2, N, D)
+        lim = 2.0 ** -8 * (a.abs().sum(2) + b.float().abs()) + 2.0 ** -18 * float(a.abs().max())
+        assert bool(((a.sum(2) - b.float()).abs() <= lim).all())
+
+
+def test_window_training_step_captured():
+    """Forward and backward captured into one graph; replayed with new inputs, eager calls between."""
+    import torch
+    q, k, v = qkv(80, 1, 4, 2, 300, 64, "fp16")
+    dout = torch.zeros_like(q)
+    o, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    out = [torch.empty_like(x) for x in (q, k, v)]
+    ws = torch.empty(bd.attn_window_bwd_workspace_size(1, 4, 2, 300, 64, 90, 3), dtype=torch.uint8, device="cuda")
+
+    def step():
+        bd.sage_attn_window_fwd(q, k, v, window=90, sinks=3, out=o, lse_out=lse)
+        bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=90, sinks=3, workspace=ws, out=out)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    g = gen(81)
+    for i in range(4):
+        for x in (q, k, v, dout):
+            x.copy_(randn(g, *x.shape))
+        graph.replay()
+        oe, le = bd.sage_attn_window_fwd(q, k, v, window=90, sinks=3)
+        ge = bd.sage_attn_window_bwd(q, k, v, oe, le, dout, window=90, sinks=3)
+        torch.cuda.synchronize()
+        assert torch.equal(o, oe) and torch.equal(lse, le) and all(torch.equal(a, b) for a, b in zip(out, ge)), i
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_window_forward_strides(dtype):
     """[B, N, H, D] tensors, heads broadcast from one, a slice of a longer buffer, an output of other
