@@ -376,10 +376,12 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
 }
 
 // Sequences whose steps several workgroups shared: O = sum O_w 2^(m_w - m) / l.
-// One workgroup per (sequence, query head).
+// One workgroup per (sequence, query head); its waves take every fourth part.
 template <int D, bool BF16>
-__global__ __launch_bounds__(64) void join_kernel(const Decode a, float shift) {
-  const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
+__global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) {
+  constexpr int CL = D / 64;                             // channels per lane
+  __shared__ float sums[4][D + 1];
+  const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Line line = steps_line(a);
   int n;
   const int steps = cdiv(seq_tiles(a, s, &n).count, DW);
@@ -389,32 +391,38 @@ __global__ __launch_bounds__(64) void join_kernel(const Decode a, float shift) {
     if (s0 + lane < s) c = cdiv(seq_tiles(a, s0 + lane, &nn).count, DW);
     before += wave_sum(c);
   }
-  uint16_t* o = (uint16_t*)a.o + ((size_t)s * a.Hq + h) * D + lane * (D / 64);
-  float l2 = -INFINITY, x[D / 64] = {};
-  if (steps > 0) {
-    const int w0 = (int)(before / line.share), w1 = (int)((before + steps - 1) / line.share);
-    if (w0 == w1) return;                                // final already
-    const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
-    // a share's slot 1 if the sequence begins in it, slot 0 if it began before
-    auto at = [&](int w) { return ((size_t)w * 2 + (w == w0 ? 1 : 0)) * a.Hq + h; };
-    float m = -INFINITY, l = 0.0f;
-    for (int w = w0 + lane; w <= w1; w += 64) m = smax(m, ml[at(w) * 2]);
+  const int w0 = steps > 0 ? (int)(before / line.share) : 0, w1 = steps > 0 ? (int)((before + steps - 1) / line.share) : -1;
+  if (w0 == w1) return;                                  // final already
+  const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
+  // a share's slot 1 if the sequence begins in it, slot 0 if it began before
+  auto at = [&](int w) { return ((size_t)w * 2 + (w == w0 ? 1 : 0)) * a.Hq + h; };
+  float m = -INFINITY, l = 0.0f, x[CL] = {};
+  for (int w = w0 + lane; w <= w1; w += 64) m = smax(m, ml[at(w) * 2]);
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) m = smax(m, __shfl_xor(m, d, 64));
-    const float mc = m == -INFINITY ? 0.0f : m;
-    for (int w = w0; w <= w1; ++w) {
-      const float f = __builtin_amdgcn_exp2f(ml[at(w) * 2] - mc);
-      l += ml[at(w) * 2 + 1] * f;
-      const float* p = a.part + at(w) * D + lane * (D / 64);
+  for (int d = 32; d >= 1; d >>= 1) m = smax(m, __shfl_xor(m, d, 64));
+  const float mc = m == -INFINITY ? 0.0f : m;
+#pragma unroll 8
+  for (int w = w0 + wave; w <= w1; w += 4) {
+    const float f = __builtin_amdgcn_exp2f(ml[at(w) * 2] - mc);
+    l += ml[at(w) * 2 + 1] * f;
+    const float* p = a.part + at(w) * D + lane * CL;
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) x[i] += p[i] * f;
-    }
-    if (l > 0.0f || l != l) {
-      l2 = m + (__builtin_log2f(l) - shift);
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) x[i] /= l;
-    }
+    for (int i = 0; i < CL; ++i) x[i] += p[i] * f;
   }
+#pragma unroll
+  for (int i = 0; i < CL; ++i) sums[wave][lane * CL + i] = x[i];
+  if (lane == 0) sums[wave][D] = l;
+  __syncthreads();
+  if (wave > 0) return;
+  l = (sums[0][D] + sums[1][D]) + (sums[2][D] + sums[3][D]);
+  const float l2 = l > 0.0f || l != l ? m + (__builtin_log2f(l) - shift) : -INFINITY;
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int i = 0; i < CL; ++i) {
+    const int c = lane * CL + i;
+    x[i] = ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])) * inv;
+  }
+  uint16_t* o = (uint16_t*)a.o + ((size_t)s * a.Hq + h) * D + lane * CL;
   if constexpr (D == 128) *reinterpret_cast<uint32_t*>(o) = pack16<BF16>(x[0], x[1]);
   else *o = (uint16_t)pack16<BF16>(x[0], 0.0f);
   if (lane == 0) {
@@ -464,7 +472,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
     const float shift = a.c.k_scale ? 0.0f : kPShift<BF16>;
-    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(64), 0, st, a, shift);
+    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.weights) {
