@@ -377,8 +377,9 @@ int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, f
                          const sage_strides* q_strides, const sage_strides* k_strides, const sage_strides* v_strides,
                          const sage_strides* o_strides, hipStream_t stream);
 
-/* Workspace bytes for sage_attn_window_bwd (two fp32 values per query row, and
- * parts of the sinks' gradients); 0 for invalid arguments.  Host only. */
+/* Workspace bytes for sage_attn_window_bwd (two fp32 values per query row, and fp32
+ * parts of the gradients of keys whose queries several workgroups share: the sinks',
+ * and all keys' of small batches); 0 for invalid arguments.  Host only. */
 size_t sage_attn_window_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D, int window, int sinks);
 
 /*
@@ -456,6 +457,9 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
                            int sinks, float* weights, int64_t weights_stride, unsigned flags, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);
 
+/* Workspace bytes for sage_kv_evict; 0 for invalid arguments.  Host only. */
+size_t sage_kv_evict_workspace_size(int S, int Hkv, int max_pages, int page_size);
+
 /*
  * sage_kv_evict -- shorten cached sequences to `budget` tokens.  Per sequence of
  * more than that, and per head: its first keep_first and last keep_last tokens
@@ -470,11 +474,13 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
  *               positions, -1 behind the last; new_weights: fp32 [S, Hkv,
  *               new_max_pages * page_size], their weights, 0 behind the last.
  *               None of them overlaps an input
+ *  workspace  : at least sage_kv_evict_workspace_size() bytes, 256-byte aligned
  * keep_first + keep_last <= budget.  Source pages are left as they were.
  */
 int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
                   int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
-                  int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, hipStream_t stream);
+                  int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream);
 
 /* Human-readable status name; never NULL. */
 const char* sage_status_string(int status);

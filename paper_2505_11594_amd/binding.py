@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsage_mi355x.so")
@@ -31,14 +32,8 @@ SAGE_ROLE_Q, SAGE_ROLE_K, SAGE_ROLE_V = 0, 1, 2
 _lib = None
 
 
-class _Strides(ctypes.Structure):
-    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("n", ctypes.c_int64)]
-
-
-class _Cache(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
-                ("k_strides", _Strides), ("v_strides", _Strides),
-                ("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("Hkv", ctypes.c_int), ("D", ctypes.c_int)]
+_strides = struct.Struct("@3q").pack      # sage_strides
+_cache = struct.Struct("@4P6q4i").pack    # sage_kv_cache
 
 
 class SageError(RuntimeError):
@@ -87,7 +82,7 @@ def lib():
         L.sage_attn_int8_bwd_workspace_size.restype = sz
         L.sage_attn_int8_bwd_min_workspace_size.argtypes = [i, i, i, i, u]
         L.sage_attn_int8_bwd_min_workspace_size.restype = sz
-        i64, st, ca = ctypes.c_int64, ctypes.POINTER(_Strides), ctypes.POINTER(_Cache)
+        i64, st, ca = ctypes.c_int64, vp, vp           # (sage_strides and sage_kv_cache by address)
         L.sage_attn_window_fwd.argtypes = [vp] * 6 + [i] * 7 + [u] + [st] * 4 + [vp]
         L.sage_attn_window_bwd_workspace_size.argtypes = [i] * 7
         L.sage_attn_window_bwd_workspace_size.restype = sz
@@ -96,7 +91,9 @@ def lib():
         L.sage_attn_paged_decode_workspace_size.argtypes = [i] * 7
         L.sage_attn_paged_decode_workspace_size.restype = sz
         L.sage_attn_paged_decode.argtypes = [ca, vp, i64, i64, vp, vp, vp, i, vp, i, i, i, i, vp, i64, u, vp, sz, vp]
-        L.sage_kv_evict.argtypes = [ca, vp, i, vp, vp, i64, vp, i, i, i, i, vp, vp, vp, i, vp]
+        L.sage_kv_evict_workspace_size.argtypes = [i] * 4
+        L.sage_kv_evict_workspace_size.restype = sz
+        L.sage_kv_evict.argtypes = [ca, vp, i, vp, vp, i64, vp, i, i, i, i, vp, vp, vp, i, vp, sz, vp]
         L.sage_status_string.argtypes = [i]
         L.sage_status_string.restype = ctypes.c_char_p
         L.sage_version.restype = ctypes.c_char_p
@@ -413,30 +410,38 @@ _NO_WINDOW = 2 ** 31 - 1
 def _call(fn: str, device, *args):
     """The C call on ``device`` and its current stream."""
     import torch
-    stream = ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
-    if torch.cuda.current_device() == device.index:
+    index = device.index
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch.cuda.current_device() == index:
         rc = getattr(lib(), fn)(*args, stream)
     else:
         with torch.cuda.device(device):
             rc = getattr(lib(), fn)(*args, stream)
-    _check(fn, rc)
+    if rc != SAGE_OK:
+        raise SageError(fn, rc)
+
+
+def _adr(t):
+    return t.data_ptr() if t is not None else None
 
 
 def _rows(t, what: str, ndim: int = 4):
-    """A strided tensor with contiguous channels whose rows start on 16 bytes: its strides but the last."""
+    """A strided tensor with contiguous channels whose rows start on 16 bytes: its strides but the
+    last (of a dimension of size 1, whose stride is never used, 0)."""
     if t.dim() != ndim or not t.is_cuda or t.numel() == 0:
         raise ValueError("%s must be a non-empty %d-d device tensor, got shape %s on %s"
                          % (what, ndim, tuple(t.shape), t.device))
-    # the stride of a dimension of size 1 is never used
-    s = tuple(x if n > 1 else n * 0 for x, n in zip(t.stride(), t.shape))
-    if (t.shape[-1] > 1 and s[-1] != 1) or any(x * t.element_size() % 16 for x in s[:-1]) or t.data_ptr() % 16:
+    s, n = t.stride(), t.shape
+    s, last = [x if y > 1 else 0 for x, y in zip(s, n[:-1])], s[-1]
+    mask = 16 // t.element_size() - 1
+    if last != 1 or t.data_ptr() & 15 or any([x & mask for x in s]):
         raise ValueError("%s must have contiguous channels and rows on 16-byte addresses, got strides %s"
                          % (what, tuple(t.stride())))
-    return s[:-1]
+    return s
 
 
 def _same(t, like, what: str, shape):
-    if t.dtype != like.dtype or t.device != like.device or tuple(t.shape) != tuple(shape):
+    if t.dtype != like.dtype or t.device != like.device or t.shape != shape:
         raise ValueError("%s must be a %s tensor of shape %s on %s, got %s %s on %s"
                          % (what, like.dtype, tuple(shape), like.device, t.dtype, tuple(t.shape), t.device))
 
@@ -459,7 +464,7 @@ def _check_window_args(q, k, v, lens):
         _same(t, q, what, (B, Hkv, N, D))
     if lens is not None:
         _check_tensor(lens, "lens", (B,), torch.int32, q.device)
-    return (B, Hq, Hkv, N, D), [_Strides(*x) for x in (qs, ks, vs)]
+    return (B, Hq, Hkv, N, D), [_strides(*x) for x in (qs, ks, vs)]
 
 
 def sage_attn_window_fwd(q, k, v, window=None, sinks: int = 0, lens=None, lse: bool = True, out=None, lse_out=None):
@@ -474,12 +479,12 @@ def sage_attn_window_fwd(q, k, v, window=None, sinks: int = 0, lens=None, lse: b
     window, sinks = _window_of(window, sinks)
     o = torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device) if out is None else out
     _same(o, q, "out", (B, Hq, N, D))
-    st.append(_Strides(*_rows(o, "out")))
+    st.append(_strides(*_rows(o, "out")))
     L = None
     if lse:
         L = torch.empty((B, Hq, N), dtype=torch.float32, device=q.device) if lse_out is None else lse_out
         _check_tensor(L, "lse_out", (B, Hq, N), torch.float32, q.device)
-    _call("sage_attn_window_fwd", q.device, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(L), _ptr(lens), B, Hq, Hkv, N, D,
+    _call("sage_attn_window_fwd", q.device, _adr(q), _adr(k), _adr(v), _adr(o), _adr(L), _adr(lens), B, Hq, Hkv, N, D,
           window, sinks, flags, *st)
     return o, L
 
@@ -500,7 +505,7 @@ def sage_attn_window_bwd(q, k, v, o, lse, dout, window=None, sinks: int = 0, len
     window, sinks = _window_of(window, sinks)
     for t, what in ((o, "o"), (dout, "dout")):
         _same(t, q, what, (B, Hq, N, D))
-        st.append(_Strides(*_rows(t, what)))
+        st.append(_strides(*_rows(t, what)))
     _check_tensor(lse, "lse", (B, Hq, N), torch.float32, q.device)
     shapes = ((B, Hq, N, D), (B, Hkv, N, D), (B, Hkv, N, D))
     dq, dk, dv = out if out is not None else [torch.empty(s, dtype=q.dtype, device=q.device) for s in shapes]
@@ -510,13 +515,13 @@ def sage_attn_window_bwd(q, k, v, o, lse, dout, window=None, sinks: int = 0, len
         n = attn_window_bwd_workspace_size(B, Hq, Hkv, N, D, window, sinks)
         workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=q.device)
     _check_workspace(workspace, q.device)
-    _call("sage_attn_window_bwd", q.device, *[_ptr(t) for t in (q, k, v, o, lse, dout, lens, dq, dk, dv)], B, Hq, Hkv, N, D,
-          window, sinks, flags, *st, _ptr(workspace), workspace.numel())
+    _call("sage_attn_window_bwd", q.device, *[_adr(t) for t in (q, k, v, o, lse, dout, lens, dq, dk, dv)], B, Hq, Hkv, N, D,
+          window, sinks, flags, *st, _adr(workspace), workspace.numel())
     return dq, dk, dv
 
 
 def _check_cache(k_cache, v_cache, k_scale, v_scale, table):
-    """The C description of a paged cache, and the table's shape."""
+    """The C description of a paged cache, and (S, max_pages, page_size, Hkv, D)."""
     import torch
     ks, vs = _rows(k_cache, "k_cache"), _rows(v_cache, "v_cache")
     P, Hkv, page, D = k_cache.shape
@@ -525,16 +530,16 @@ def _check_cache(k_cache, v_cache, k_scale, v_scale, table):
     if (k_scale is None) != (v_scale is None) or (k_cache.dtype == torch.int8) != (k_scale is not None):
         raise ValueError("an int8 cache has k_scale and v_scale, a 16-bit one has neither")
     if k_scale is not None:
-        for t, what in ((k_scale, "k_scale"), (v_scale, "v_scale")):
-            _check_tensor(t, what, (P, Hkv, page), torch.float32, dev)
+        _check_tensor(k_scale, "k_scale", (P, Hkv, page), torch.float32, dev)
+        _check_tensor(v_scale, "v_scale", (P, Hkv, page), torch.float32, dev)
     else:
         _in_flag(k_cache)
     if table.dim() != 2 or table.numel() == 0:
         raise ValueError("table must be a non-empty [S, max_pages] tensor")
-    _check_tensor(table, "table", table.shape, torch.int32, dev)
-    ptr = lambda t: t.data_ptr() if t is not None else None
-    c = _Cache(ptr(k_cache), ptr(v_cache), ptr(k_scale), ptr(v_scale), _Strides(*ks), _Strides(*vs), P, page, Hkv, D)
-    return c, int(table.shape[0]), int(table.shape[1])
+    S, M = table.shape
+    _check_tensor(table, "table", (S, M), torch.int32, dev)
+    return _cache(k_cache.data_ptr(), v_cache.data_ptr(), _adr(k_scale) or 0, _adr(v_scale) or 0, *ks, *vs, P, page, Hkv, D), \
+        (S, M, page, Hkv, D)
 
 
 def _check_weights(w, what: str, S: int, Hkv: int, capacity: int, device):
@@ -551,21 +556,21 @@ def sage_kv_append(k, v, k_cache, v_cache, table, pos, counts=None, k_scale=None
     [S, max_pages] holds the sequences' pages.  ``weights`` [S, Hkv, >= max_pages * page_size] is set
     to 0 at the new tokens."""
     import torch
-    c, S, M = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
     flags = _in_flag(k)
     ks, vs = _rows(k, "k"), _rows(v, "v")
     N, dev = int(k.shape[2]), k_cache.device
-    _same(v, k, "v", (S, c.Hkv, N, c.D))
-    _same(k, v, "k", (S, c.Hkv, N, c.D))
+    _same(v, k, "v", (S, Hkv, N, D))
+    _same(k, v, "k", (S, Hkv, N, D))
     if k.device != dev or (k_scale is None and k.dtype != k_cache.dtype):
         raise ValueError("k and v must be on %s and of the cache's type" % dev)
     _check_tensor(pos, "pos", (S,), torch.int32, dev)
     if counts is not None:
         _check_tensor(counts, "counts", (S,), torch.int32, dev)
     if weights is not None:
-        _check_weights(weights, "weights", S, c.Hkv, M * c.page_size, dev)
-    _call("sage_kv_append", dev, ctypes.byref(c), _ptr(k), _ptr(v), _Strides(*ks), _Strides(*vs), _ptr(table), M, _ptr(pos),
-          _ptr(counts), _ptr(weights), weights.shape[2] if weights is not None else 0, S, N, flags)
+        _check_weights(weights, "weights", S, Hkv, M * page, dev)
+    _call("sage_kv_append", dev, c, _adr(k), _adr(v), _strides(*ks), _strides(*vs), _adr(table), M, _adr(pos),
+          _adr(counts), _adr(weights), weights.shape[2] if weights is not None else 0, S, N, flags)
 
 
 def attn_paged_decode_workspace_size(S: int, Hq: int, Hkv: int, D: int, max_pages: int, page_size: int,
@@ -581,58 +586,69 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
     [S, Hq] (None when ``lse`` is False).  With ``workspace`` (uint8, at least
     attn_paged_decode_workspace_size bytes) and ``out``, ``lse_out`` nothing is allocated inside."""
     import torch
-    c, S, M = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
     flags, dev = _in_flag(q), k_cache.device
     qs = _rows(q, "q", 3)
     Hq = int(q.shape[1])
-    if tuple(q.shape) != (S, Hq, c.D) or q.device != dev or (k_scale is None and q.dtype != k_cache.dtype):
+    if tuple(q.shape) != (S, Hq, D) or q.device != dev or (k_scale is None and q.dtype != k_cache.dtype):
         raise ValueError("q must be [%d, Hq, %d] of the cache's type on %s, got %s %s on %s"
-                         % (S, c.D, dev, q.dtype, tuple(q.shape), q.device))
-    if Hq % c.Hkv:
-        raise ValueError("q's %d heads are no multiple of the cache's %d" % (Hq, c.Hkv))
+                         % (S, D, dev, q.dtype, tuple(q.shape), q.device))
+    if Hq % Hkv:
+        raise ValueError("q's %d heads are no multiple of the cache's %d" % (Hq, Hkv))
     window, sinks = _window_of(window, sinks)
     _check_tensor(lens, "lens", (S,), torch.int32, dev)
     if weights is not None:
-        _check_weights(weights, "weights", S, c.Hkv, M * c.page_size, dev)
-    o = torch.empty((S, Hq, c.D), dtype=q.dtype, device=dev) if out is None else out
-    _check_tensor(o, "out", (S, Hq, c.D), q.dtype, dev)
+        _check_weights(weights, "weights", S, Hkv, M * page, dev)
+    o = torch.empty((S, Hq, D), dtype=q.dtype, device=dev) if out is None else out
+    _check_tensor(o, "out", (S, Hq, D), q.dtype, dev)
     L = None
     if lse:
         L = torch.empty((S, Hq), dtype=torch.float32, device=dev) if lse_out is None else lse_out
         _check_tensor(L, "lse_out", (S, Hq), torch.float32, dev)
     if workspace is None:
-        n = attn_paged_decode_workspace_size(S, Hq, c.Hkv, c.D, M, c.page_size, weights is not None)
+        n = attn_paged_decode_workspace_size(S, Hq, Hkv, D, M, page, weights is not None)
         workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
     _check_workspace(workspace, dev)
-    _call("sage_attn_paged_decode", dev, ctypes.byref(c), _ptr(q), qs[0], qs[1], _ptr(o), _ptr(L), _ptr(table), M, _ptr(lens),
-          S, Hq, window, sinks, _ptr(weights), weights.shape[2] if weights is not None else 0, flags, _ptr(workspace),
+    _call("sage_attn_paged_decode", dev, c, _adr(q), qs[0], qs[1], _adr(o), _adr(L), _adr(table), M, _adr(lens),
+          S, Hq, window, sinks, _adr(weights), weights.shape[2] if weights is not None else 0, flags, _adr(workspace),
           workspace.numel())
     return o, L
 
 
+def kv_evict_workspace_size(S: int, Hkv: int, max_pages: int, page_size: int) -> int:
+    return int(lib().sage_kv_evict_workspace_size(S, Hkv, max_pages, page_size))
+
+
 def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int, keep_first: int = 0, keep_last: int = 0,
-                  k_scale=None, v_scale=None):
+                  k_scale=None, v_scale=None, out=None, workspace=None):
     """Shorten cached sequences to ``budget`` tokens: the first keep_first, the last keep_last and the
     heaviest of those between by ``weights`` [S, Hkv, >= max_pages * page_size], per head, in their
     order; copied to the pages of ``new_table`` (int32 [S, new_max_pages]), which hold nothing else
     that the call moves.  Returns (new_lens [S], new_weights [S, Hkv, new_max_pages * page_size],
-    kept [S, Hkv, budget]: the old positions, -1 behind the last)."""
+    kept [S, Hkv, budget]: the old positions, -1 behind the last).  With ``out`` (these three) and
+    ``workspace`` (uint8, at least kv_evict_workspace_size bytes) nothing is allocated inside."""
     import torch
-    c, S, M = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
     dev = k_cache.device
     _check_tensor(lens, "lens", (S,), torch.int32, dev)
-    _check_weights(weights, "weights", S, c.Hkv, M * c.page_size, dev)
+    _check_weights(weights, "weights", S, Hkv, M * page, dev)
     if new_table.dim() != 2 or new_table.numel() == 0:
         raise ValueError("new_table must be a non-empty [S, new_max_pages] tensor")
     M2 = int(new_table.shape[1])
     _check_tensor(new_table, "new_table", (S, M2), torch.int32, dev)
-    if not (1 <= budget <= M2 * c.page_size) or keep_first < 0 or keep_last < 0 or keep_first + keep_last > budget:
+    if not (1 <= budget <= M2 * page) or keep_first < 0 or keep_last < 0 or keep_first + keep_last > budget:
         raise ValueError("budget must be at least 1, keep_first + keep_last and at most new_table's capacity")
-    new_lens = torch.empty((S,), dtype=torch.int32, device=dev)
-    new_weights = torch.empty((S, c.Hkv, M2 * c.page_size), dtype=torch.float32, device=dev)
-    kept = torch.empty((S, c.Hkv, budget), dtype=torch.int32, device=dev)
-    _call("sage_kv_evict", dev, ctypes.byref(c), _ptr(table), M, _ptr(lens), _ptr(weights), weights.shape[2], _ptr(new_table),
-          M2, budget, keep_first, keep_last, _ptr(new_lens), _ptr(new_weights), _ptr(kept), S)
+    shapes = ((S,), (S, Hkv, M2 * page), (S, Hkv, budget))
+    types = (torch.int32, torch.float32, torch.int32)
+    new_lens, new_weights, kept = out if out is not None else [torch.empty(n, dtype=d, device=dev) for n, d in zip(shapes, types)]
+    for t, n, d, what in zip((new_lens, new_weights, kept), shapes, types, ("new_lens", "new_weights", "kept")):
+        _check_tensor(t, what, n, d, dev)
+    if workspace is None:
+        workspace = torch.empty(max(kv_evict_workspace_size(S, Hkv, M, page), 1), dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev)
+    _call("sage_kv_evict", dev, c, _adr(table), M, _adr(lens), _adr(weights), weights.shape[2], _adr(new_table),
+          M2, budget, keep_first, keep_last, _adr(new_lens), _adr(new_weights), _adr(kept), S, _adr(workspace),
+          workspace.numel())
     return new_lens, new_weights, kept
 
 

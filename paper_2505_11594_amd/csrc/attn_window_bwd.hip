@@ -116,107 +116,141 @@ __device__ __forceinline__ float ds_scale(const WindowBwd& a, int b, int hk) {
   return __builtin_ldexpf(1.0f, imax(-100, imin(100, 15 - e)));
 }
 
-// Address pieces of the transposing reads of a tile at LDS offset 0 (see attn_window.hip).
+// A lane's LDS addresses in a tile at offset 0 of LDS: rows start on multiples of
+// their size, so the swizzled chunk is or-ed in, and the other chunks follow by xor with
+// constants: row_at ^ 32 i is chunk 2 i + hi of row l % 32, tr_at ^ 64 db the piece of
+// channel block db of the transposing read (see attn_window.hip).  They are made
+// opaque where they are used, as the compiler would keep every one in a register.
 template <int D>
-__device__ __forceinline__ void tr_offsets(uint32_t* vo) {
-  constexpr int ROW = D * 2;
+__device__ __forceinline__ uint32_t row_at() {
+  const int lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
+  return col * (D * 2) + vswz<D>(col, hi) * 16;
+}
+template <int D>
+__device__ __forceinline__ uint32_t tr_at() {
   const int lane = threadIdx.x & 63, hi = lane >> 5;
   const int r = 4 * hi + (lane & 15) / 4, c0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db) vo[db] = r * ROW + vswz<D>(r, 4 * db + c0) * 16 + 8 * (lane & 1);
+  return r * (D * 2) + vswz<D>(r, c0) * 16 + 8 * (lane & 1);
 }
-template <int D, int OFF>
-__device__ __forceinline__ void tr_read(const uint32_t* va, v4i* r) {
-  v8bf t[D / 32];
-  if constexpr (D == 128) vt_read4<OFF, OFF + 8 * D * 2>(va[0], va[1], va[2], va[3], t[0], t[1], t[2], t[3]);
-  else vt_read2<OFF, OFF + 8 * D * 2>(va[0], va[1], t[0], t[1]);
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ v4i lds16(uint32_t at) { return *(const __attribute__((address_space(3))) v4i*)at; }
+__device__ __forceinline__ v4f lds4f(uint32_t at) { return *(const __attribute__((address_space(3))) v4f*)at; }
+
+// S and dP: the 32 rows at `at` and TB bytes behind times the 32 columns of b and c, the
+// two products in turn (each alone would wait for its own last result, and its rows,
+// all read ahead, would not leave enough registers for two waves per SIMD).
+template <int D, bool BF16, int TB>
+__device__ __forceinline__ void rows_times(uint32_t at, const v4i* b, const v4i* c, v16f& s, v16f& g) {
+  s = g = v16f{};
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) r[db] = __builtin_bit_cast(v4i, t[db]);
+  for (int i = 0; i < D / 16; ++i) {
+    s = mma32<BF16>(lds16(at ^ (32 * i)), b[i], s);
+    g = mma32<BF16>(lds16((at + TB) ^ (32 * i)), c[i], g);
+  }
+}
+// acc (dims x columns) += the transpose of 16 rows OFF bytes behind `at` times b.
+template <int D, bool BF16, int OFF>
+__device__ __forceinline__ void cols_times(uint32_t at, const v4i b, v16f* acc) {
+  v8bf x[D / 32];
+  if constexpr (D == 128) vt_read4<OFF, OFF + 8 * D * 2>(at, at ^ 64, at ^ 128, at ^ 192, x[0], x[1], x[2], x[3]);
+  else vt_read2<OFF, OFF + 8 * D * 2>(at, at ^ 64, x[0], x[1]);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) acc[db] = mma32<BF16>(__builtin_bit_cast(v4i, x[db]), b, acc[db]);
+}
+
+// The query tiles [t0, t1) of which some query sees one of the keys [k0, k0 + keys).
+struct TileRange {
+  int t0, t1;
+};
+__host__ __device__ __forceinline__ TileRange query_tiles(int k0, int keys, int n, int N, int window, bool sink) {
+  TileRange r = {k0 / BT, k0 / BT};
+  if (k0 < n) r.t1 = cdiv(sink ? n : imin(n, imin(N, k0 + keys - 1 + window)), BT);
+  return r;
 }
 
 // One 32 x 32 block of (query, key) pairs for a wave that holds 32 keys (kreg, vreg;
 // lane: key l % 32): adds to dv and dk (dims x keys).  The block's queries are rows
 // [32 t, +32) of the tile at L (Q, then dO, then lb and delta).
-template <int D, bool BF16, bool MASK>
-__device__ __forceinline__ void dkv_block(const uint8_t* L, uint32_t lbase, const uint32_t* vo, int t, const v4i* kreg,
-                                          const v4i* vreg, v16f* dk, v16f* dv, float c2, float f15, int first, int past) {
-  constexpr int ROW = D * 2, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
-  const int lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
-  const int row = 32 * t + col;
-  v16f s = v16f{}, g = v16f{};
-#pragma unroll
-  for (int i = 0; i < NKS; ++i) s = mma32<BF16>(*reinterpret_cast<const v4i*>(L + row * ROW + vswz<D>(row, 2 * i + hi) * 16), kreg[i], s);
-#pragma unroll
-  for (int i = 0; i < NKS; ++i) g = mma32<BF16>(*reinterpret_cast<const v4i*>(L + TB + row * ROW + vswz<D>(row, 2 * i + hi) * 16), vreg[i], g);
+template <int D, bool BF16>
+__device__ __forceinline__ void dkv_block(uint32_t L, uint32_t rat, uint32_t tat, int t, const v4i* kreg, const v4i* vreg,
+                                          v16f* dk, v16f* dv, float c2, float f15, bool mask, int first, int past) {
+  constexpr int ROW = D * 2, TB = BT * ROW;
+  const int hi = (threadIdx.x & 63) >> 5;
+  const uint32_t ra = opaque(L + t * 32 * ROW + rat);
+  v16f s, g;
+  rows_times<D, BF16, TB>(ra, kreg, vreg, s, g);
   // element e is query 32 t + 8 (e >> 2) + 4 hi + (e & 3) of the tile, visible iff first <= it < past
+  const int at = 32 * t + 4 * hi;
+  if (mask) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int c = at + 8 * (e >> 2) + (e & 3);
+      s[e] = c >= first && c < past ? s[e] : -INFINITY;
+    }
+  }
+  const uint32_t la = opaque(L + 2 * TB + 4 * at);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const v4f lb = lds4f(la + 32 * q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[4 * q + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * q + e], c2, kPShift<BF16> - lb[e]));
+  }
   uint32_t pw[8], dw[8];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int at = 32 * t + 8 * q + 4 * hi;
-    const v4f lb = *reinterpret_cast<const v4f*>(L + 2 * TB + 4 * at), dl = *reinterpret_cast<const v4f*>(L + 2 * TB + 4 * BT + 4 * at);
-    float p[4], d[4];
+    const v4f dl = lds4f(la + 4 * BT + 32 * q);
+    float d[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * q + e], c2, kPShift<BF16> - lb[e]));
-      if constexpr (MASK) {
-        const uint32_t keep = (uint32_t)((~(at + e - first) & (at + e - past)) >> 31);
-        p[e] = __uint_as_float(__float_as_uint(p[e]) & keep);
-      }
       const float x = g[4 * q + e] - dl[e];
-      d[e] = p[e] * (BF16 ? x : x * f15);
+      d[e] = s[4 * q + e] * (BF16 ? x : x * f15);
     }
-    pw[2 * q] = pack16<BF16>(p[0], p[1]); pw[2 * q + 1] = pack16<BF16>(p[2], p[3]);
+    pw[2 * q] = pack16<BF16>(s[4 * q], s[4 * q + 1]); pw[2 * q + 1] = pack16<BF16>(s[4 * q + 2], s[4 * q + 3]);
     dw[2 * q] = pack16<BF16>(d[0], d[1]); dw[2 * q + 1] = pack16<BF16>(d[2], d[3]);
   }
-  uint32_t va[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) va[db] = vo[db] + lbase + (uint32_t)t * 32 * ROW;
+  const uint32_t ta = opaque(L + t * 32 * ROW + tat);
   static_for<2>([&](auto U_) {
     constexpr int u = decltype(U_)::value;
     const v4i pk = {(int)pw[4 * u], (int)pw[4 * u + 1], (int)pw[4 * u + 2], (int)pw[4 * u + 3]};
     const v4i dsk = {(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]};
-    v4i x[NDB];
-    tr_read<D, TB + 16 * u * ROW>(va, x);
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) dv[db] = mma32<BF16>(x[db], pk, dv[db]);
-    tr_read<D, 16 * u * ROW>(va, x);
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) dk[db] = mma32<BF16>(x[db], dsk, dk[db]);
+    cols_times<D, BF16, TB + 16 * u * ROW>(ta, pk, dv);
+    cols_times<D, BF16, 16 * u * ROW>(ta, dsk, dk);
   });
 }
 
 // dK and dV.  SINK: 2 waves share 32 sink keys and take one half of each query tile;
-// else 4 waves x 32 keys.  Grid x: (sequence, key head) times the key blocks (times
-// the chunks of the sinks' query tiles).
+// else 4 waves x 32 keys.  Grid x: (sequence, key head) times the key blocks times
+// the chunks of the blocks' query tiles (over all heads of the group), `share` tiles
+// each; with more than one chunk their parts go to the workspace, in fp32.
 template <int D, bool BF16, bool SINK>
-__global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dkv_kernel(const WindowBwd a) {
+__global__ __launch_bounds__(SINK ? 128 : 256, SINK ? 1 : 2) void dkv_kernel(const WindowBwd a) {
   constexpr int W = SINK ? 2 : 4;                        // waves
   constexpr int KB = SINK ? 32 : 128;                    // keys per workgroup
   constexpr int ROW = D * 2, CH = ROW / 16, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
   constexpr int STAGE = 2 * TB + 2 * BT * 4;             // Q, dO, lb, delta
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
+  static_assert(STAGE % 256 == 0, "addresses inside a tile are xor-ed");
+  __shared__ __attribute__((aligned(256))) uint8_t lds[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5;
   const int nkb = SINK ? cdiv(a.sinks, KB) : cdiv(a.N, KB);
   const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
   unsigned lin = xcd * (total >> 3) + min(xcd, total & 7u) + (blockIdx.x >> 3);
-  int chunk = 0;
-  if constexpr (SINK) { chunk = lin % a.chunks; lin /= a.chunks; }
+  const int chunks = SINK ? a.chunks : a.mchunks, chunk = (int)(lin % chunks);
+  lin /= chunks;
   const int bh = (int)(lin / nkb), b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.Hq / a.Hkv;
   const int k0 = (int)(lin % nkb) * KB, kw = SINK ? k0 : k0 + 32 * wave, key = kw + col;
   const int n = seq_len(a, b), Np = row_pad(a.N);
 
   // query tiles that see some of the keys, once per head of the group
-  int t0 = k0 / BT, t1 = 0;                              // tiles [t0, t1)
-  if (k0 < n) t1 = cdiv(SINK ? n : imin(n, imin(a.N, k0 + KB - 1 + a.window)), BT);
-  if (!SINK && k0 + KB <= a.sinks) t1 = 0;               // sink keys alone
-  const int nt = imax(0, t1 - t0), all = nt * G;
-  int it0 = 0, it1 = all;
-  if constexpr (SINK) {
-    const int share = cdiv(all, a.chunks);
-    it0 = imin(all, chunk * share);
-    it1 = imin(all, it0 + share);
-  }
+  const TileRange tr = query_tiles(k0, KB, n, a.N, a.window, SINK);
+  const int t0 = tr.t0, t1 = tr.t1, nt = t1 - t0;
+  const int all = !SINK && k0 + KB <= a.sinks ? 0 : nt * G;      // (not for sink keys alone)
+  const int share = SINK ? cdiv(all, chunks) : a.mshare;
+  const int it0 = imin(all, chunk * share), it1 = imin(all, it0 + share);
+  if (!SINK && chunk > 0 && it0 == it1) return;
 
   v4i kreg[NKS], vreg[NKS];
   {
@@ -232,14 +266,10 @@ __global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dk
   const float f = ds_scale<BF16>(a, b, hk), f15 = f * 0x1p-15f;
 
   constexpr int JR = 1024 / ROW, NJ = BT / JR, JW = NJ / W;
-  uint32_t qlo[JW], glo[JW];
+  static_assert(W * JR % 8 == 0, "a lane's pieces have the same swizzle");
   const uint32_t qst = (uint32_t)(a.qs.n * 2), gst = (uint32_t)(a.gs.n * 2);
-#pragma unroll
-  for (int i = 0; i < JW; ++i) {
-    const int r = (wave + W * i) * JR + lane / CH, c = vswz<D>(r, lane % CH) * 16;
-    qlo[i] = r * qst + c;
-    glo[i] = r * gst + c;
-  }
+  const int jr = wave * JR + lane / CH;
+  const uint32_t qlo = jr * qst + vswz<D>(jr, lane % CH) * 16, glo = jr * gst + vswz<D>(jr, lane % CH) * 16;
   auto issue = [&](int g, int tile, int stage) {
     uint8_t* L = lds + stage * STAGE;
     const int h = hk * G + g, qb = tile * BT;
@@ -247,17 +277,17 @@ __global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dk
     const uint8_t* q = (const uint8_t*)a.q + 2 * (b * a.qs.b + h * a.qs.h) + (size_t)qb * qst;
     const uint8_t* o = (const uint8_t*)a.dout + 2 * (b * a.gs.b + h * a.gs.h) + (size_t)qb * gst;
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(q, (rows - 1) * qst + ROW), rg = make_rsrc(o, (rows - 1) * gst + ROW);
+    const uint32_t q0 = opaque(qlo), g0 = opaque(glo);
 #pragma unroll
     for (int i = 0; i < JW; ++i) {
-      buf_load16(rq, qlo[i], 0u, L + (wave + W * i) * 1024);
-      buf_load16(rg, glo[i], 0u, L + TB + (wave + W * i) * 1024);
+      buf_load16(rq, q0 + W * JR * i * qst, 0u, L + (wave + W * i) * 1024);
+      buf_load16(rg, g0 + W * JR * i * gst, 0u, L + TB + (wave + W * i) * 1024);
     }
     const size_t at = ((size_t)b * a.Hq + h) * Np + qb;
     if (wave == 0) buf_load4(make_rsrc(a.lb + at, BT * 4), 4 * lane, 0u, L + 2 * TB);
     if (wave == 1) buf_load4(make_rsrc(a.delta + at, BT * 4), 4 * lane, 0u, L + 2 * TB + BT * 4);
   };
-  uint32_t vo[NDB];
-  tr_offsets<D>(vo);
+  const uint32_t rat = row_at<D>(), tat = tr_at<D>();
   const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
 
   v16f dk[NDB], dv[NDB];
@@ -272,21 +302,18 @@ __global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dk
     __syncthreads();                                     // everyone's; every wave is past the tile before
     const int st = (it - it0) & 1;
     if (it + 1 < it1) issue(g, tile, st ^ 1);
-    const uint8_t* L = lds + st * STAGE;
-    const uint32_t lb = l0 + st * STAGE;
+    const uint32_t L = l0 + st * STAGE;
     // queries [first, past) of the tile see this lane's key
     const int first = key - qb, past = SINK ? BT : key + a.window - qb;
     if constexpr (SINK) {
       if (qb + 32 * wave + 31 < kw) continue;
-      if (qb + 32 * wave >= kw + 31) dkv_block<D, BF16, false>(L, lb, vo, wave, kreg, vreg, dk, dv, a.c2, f15, first, past);
-      else dkv_block<D, BF16, true>(L, lb, vo, wave, kreg, vreg, dk, dv, a.c2, f15, first, past);
+      dkv_block<D, BF16>(L, rat, tat, wave, kreg, vreg, dk, dv, a.c2, f15, qb + 32 * wave < kw + 31, first, past);
     } else {
 #pragma unroll 1
       for (int t = 0; t < 2; ++t) {
         const int q0 = qb + 32 * t;
         if (q0 + 31 < kw || q0 >= kw + 31 + a.window) continue;
-        if (q0 >= kw + 31 && q0 + 31 < kw + a.window) dkv_block<D, BF16, false>(L, lb, vo, t, kreg, vreg, dk, dv, a.c2, f15, first, past);
-        else dkv_block<D, BF16, true>(L, lb, vo, t, kreg, vreg, dk, dv, a.c2, f15, first, past);
+        dkv_block<D, BF16>(L, rat, tat, t, kreg, vreg, dk, dv, a.c2, f15, q0 < kw + 31 || q0 + 31 >= kw + a.window, first, past);
       }
     }
   }
@@ -327,6 +354,23 @@ __global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dk
   } else {
     if (key >= a.N || key < a.sinks) return;             // the sinks' rows are join_sinks_kernel's
     const bool live = key < n;
+    if (chunks > 1) {
+      float* part = a.mpart + ((((size_t)bh * nkb + k0 / KB) * chunks + chunk) * 2 * KB + (key - k0)) * D;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v4f y, z;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            y[e] = live ? dk[db][4 * q + e] * sk : 0.0f;
+            z[e] = live ? dv[db][4 * q + e] * sv : 0.0f;
+          }
+          *reinterpret_cast<v4f*>(part + 32 * db + 8 * q + 4 * hi) = y;
+          *reinterpret_cast<v4f*>(part + KB * D + 32 * db + 8 * q + 4 * hi) = z;
+        }
+      return;
+    }
     uint16_t* kr = (uint16_t*)a.dk + ((size_t)bh * a.N + key) * D;
     uint16_t* vr = (uint16_t*)a.dv + ((size_t)bh * a.N + key) * D;
 #pragma unroll
@@ -341,21 +385,35 @@ __global__ __launch_bounds__(SINK ? 128 : 256, SINK || D == 128 ? 1 : 2) void dk
   }
 }
 
-// Sink keys' dK and dV from the chunks' parts, in their order.
+// Sink keys' dK and dV from the chunks' parts, in their order: one workgroup per key,
+// one thread per channel of dK and dV.
 template <int D, bool BF16>
-__global__ __launch_bounds__(256) void join_sinks_kernel(const WindowBwd a) {
-  const int bh = blockIdx.y, nkb = cdiv(a.sinks, 32);
-  const int at = (blockIdx.x * 256 + threadIdx.x) * 2, key = at / D, d = at % D;
-  if (key >= a.sinks) return;
-  const float* p = a.part + (((size_t)bh * nkb + key / 32) * a.chunks * 2 * 32 + key % 32) * D + d;
-  float k0 = 0.0f, k1 = 0.0f, v0 = 0.0f, v1 = 0.0f;
-  for (int c = 0; c < a.chunks; ++c, p += 2 * 32 * D) {
-    k0 += p[0]; k1 += p[1];
-    v0 += p[32 * D]; v1 += p[32 * D + 1];
-  }
-  const size_t o = ((size_t)bh * a.N + key) * D + d;
-  *reinterpret_cast<uint32_t*>((uint16_t*)a.dk + o) = pack16<BF16>(k0, k1);
-  *reinterpret_cast<uint32_t*>((uint16_t*)a.dv + o) = pack16<BF16>(v0, v1);
+__global__ __launch_bounds__(2 * D) void join_sinks_kernel(const WindowBwd a) {
+  const int bh = blockIdx.y, key = blockIdx.x, nkb = cdiv(a.sinks, 32), which = threadIdx.x / D, d = threadIdx.x % D;
+  const float* p = a.part + ((((size_t)bh * nkb + key / 32) * a.chunks * 2 + which) * 32 + key % 32) * D + d;
+  float x = 0.0f;
+#pragma unroll 16
+  for (int c = 0; c < a.chunks; ++c) x += p[(size_t)c * 2 * 32 * D];
+  uint16_t* o = (uint16_t*)(which ? a.dv : a.dk) + ((size_t)bh * a.N + key) * D;
+  o[d] = (uint16_t)pack16<BF16>(x, 0.0f);
+}
+
+// The other keys' dK and dV, where their query tiles were cut into chunks: 4 channels
+// of one key per thread.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void join_keys_kernel(const WindowBwd a) {
+  constexpr int KB = 128, TPK = D / 2;                   // threads per key: D / 4 for each of dK and dV
+  const int bh = blockIdx.y, b = bh / a.Hkv, nkb = cdiv(a.N, KB);
+  const int key = blockIdx.x * (256 / TPK) + threadIdx.x / TPK, x = threadIdx.x % TPK, which = x / (D / 4), d = x % (D / 4) * 4;
+  if (key >= a.N || key < a.sinks) return;
+  const TileRange tr = query_tiles(key / KB * KB, KB, seq_len(a, b), a.N, a.window, false);
+  const int parts = imax(1, cdiv((tr.t1 - tr.t0) * (a.Hq / a.Hkv), a.mshare));
+  const float* p = a.mpart + ((((size_t)bh * nkb + key / KB) * a.mchunks * 2 + which) * KB + key % KB) * D + d;
+  v4f y = v4f{};
+#pragma unroll 4
+  for (int c = 0; c < parts; ++c) y += *reinterpret_cast<const v4f*>(p + (size_t)c * 2 * KB * D);
+  uint16_t* o = (uint16_t*)(which ? a.dv : a.dk) + ((size_t)bh * a.N + key) * D + d;
+  *reinterpret_cast<v2u*>(o) = v2u{pack16<BF16>(y[0], y[1]), pack16<BF16>(y[2], y[3])};
 }
 
 // dQ: 4 waves x 32 queries, the forward's walk over the key tiles.
@@ -370,7 +428,7 @@ __global__ __launch_bounds__(256) void join_sinks_kernel(const WindowBwd a) {
 template <int D, bool BF16>
 __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
   constexpr int W = 4, ROW = D * 2, CH = ROW / 16, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TB];   // two stages of a K tile and a V tile
+  __shared__ __attribute__((aligned(256))) uint8_t lds[4 * TB];  // two stages of a K tile and a V tile
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5;
   const int nqt = cdiv(a.N, 32 * W);
@@ -397,14 +455,10 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
   const float f = ds_scale<BF16>(a, b, hk), f15 = f * 0x1p-15f;
 
   constexpr int JR = 1024 / ROW, NJ = BT / JR, JW = NJ / W;
-  uint32_t klo[JW], vlo[JW];
+  static_assert(W * JR % 8 == 0, "a lane's pieces have the same swizzle");
   const uint32_t kst = (uint32_t)(a.ks.n * 2), vst = (uint32_t)(a.vs.n * 2);
-#pragma unroll
-  for (int i = 0; i < JW; ++i) {
-    const int r = (wave + W * i) * JR + lane / CH, c = vswz<D>(r, lane % CH) * 16;
-    klo[i] = r * kst + c;
-    vlo[i] = r * vst + c;
-  }
+  const int jr = wave * JR + lane / CH;
+  const uint32_t klo = jr * kst + vswz<D>(jr, lane % CH) * 16, vlo = jr * vst + vswz<D>(jr, lane % CH) * 16;
   const uint8_t* kbase = (const uint8_t*)a.k + 2 * (b * a.ks.b + hk * a.ks.h);
   const uint8_t* vbase = (const uint8_t*)a.v + 2 * (b * a.vs.b + hk * a.vs.h);
   auto issue = [&](int kb, int stage) {
@@ -412,14 +466,14 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
     const uint32_t rows = (uint32_t)imin(n - kb, BT);
     const __amdgpu_buffer_rsrc_t rk = make_rsrc(kbase + (size_t)kb * kst, (rows - 1) * kst + ROW);
     const __amdgpu_buffer_rsrc_t rv = make_rsrc(vbase + (size_t)kb * vst, (rows - 1) * vst + ROW);
+    const uint32_t k0 = opaque(klo), v0 = opaque(vlo);
 #pragma unroll
     for (int i = 0; i < JW; ++i) {
-      buf_load16(rk, klo[i], 0u, L + (wave + W * i) * 1024);
-      buf_load16(rv, vlo[i], 0u, L + TB + (wave + W * i) * 1024);
+      buf_load16(rk, k0 + W * JR * i * kst, 0u, L + (wave + W * i) * 1024);
+      buf_load16(rv, v0 + W * JR * i * vst, 0u, L + TB + (wave + W * i) * 1024);
     }
   };
-  uint32_t vo[NDB];
-  tr_offsets<D>(vo);
+  const uint32_t rat = row_at<D>(), tat = tr_at<D>();
   const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
   v16f dq[NDB];
 #pragma unroll
@@ -431,18 +485,15 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
     if (j + 1 < tl.count) issue(tl.tile(j + 1) * BT, (j + 1) & 1);
-    const uint8_t* L = lds + (j & 1) * 2 * TB;
+    const uint32_t L = l0 + (j & 1) * 2 * TB;
     const int kb = tl.tile(j) * BT;
     static_for<2>([&](auto T_) {
       constexpr int t = decltype(T_)::value;
       const int kt = kb + 32 * t;
       if (kt > qw + 31 || (kt + 32 <= qw - win + 1 && kt >= sinks)) return;
-      const int row = 32 * t + col;
-      v16f s = v16f{}, g = v16f{};
-#pragma unroll
-      for (int i = 0; i < NKS; ++i) s = mma32<BF16>(*reinterpret_cast<const v4i*>(L + row * ROW + vswz<D>(row, 2 * i + hi) * 16), qreg[i], s);
-#pragma unroll
-      for (int i = 0; i < NKS; ++i) g = mma32<BF16>(*reinterpret_cast<const v4i*>(L + TB + row * ROW + vswz<D>(row, 2 * i + hi) * 16), greg[i], g);
+      const uint32_t ra = opaque(L + t * 32 * ROW + rat);
+      v16f s, g;
+      rows_times<D, BF16, TB>(ra, qreg, greg, s, g);
       uint32_t dw[8];
       const bool mask = kt + 31 > qw || kt + 32 > n || (kt <= qw + 31 - win && kt + 32 > sinks);
       const int base = kt + 4 * hi, rem = imin(n, qi + 1) - base, low = qi - win + 1 - base, sk = sinks - base;
@@ -464,16 +515,10 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
         dw[e] = pack16<BF16>(d[2 * e], d[2 * e + 1]);
         dsum = add_pair<BF16>(dw[e], dsum);
       }
-      uint32_t va[NDB];
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) va[db] = vo[db] + l0 + (uint32_t)((j & 1) * 2 * TB);
+      const uint32_t ta = opaque(L + tat);
       static_for<2>([&](auto U_) {
         constexpr int u = decltype(U_)::value;
-        const v4i dsk = {(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]};
-        v4i x[NDB];
-        tr_read<D, (32 * t + 16 * u) * ROW>(va, x);
-#pragma unroll
-        for (int db = 0; db < NDB; ++db) dq[db] = mma32<BF16>(x[db], dsk, dq[db]);
+        cols_times<D, BF16, (32 * t + 16 * u) * ROW>(ta, v4i{(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]}, dq);
       });
     });
   }
@@ -521,6 +566,28 @@ int window_bwd_chunks(int B, int Hq, int Hkv, int N, int sinks) {
   const long long want = 512 / (blocks > 0 ? blocks : 1), most = (tiles + 3) / 4;
   return (int)imax(1, (int)(want < most ? want : most));
 }
+// Query tiles per chunk of the other keys' dK and dV: one chunk where the longest block
+// takes no more than 5/4 of what each of 512 workgroups (two per CU) would of the
+// whole; else half of that whole's share, and 8 tiles at least (a chunk's part costs the
+// traffic of about one).  2 x 12 / 4 heads of 1000 tokens, D = 64: 91 us in one chunk,
+// 30 + 5 in up to 6 (join_keys_kernel is the 5).
+int window_bwd_share(int B, int Hq, int Hkv, int N, int window, int* chunks) {
+  long long total = 0;
+  int most = 1;
+  for (int k0 = 0; k0 < N; k0 += 128) {
+    const TileRange r = query_tiles(k0, 128, N, N, window, false);
+    total += r.t1 - r.t0;
+    most = imax(most, r.t1 - r.t0);
+  }
+  const long long G = Hq / Hkv, each = (total * G * B * Hkv + 511) / 512;
+  long long share = most * G;
+  if (most * G * 4 > each * 5) share = each / 2 > 8 ? each / 2 : 8;
+  *chunks = (int)((most * G + share - 1) / share);
+  return (int)share;
+}
+size_t window_bwd_mpart_floats(int B, int Hkv, int N, int D, int chunks) {
+  return chunks > 1 ? (size_t)B * Hkv * cdiv(N, 128) * chunks * 2 * 128 * D : 0;
+}
 size_t window_bwd_row_floats(int B, int Hq, int N) { return (size_t)B * Hq * ((N + BT - 1) / BT * BT); }
 size_t window_bwd_norm_floats(int B, int Hq, int Hkv, int N) { return (size_t)B * (Hq + Hkv) * cdiv(N, PR); }
 size_t window_bwd_part_floats(int B, int Hq, int Hkv, int N, int D, int sinks) {
@@ -534,12 +601,16 @@ static hipError_t launch_window_bwd_t(const WindowBwd& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const unsigned heads = (unsigned)(a.B * a.Hkv);
-  hipLaunchKernelGGL((dkv_kernel<D, BF16, false>), dim3(heads * cdiv(a.N, 128)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((dkv_kernel<D, BF16, false>), dim3(heads * cdiv(a.N, 128) * a.mchunks), dim3(256), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.mchunks > 1) {
+    hipLaunchKernelGGL((join_keys_kernel<D, BF16>), dim3((unsigned)cdiv(a.N, 512 / D), heads), dim3(256), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   if (a.sinks > 0) {
     hipLaunchKernelGGL((dkv_kernel<D, BF16, true>), dim3(heads * cdiv(a.sinks, 32) * a.chunks), dim3(128), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((join_sinks_kernel<D, BF16>), dim3((unsigned)cdiv(a.sinks * (D / 2), 256), heads), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((join_sinks_kernel<D, BF16>), dim3((unsigned)a.sinks, heads), dim3(2 * D), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   hipLaunchKernelGGL((dq_kernel<D, BF16>), dim3((unsigned)(a.B * a.Hq) * cdiv(a.N, 128)), dim3(256), 0, st, a);

@@ -100,11 +100,24 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
 // keep_first and last keep_last tokens and the heaviest of those between, ties
 // with the lowest index first, in ascending order.
 //
-// select: one workgroup per (sequence, head) finds the weight of the last token
-// that is kept (a radix selection: 4 passes over 8-bit digits, from the top) and
-// writes the kept indices and weights.  move: the kept rows to their new pages.
+// The weight of the last token that is kept comes from a radix selection from the
+// top (digits of 11, 11 and 10 bits, so that the first one spreads weights of like
+// size over 4 bins per power of two); then the kept indices and weights are written, and
+// move copies the rows to their new pages.
+//
+// One workgroup per (sequence, head) does the selection in one launch where that
+// fills half the GPU, or the sequences are short.  A single workgroup takes 74 us for
+// 65536 tokens (its LDS atomics and scattered stores bound it), so a few long
+// sequences are cut into chunks: a launch per digit leaves each chunk's histogram in
+// the workspace, from which the next ones add up all chunks' to pick the digit, and
+// the last finds its place behind the chunks before it (4 launches).
 // ---------------------------------------------------------------------------
 constexpr int EV = 1024;                                 // threads of the selection
+constexpr int ER = 8;                                    // neighbouring tokens per thread and round of the writing
+constexpr int EL = 16;                                   // loads per thread in flight
+constexpr int BINS = 2048;
+constexpr int EVICT_CHUNK = EV * ER, EVICT_MOST = 16;    // tokens per chunk at least, chunks at most
+static_assert(EV * 2 == BINS && EV * ER < 1 << 14, "bins per thread; counts of a round");
 
 // Ascending in the weight as an unsigned number; -0 and 0 are equal, NaN is lowest.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -112,8 +125,16 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ int digit_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t digit_mask(int pass) { return pass == 2 ? 1023u : BINS - 1u; }
 
-// Exclusive sum over the workgroup, and the total.  `red`: 16 words of LDS.
+struct EvictLds {
+  int hist[BINS];
+  int red[EV / 64];
+  int pick[2];
+};
+
+// Exclusive sum over the workgroup, and the total.
 __device__ __forceinline__ int block_scan(int x, int* red, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int inc = x;
@@ -135,75 +156,176 @@ __device__ __forceinline__ int block_scan(int x, int* red, int* total) {
   return before + inc - x;
 }
 
-__global__ __launch_bounds__(EV) void evict_select_kernel(const Evict a) {
-  __shared__ int hist[256];
-  __shared__ int red[EV / 64];
-  __shared__ int pick[2];
-  const int s = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
-  const int n = cached_len(a.lens[s], a.c.max_pages * a.c.page_size);
-  const size_t sh = (size_t)s * a.c.Hkv + h;
-  const float* w = a.weights + sh * a.wstride;
-  float* nw = a.new_weights + sh * a.new_wstride;
-  int32_t* kept = a.kept + sh * a.budget;
-  const int m = imin(n, a.budget);
-  if (tid == 0 && h == 0) a.new_lens[s] = m;
-  for (int j = m + tid; j < a.budget; j += EV) kept[j] = -1;
-  const int new_capacity = a.new_max_pages * a.c.page_size;
-  for (int j = m + tid; j < new_capacity; j += EV) nw[j] = 0.0f;
-  if (n <= a.budget) {
-    for (int j = tid; j < n; j += EV) { kept[j] = j; nw[j] = w[j]; }
-    return;
-  }
-  const int lo = a.keep_first, hi = n - a.keep_last;     // the tokens between are chosen from
-  int need = a.budget - a.keep_first - a.keep_last;      // < hi - lo
-  uint32_t prefix = 0, mask = 0;                         // digits found so far
-  if (need > 0)
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += EV) hist[i] = 0;
-      __syncthreads();
-      for (int j = lo + tid; j < hi; j += EV) {
-        const uint32_t k = weight_key(w[j]);
-        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1);
-      }
-      __syncthreads();
-      // the digit of the need-th largest: thread t holds digit 255 - t
-      const int c = tid < 256 ? hist[255 - tid] : 0;
-      int total;
-      const int above = block_scan(c, red, &total);
-      if (tid < 256 && above < need && above + c >= need) {
-        pick[0] = 255 - tid;
-        pick[1] = above;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)pick[0] << shift;
-      mask |= 255u << shift;
-      need -= pick[1];
-      __syncthreads();
+// What is known of the last kept key: its top digits, and how many of the tokens that
+// have them are kept.
+struct Last {
+  uint32_t prefix, mask;
+  int need;
+};
+
+// Histogram of one digit of the tokens [lo, hi) whose upper digits are known.
+__device__ __forceinline__ void histogram(EvictLds& l, const float* w, int lo, int hi, int pass, const Last& last) {
+  const int tid = threadIdx.x, shift = digit_shift(pass);
+  const uint32_t bins = digit_mask(pass);
+  for (int i = tid; i < BINS; i += EV) l.hist[i] = 0;
+  __syncthreads();
+  for (int j0 = lo + tid; j0 < hi; j0 += EV * EL) {
+    float x[EL];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) x[e] = w[imin(j0 + e * EV, hi - 1)];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) {
+      const uint32_t k = weight_key(x[e]);
+      if (j0 + e * EV < hi && (k & last.mask) == last.prefix) atomicAdd(&l.hist[(k >> shift) & bins], 1);
     }
-  // `prefix` is the last kept key, `need` of the tokens that have it are kept
-  const bool any = a.budget - a.keep_first - a.keep_last > 0;
-  int out = 0, ties = 0;
-  for (int j0 = 0; j0 < n; j0 += EV) {
-    const int j = j0 + tid;
-    bool keep = false, tie = false;
-    if (j < n) {
-      if (j < lo || j >= hi) keep = true;
-      else if (any) {
-        const uint32_t k = weight_key(w[j]);
-        keep = k > prefix;
-        tie = k == prefix;
-      }
+  }
+  __syncthreads();
+}
+// Thread t holds the counts c0, c1 of bins 2047 - 2 t and 2046 - 2 t: the digit of the
+// need-th largest.
+__device__ __forceinline__ void pick_digit(EvictLds& l, int c0, int c1, int pass, Last& last) {
+  const int d = BINS - 1 - 2 * threadIdx.x;
+  int total;
+  const int above = block_scan(c0 + c1, l.red, &total);
+  if (above < last.need && above + c0 >= last.need) {
+    l.pick[0] = d;
+    l.pick[1] = above;
+  } else if (above + c0 < last.need && above + c0 + c1 >= last.need) {
+    l.pick[0] = d - 1;
+    l.pick[1] = above + c0;
+  }
+  __syncthreads();
+  last.prefix |= (uint32_t)l.pick[0] << digit_shift(pass);
+  last.mask |= digit_mask(pass) << digit_shift(pass);
+  last.need -= l.pick[1];
+  __syncthreads();
+}
+
+// The kept tokens of [j0, j1): those outside [lo, hi), above last.prefix, and the first
+// last.need with it; `out` tokens are kept in front of j0 without the last kind, and
+// `ties` of that kind lie there.
+__device__ __forceinline__ void write_kept(EvictLds& l, const float* w, int32_t* kept, float* nw, int j0, int j1, int lo, int hi,
+                                           bool any, const Last& last, int out, int ties) {
+  for (; j0 < j1; j0 += EV * ER) {
+    const int j = j0 + threadIdx.x * ER;
+    float x[ER];
+    uint32_t keep = 0, tie = 0;                          // bit e: token j + e
+#pragma unroll
+    for (int e = 0; e < ER; ++e) x[e] = j + e < j1 ? w[j + e] : 0.0f;
+#pragma unroll
+    for (int e = 0; e < ER; ++e) {
+      const uint32_t k = weight_key(x[e]);
+      const bool fixed = j + e < lo || j + e >= hi;
+      if (j + e < j1 && (fixed || (any && k > last.prefix))) keep |= 1u << e;
+      if (!fixed && any && k == last.prefix && j + e < j1) tie |= 1u << e;
     }
     int total;
-    const int tb = ties + block_scan(tie, red, &total);
-    ties += total;
-    if (tie && tb < need) keep = true;
-    const int at = out + block_scan(keep, red, &total);
-    out += total;
-    if (keep) {
-      kept[at] = j;
-      nw[at] = w[j];
+    const int scan = block_scan(__builtin_popcount(keep) | __builtin_popcount(tie) << 16, l.red, &total);   // both below 2^14
+    int kb = out + (scan & 0xFFFF), tb = ties + (scan >> 16);
+    out += total & 0xFFFF;
+    ties += total >> 16;
+#pragma unroll
+    for (int e = 0; e < ER; ++e) {
+      const bool t = tie >> e & 1u;
+      if ((keep >> e & 1u) || (t && tb < last.need)) {
+        const int at = kb + imin(tb, last.need);
+        kept[at] = j + e;
+        nw[at] = x[e];
+      }
+      kb += keep >> e & 1u;
+      tb += t;
     }
+  }
+}
+
+struct EvictHead {                                       // one sequence and head
+  int n, lo, hi, need;
+  const float* w;
+  float* nw;
+  int32_t* kept;
+};
+__device__ __forceinline__ EvictHead evict_head(const Evict& a, int s, int h) {
+  EvictHead e;
+  const size_t sh = (size_t)s * a.c.Hkv + h;
+  e.n = cached_len(a.lens[s], a.c.max_pages * a.c.page_size);
+  e.lo = a.keep_first;
+  e.hi = e.n - a.keep_last;
+  e.need = a.budget - a.keep_first - a.keep_last;        // below hi - lo if n is above the budget
+  e.w = a.weights + sh * a.wstride;
+  e.nw = a.new_weights + sh * a.new_wstride;
+  e.kept = a.kept + sh * a.budget;
+  return e;
+}
+// What lies behind the kept tokens, and sequences that are kept whole (then true);
+// part `c` of `parts`.
+__device__ __forceinline__ bool evict_ends(const Evict& a, const EvictHead& e, int s, int h, int c, int parts) {
+  const int m = imin(e.n, a.budget), first = c * EV + threadIdx.x, step = parts * EV;
+  if (first == 0 && h == 0) a.new_lens[s] = m;
+  for (int j = m + first; j < a.budget; j += step) e.kept[j] = -1;
+  const int new_capacity = a.new_max_pages * a.c.page_size;
+  for (int j = m + first; j < new_capacity; j += step) e.nw[j] = 0.0f;
+  if (e.n > a.budget) return false;
+  for (int j = first; j < e.n; j += step) { e.kept[j] = j; e.nw[j] = e.w[j]; }
+  return true;
+}
+
+__global__ __launch_bounds__(EV) void evict_select_kernel(const Evict a) {
+  __shared__ EvictLds l;
+  const int s = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+  const EvictHead e = evict_head(a, s, h);
+  if (evict_ends(a, e, s, h, 0, 1)) return;
+  Last last = {0u, 0u, e.need};
+  if (e.need > 0)
+    for (int pass = 0; pass < 3; ++pass) {
+      histogram(l, e.w, e.lo, e.hi, pass, last);
+      pick_digit(l, l.hist[BINS - 1 - 2 * tid], l.hist[BINS - 2 - 2 * tid], pass, last);
+    }
+  write_kept(l, e.w, e.kept, e.nw, 0, e.n, e.lo, e.hi, e.need > 0, last, 0, 0);
+}
+
+// The same in chunks: a launch for each digit (pass 0, 1, 2), and one that writes (3).
+__global__ __launch_bounds__(EV) void evict_chunk_kernel(const Evict a, int pass) {
+  __shared__ EvictLds l;
+  const int c = blockIdx.x, h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
+  const EvictHead e = evict_head(a, s, h);
+  if (pass == 3 && evict_ends(a, e, s, h, c, a.chunks)) return;
+  if (e.n <= a.budget) return;
+  const int b0 = imin(e.n, c * a.chunk), b1 = imin(e.n, b0 + a.chunk);
+  int* const mine = a.hist + (((size_t)s * a.c.Hkv + h) * a.chunks) * 3 * BINS;   // [chunk][digit][bin]
+  Last last = {0u, 0u, e.need};
+  int out = 0, ties = 0;
+  if (e.need > 0) {
+    for (int p = 0; p < pass; ++p) {
+      // this digit over all chunks, and over those before this one (bins BINS - 1 - 2 tid and the next)
+      int t0 = 0, t1 = 0, f0 = 0, f1 = 0;
+      const int* x = mine + p * BINS + BINS - 2 - 2 * tid;
+#pragma unroll 4
+      for (int k = 0; k < a.chunks; ++k) {
+        const int y1 = x[(size_t)k * 3 * BINS], y0 = x[(size_t)k * 3 * BINS + 1];
+        t0 += y0; t1 += y1;
+        if (k < c) { f0 += y0; f1 += y1; }
+      }
+      const int d = BINS - 1 - 2 * tid;
+      pick_digit(l, t0, t1, p, last);
+      if (pass == 3) {
+        const int at = (int)(last.prefix >> digit_shift(p) & digit_mask(p));
+        int total;
+        block_scan((d > at ? f0 : 0) + (d - 1 > at ? f1 : 0), l.red, &total);
+        out += total;
+        if (p == 2) {
+          block_scan((d == at ? f0 : 0) + (d - 1 == at ? f1 : 0), l.red, &total);
+          ties = total;
+        }
+      }
+    }
+  }
+  if (pass == 3) {
+    out += imin(b0, e.lo) + imax(0, b0 - e.hi);          // first and last tokens before the chunk
+    write_kept(l, e.w, e.kept, e.nw, b0, b1, e.lo, e.hi, e.need > 0, last, out, ties);
+  } else if (e.need > 0) {
+    histogram(l, e.w, imax(e.lo, b0), imin(e.hi, b1), pass, last);
+    int* x = mine + ((size_t)c * 3 + pass) * BINS;
+    for (int i = tid; i < BINS; i += EV) x[i] = l.hist[i];
   }
 }
 
@@ -233,9 +355,30 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const Evict a, int elem
   }
 }
 
-hipError_t launch_kv_evict(const Evict& a, int D, hipStream_t st) {
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)a.c.S, (unsigned)a.c.Hkv), dim3(EV), 0, st, a);
-  hipError_t e = hipGetLastError();
+int evict_chunks(int S, int Hkv, int capacity) {
+  if ((long long)S * Hkv >= 128 || capacity <= 2 * EVICT_CHUNK) return 1;
+  return imin(EVICT_MOST, cdiv(capacity, EVICT_CHUNK));
+}
+size_t evict_hist_ints(int S, int Hkv, int capacity) {
+  const int c = evict_chunks(S, Hkv, capacity);
+  return c > 1 ? (size_t)S * Hkv * c * 3 * BINS : 0;
+}
+
+hipError_t launch_kv_evict(const Evict& x, int D, hipStream_t st) {
+  Evict a = x;
+  const int capacity = a.c.max_pages * a.c.page_size;
+  a.chunks = evict_chunks(a.c.S, a.c.Hkv, capacity);
+  a.chunk = cdiv(cdiv(capacity, a.chunks), EVICT_CHUNK) * EVICT_CHUNK;
+  hipError_t e = hipSuccess;
+  if (a.chunks > 1) {
+    for (int pass = 0; pass < 4 && e == hipSuccess; ++pass) {
+      hipLaunchKernelGGL(evict_chunk_kernel, dim3((unsigned)a.chunks, (unsigned)a.c.Hkv, (unsigned)a.c.S), dim3(EV), 0, st, a, pass);
+      e = hipGetLastError();
+    }
+  } else {
+    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)a.c.S, (unsigned)a.c.Hkv), dim3(EV), 0, st, a);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess) return e;
   const int elem = a.c.k_scale ? 1 : 2, rb = D * elem, per = 256 / (rb / 16);
   const dim3 grid((unsigned)imin(cdiv(a.budget, per), imax(1, 8192 / imax(1, imin(8192, a.c.S * a.c.Hkv)))),

@@ -25,12 +25,15 @@ struct WindowBwd {
   const float* lse;
   const int32_t* lens;     // may be null
   void *dq, *dk, *dv;      // contiguous
-  int B, Hq, Hkv, N, window, sinks, chunks;
+  int B, Hq, Hkv, N, window, sinks;
+  int chunks, mchunks, mshare;           // of the sinks' query tiles, of the other keys', and tiles in one of these
   Strides qs, ks, vs, os, gs;            // gs: dout
   float c2, rsd;           // rsd = 1 / sqrt(D)
-  float *lb, *delta, *norms, *part;      // workspace
+  float *lb, *delta, *norms, *part, *mpart;   // workspace
 };
 int window_bwd_chunks(int B, int Hq, int Hkv, int N, int sinks);
+int window_bwd_share(int B, int Hq, int Hkv, int N, int window, int* chunks);
+size_t window_bwd_mpart_floats(int B, int Hkv, int N, int D, int chunks);
 size_t window_bwd_row_floats(int B, int Hq, int N);
 size_t window_bwd_norm_floats(int B, int Hq, int Hkv, int N);
 size_t window_bwd_part_floats(int B, int Hq, int Hkv, int N, int D, int sinks);
@@ -85,7 +88,10 @@ struct Evict {
   int32_t *new_lens, *kept;
   long long wstride, new_wstride;
   int new_max_pages, budget, keep_first, keep_last;
+  int* hist;                             // workspace; chunks and chunk are the launcher's
+  int chunks, chunk;
 };
+size_t evict_hist_ints(int S, int Hkv, int capacity);
 hipError_t launch_kv_evict(const Evict& a, int D, hipStream_t st);
 
 }  // namespace sage

@@ -93,16 +93,20 @@ sage::Cache cache_of(const sage_kv_cache* c, const int32_t* table, int max_pages
 }
 
 struct BwdWs {
-  size_t lb, delta, norms, part, total;
+  size_t lb, delta, norms, part, mpart, total;
+  int chunks, mchunks, mshare;
 };
-BwdWs bwd_ws(int B, int Hq, int Hkv, int N, int D, int sinks) {
+BwdWs bwd_ws(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
   BwdWs w;
+  w.chunks = sage::window_bwd_chunks(B, Hq, Hkv, N, sinks);
+  w.mshare = sage::window_bwd_share(B, Hq, Hkv, N, window, &w.mchunks);
   size_t off = 0;
   const size_t rows = up256(sage::window_bwd_row_floats(B, Hq, N) * sizeof(float));
   w.lb = off; off += rows;
   w.delta = off; off += rows;
   w.norms = off; off += up256(sage::window_bwd_norm_floats(B, Hq, Hkv, N) * sizeof(float));
   w.part = off; off += up256(sage::window_bwd_part_floats(B, Hq, Hkv, N, D, sinks) * sizeof(float));
+  w.mpart = off; off += up256(sage::window_bwd_mpart_floats(B, Hkv, N, D, w.mchunks) * sizeof(float));
   w.total = off;
   return w;
 }
@@ -153,7 +157,7 @@ int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, f
 size_t sage_attn_window_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
   if (check_window(B, Hq, Hkv, N, D, window, sinks) != SAGE_OK) return 0;
   clamp_window(N, &window, &sinks);
-  return bwd_ws(B, Hq, Hkv, N, D, sinks).total;
+  return bwd_ws(B, Hq, Hkv, N, D, window, sinks).total;
 }
 
 int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* dout,
@@ -178,14 +182,15 @@ int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void
     if (!strides_ok(s, 8, kMaxRowStride)) return SAGE_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
   clamp_window(N, &a.window, &a.sinks);
-  const BwdWs w = bwd_ws(B, Hq, Hkv, N, D, a.sinks);
+  const BwdWs w = bwd_ws(B, Hq, Hkv, N, D, a.window, a.sinks);
   if (workspace_bytes < w.total) return SAGE_ERR_WORKSPACE;
   uint8_t* base = static_cast<uint8_t*>(workspace);
   a.lb = reinterpret_cast<float*>(base + w.lb);
   a.delta = reinterpret_cast<float*>(base + w.delta);
   a.norms = reinterpret_cast<float*>(base + w.norms);
   a.part = reinterpret_cast<float*>(base + w.part);
-  a.chunks = sage::window_bwd_chunks(B, Hq, Hkv, N, a.sinks);
+  a.mpart = reinterpret_cast<float*>(base + w.mpart);
+  a.chunks = w.chunks; a.mchunks = w.mchunks; a.mshare = w.mshare;
   a.c2 = softmax_c2(D);
   a.rsd = (float)(1.0 / std::sqrt((double)D));
   return hip_status(sage::launch_window_bwd(a, D, (flags & SAGE_IN_BF16) != 0, stream));
@@ -254,9 +259,17 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   return hip_status(sage::launch_paged_decode(a, cache->D, (flags & SAGE_IN_BF16) != 0, stream));
 }
 
+size_t sage_kv_evict_workspace_size(int S, int Hkv, int max_pages, int page_size) {
+  if (S <= 0 || S > kMaxSeqs || Hkv <= 0 || Hkv > kMaxHeads || max_pages <= 0 || page_size <= 0 ||
+      (long long)max_pages * page_size > kMaxCapacity)
+    return 0;
+  return std::max<size_t>(256, up256(sage::evict_hist_ints(S, Hkv, max_pages * page_size) * sizeof(int)));
+}
+
 int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
                   int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
-                  int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, hipStream_t stream) {
+                  int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream) {
   const int rc = check_cache(cache, table, max_pages, S, true);
   if (rc != SAGE_OK) return rc;
   if (!lens || !weights || !new_table || !new_lens || !new_weights || !kept) return SAGE_ERR_INVALID_ARG;
@@ -269,7 +282,10 @@ int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_page
     return SAGE_ERR_INVALID_ARG;
   // outputs that other workgroups still read would change under them
   if (new_lens == lens || new_weights == weights) return SAGE_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
+  if (workspace_bytes < sage_kv_evict_workspace_size(S, cache->Hkv, max_pages, cache->page_size)) return SAGE_ERR_WORKSPACE;
   sage::Evict a;
+  a.hist = static_cast<int*>(workspace);
   a.c = cache_of(cache, table, max_pages, S);
   a.lens = lens; a.new_table = new_table; a.weights = weights; a.new_weights = new_weights;
   a.new_lens = new_lens; a.kept = kept; a.wstride = weights_stride;

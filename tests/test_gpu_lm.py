@@ -547,6 +547,9 @@ EVICTS = [
     (1, 1, 64, [77, 30], 20, 20, 0, "bf16", True),
     (2, 64, 128, [700], 699, 0, 0, "fp16", False),
     (1, 128, 128, [40000], 1, 0, 0, "bf16", False),
+    (2, 64, 64, [40001, 9000, 16385], 9001, 8200, 100, "bf16", False),
+    (1, 256, 64, [200000], 150000, 3, 20000, "fp16", True),
+    (1, 32, 64, [20000], 300, 100, 200, "fp16", False),
 ]
 
 

@@ -1,6 +1,5 @@
 """Window attention, paged cache, one-token attention and eviction: every refusal
 happens on the host before any HIP call, in the C ABI and in the binding (no GPU)."""
-import ctypes
 import os
 
 import pytest
@@ -20,7 +19,7 @@ def L():
 
 
 def st(b=4 * 128 * 128, h=128 * 128, n=128):
-    return bd._Strides(b, h, n)
+    return bd._strides(b, h, n)
 
 
 def fwd(L, **kw):
@@ -67,35 +66,36 @@ def test_window_backward_workspace(L):
 
 
 def cache(**kw):
-    a = dict(k=FAKE, v=FAKE, k_scale=None, v_scale=None, ks=st(2 * 16 * 128, 16 * 128, 128), vs=st(2 * 16 * 128, 16 * 128, 128),
+    a = dict(k=FAKE, v=FAKE, k_scale=0, v_scale=0, ks=(2 * 16 * 128, 16 * 128, 128), vs=(2 * 16 * 128, 16 * 128, 128),
              pages=10, page_size=16, Hkv=2, D=128)
     a.update(kw)
-    return bd._Cache(*a.values())
+    a = [x for v in a.values() for x in (v if isinstance(v, tuple) else (v,))]
+    return bd._cache(*a)
 
 
 def append(L, c=None, **kw):
     a = dict(k=FAKE, v=FAKE, ks=None, vs=None, table=FAKE, M=4, pos=FAKE, counts=None, weights=None, ws=0, S=2, N=3, flags=4)
     a.update(kw)
-    return L.sage_kv_append(ctypes.byref(c or cache()), *a.values(), None)
+    return L.sage_kv_append(c or cache(), *a.values(), None)
 
 
 def decode(L, c=None, **kw):
     a = dict(q=FAKE, qss=4 * 128, qsh=128, o=FAKE, lse=None, table=FAKE, M=4, lens=FAKE, S=2, Hq=4, window=64, sinks=0, weights=None,
              wstride=0, flags=4, ws=FAKE, size=1 << 30)
     a.update(kw)
-    return L.sage_attn_paged_decode(ctypes.byref(c or cache()), *a.values(), None)
+    return L.sage_attn_paged_decode(c or cache(), *a.values(), None)
 
 
 def evict(L, c=None, **kw):
     a = dict(table=FAKE, M=4, lens=FAKE, weights=FAKE, wstride=64, new_table=FAKE, M2=2, budget=20, first=2, last=3,
-             new_lens=FAKE + 4096, new_weights=FAKE + 4096, kept=FAKE, S=2)
+             new_lens=FAKE + 4096, new_weights=FAKE + 4096, kept=FAKE, S=2, ws=FAKE, size=1 << 30)
     a.update(kw)
-    return L.sage_kv_evict(ctypes.byref(c or cache()), *a.values(), None)
+    return L.sage_kv_evict(c or cache(), *a.values(), None)
 
 
-CACHES = [dict(k=None), dict(v=FAKE + 8), dict(k_scale=FAKE), dict(k_scale=FAKE, v_scale=FAKE + 2), dict(pages=0), dict(page_size=0),
-          dict(Hkv=0), dict(D=96), dict(ks=st(n=4)), dict(vs=st(b=-8)), dict(page_size=1 << 29),
-          dict(k_scale=FAKE, v_scale=FAKE, ks=st(n=136))]     # 8-bit rows start on 16 bytes too
+CACHES = [dict(k=0), dict(v=FAKE + 8), dict(k_scale=FAKE), dict(k_scale=FAKE, v_scale=FAKE + 2), dict(pages=0), dict(page_size=0),
+          dict(Hkv=0), dict(D=96), dict(ks=(4096, 2048, 4)), dict(vs=(-8, 2048, 128)), dict(page_size=1 << 29),
+          dict(k_scale=FAKE, v_scale=FAKE, ks=(4352, 2176, 136))]     # 8-bit rows start on 16 bytes too
 
 
 @pytest.mark.parametrize("bad", CACHES)
@@ -104,7 +104,7 @@ def test_cache_refusals(L, bad):
         assert f(L, cache(**bad)) == INVALID, f.__name__
 
 
-@pytest.mark.parametrize("bad", [dict(ks=st(2 * 16 * 128, 16 * 128, 64)), dict(vs=st(0, 16 * 128, 128)), dict(vs=st(2 * 16 * 128, 0, 128))])
+@pytest.mark.parametrize("bad", [dict(ks=(2 * 16 * 128, 16 * 128, 64)), dict(vs=(0, 16 * 128, 128)), dict(vs=(2 * 16 * 128, 0, 128))])
 def test_written_caches_have_no_rows_in_common(L, bad):
     for f in (append, evict):
         assert f(L, cache(**bad)) == INVALID, f.__name__
@@ -138,9 +138,19 @@ def test_decode_workspace(L):
 
 @pytest.mark.parametrize("bad", [dict(lens=None), dict(weights=None), dict(new_table=None), dict(new_lens=None), dict(new_weights=None),
                                  dict(kept=FAKE + 2), dict(budget=0), dict(budget=33), dict(first=-1), dict(first=18), dict(last=-1),
-                                 dict(M2=0), dict(wstride=63), dict(new_lens=FAKE), dict(new_weights=FAKE), dict(S=70000)])
+                                 dict(M2=0), dict(wstride=63), dict(new_lens=FAKE), dict(new_weights=FAKE), dict(S=70000), dict(ws=None), dict(ws=FAKE + 64)])
 def test_evict_refusals(L, bad):
     assert evict(L, **bad) == INVALID
+
+
+def test_evict_workspace(L):
+    need = bd.kv_evict_workspace_size(2, 2, 100, 1000)
+    assert need >= 2 * 2 * 13 * 3 * 2048 * 4
+    big = cache(page_size=1000, ks=(256000, 128000, 128), vs=(256000, 128000, 128))
+    assert evict(L, big, M=100, wstride=100000, size=need - 1) == WORKSPACE
+    assert evict(L, size=255) == WORKSPACE
+    for bad in ((0, 2, 1, 1), (2, 0, 1, 1), (2, 2, 0, 1), (2, 2, 1 << 16, 1 << 16)):
+        assert bd.kv_evict_workspace_size(*bad) == 0
 
 
 def test_binding_refuses_host_tensors_and_wrong_types():
