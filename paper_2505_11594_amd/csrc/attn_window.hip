@@ -10,6 +10,11 @@
 // computes only those that its own 32 queries see; scores are masked in the tiles
 // on the diagonal and at the two edges of the window.
 //
+// Bound by issue: per 32 x 64 piece of D = 128 the 32 MFMAs take 1024 cycles of a SIMD,
+// 32 exponentials 512 and the other VALU work about 400, and the two waves of a SIMD
+// hide little of one kind under the other.  32768 tokens, 32/8 heads, window 4096:
+// 2.2-2.35 ms over several boxes, 880-940 TFLOP/s (a large bf16 matrix product: 1200).
+//
 // P is rounded to the input's type for the second product (relative error 2^-8
 // in bf16, 2^-11 in fp16 per probability); everything else is fp32.
 #include "bf16_tile.h"
@@ -49,9 +54,11 @@ __device__ __forceinline__ void split_nonfinite(const v4i x, v4i& fin, v4i& pos,
 
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * WW, 2) void window_fwd_kernel(const WindowFwd a) {
-  constexpr int NSUB = WK / 32, NKS = D / 16, NPK = WK / 16, NDB = D / 32;
+  constexpr int NKS = D / 16, NDB = D / 32;
+  constexpr float LAZY = 8.0f, SHIFT = BF16 ? 0.0f : kPShift<false> - LAZY;   // fp16: P at most 2^15 all the same
+  static_assert(WK == 64, "a tile is two 32-key pieces");
   constexpr int ROW = D * 2, CH = ROW / 16, TB = WK * ROW;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TB];   // two stages of a K tile and a V tile
+  __shared__ __attribute__((aligned(256))) uint8_t lds[4 * TB];  // two stages of a K tile and a V tile
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5;
   const int nqt = cdiv(a.N, 32 * WW);
@@ -82,14 +89,11 @@ __global__ __launch_bounds__(64 * WW, 2) void window_fwd_kernel(const WindowFwd 
   // Tile loads as in attn_bf16.hip, with the rows' stride; rows past n read zero.
   constexpr int JR = 1024 / ROW, NJ = WK / JR, JW = NJ / WW;
   static_assert(NJ % WW == 0, "every wave loads the same number of pieces");
-  uint32_t klo[JW], vlo[JW];
+  static_assert(WW * JR % 16 == 0 || D == 64, "a lane's pieces have the same swizzle");
+  static_assert(WW * JR % 32 == 0 || D == 128, "a lane's pieces have the same swizzle");
   const uint32_t kst = (uint32_t)(a.ks.n * 2), vst = (uint32_t)(a.vs.n * 2);
-#pragma unroll
-  for (int i = 0; i < JW; ++i) {
-    const int r = (wave + WW * i) * JR + lane / CH;
-    klo[i] = r * kst + bswz<CH>(r, lane % CH) * 16;
-    vlo[i] = r * vst + vswz<D>(r, lane % CH) * 16;
-  }
+  const int jr = wave * JR + lane / CH;
+  const uint32_t klo = jr * kst + bswz<CH>(jr, lane % CH) * 16, vlo = jr * vst + vswz<D>(jr, lane % CH) * 16;
   const uint8_t* kbase = (const uint8_t*)a.k + 2 * (b * a.ks.b + hk * a.ks.h);
   const uint8_t* vbase = (const uint8_t*)a.v + 2 * (b * a.vs.b + hk * a.vs.h);
   auto issue = [&](int kb, int stage) {
@@ -97,25 +101,126 @@ __global__ __launch_bounds__(64 * WW, 2) void window_fwd_kernel(const WindowFwd 
     const uint32_t rows = (uint32_t)min(n - kb, WK);
     const __amdgpu_buffer_rsrc_t rk = make_rsrc(kbase + (size_t)kb * kst, (rows - 1) * kst + ROW);
     const __amdgpu_buffer_rsrc_t rv = make_rsrc(vbase + (size_t)kb * vst, (rows - 1) * vst + ROW);
+    const uint32_t k0 = opaque(klo), v0 = opaque(vlo);
 #pragma unroll
     for (int i = 0; i < JW; ++i) {
-      buf_load16(rk, klo[i], 0u, L + (wave + WW * i) * 1024);
-      buf_load16(rv, vlo[i], 0u, L + TB + (wave + WW * i) * 1024);
+      buf_load16(rk, k0 + WW * JR * i * kst, 0u, L + (wave + WW * i) * 1024);
+      buf_load16(rv, v0 + WW * JR * i * vst, 0u, L + TB + (wave + WW * i) * 1024);
     }
   };
 
-  uint32_t vo[NDB];
-  {
-    const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    const int r = 4 * hi + (lane & 15) / 4, c0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) vo[db] = l0 + TB + r * ROW + vswz<D>(r, 4 * db + c0) * 16 + 8 * (lane & 1);
-  }
+  const uint32_t l0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+  const uint32_t rat = row_at<D, true>(), tat = tr_at<D>();
 
   v16f oacc[NDB];
   float m, l;
-  auto attend = [&](auto CAREFUL_) {
+  // NS 32-key pieces of the tile at stage, from its row `off` on, key kb; hide0 / hide1: not that one
+  auto piece = [&](auto NS_, auto CAREFUL_, int stage, int off, int kb, bool hide0, bool hide1) {
+    constexpr int NS = decltype(NS_)::value;
     constexpr bool CAREFUL = decltype(CAREFUL_)::value != 0;
+    const uint32_t L = l0 + stage * 2 * TB + off * ROW;  // (32 rows on, the swizzle is the same)
+    v16f sacc[NS];
+    {
+      const uint32_t ra = opaque(L + rat);
+      if (NS == 2 && !hide0 && !hide1) {                 // the two halves in turn: neither waits for its own last result
+        sacc[0] = sacc[NS - 1] = v16f{};
+#pragma unroll
+        for (int s = 0; s < NKS; ++s) {
+          sacc[0] = mma32<BF16>(lds16(ra ^ (32 * s)), qreg[s], sacc[0]);
+          sacc[NS - 1] = mma32<BF16>(lds16((ra ^ (32 * s)) + 32 * ROW), qreg[s], sacc[NS - 1]);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < NS; ++t) {
+          v16f acc = v16f{};
+          if (!(t ? hide1 : hide0)) {
+#pragma unroll
+            for (int s = 0; s < NKS; ++s) acc = mma32<BF16>(lds16((ra ^ (32 * s)) + 32 * t * ROW), qreg[s], acc);
+          }
+          sacc[t] = acc;
+        }
+      }
+    }
+    if (kb + 32 * NS - 1 > qw || kb + 32 * NS > n || (kb <= qw + 31 - W && kb + 32 * NS > sinks)) {
+      // element (t, e) is key kb + 4 hi + c with c = 32t + 8 (e >> 2) + (e & 3), kept iff
+      // c < rem and (c >= low or c < sk): a sign mask selects its bits or those of -inf
+      // (a minimum with -inf would let the NaN of a masked key through)
+      const int base = kb + 4 * hi, rem = min(n, qi + 1) - base, low = qi - W + 1 - base, sk = sinks - base;
+#pragma unroll
+      for (int t = 0; t < NS; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int c = 32 * t + 8 * (e >> 2) + (e & 3);
+          const uint32_t keep = (uint32_t)(((c - rem) & ~((c - low) & ~(c - sk))) >> 31);
+          sacc[t][e] = __uint_as_float((__float_as_uint(sacc[t][e]) & keep) | (0xFF800000u & ~keep));
+        }
+    }
+    float x = sacc[0][0];
+#pragma unroll
+    for (int t = 0; t < NS; ++t)
+#pragma unroll
+      for (int e = (t == 0 ? 1 : 0); e < 16; ++e) x = smax(x, sacc[t][e]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float m_new = smax(m, smax(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+    // The sums are rescaled only when some row's maximum has grown by more than 2^LAZY
+    // (a row's first key always has): until then its probabilities are up to 2^LAZY
+    // larger.  Of 32 rows one has a new maximum in most of the first 30 tiles.
+    if (__builtin_amdgcn_ballot_w64((m_new - m) * a.c2 > LAZY) != 0) {
+      // (a row that has seen no key yet keeps m = -inf: 0 in its place is as good)
+      const float alpha = __builtin_amdgcn_exp2f(m * a.c2 - (m_new == -INFINITY ? 0.0f : m_new * a.c2));   // 0 the first time
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
+    }
+    // against 0 the probabilities of a row that has seen no key are 0, not NaN
+    const float mp = (m == -INFINITY ? 0.0f : m * a.c2) - SHIFT;
+    const uint32_t va = opaque(L + TB + tat);
+    float ps[2] = {0.0f, 0.0f};
+    static_for<2 * NS>([&](auto U_) {
+      constexpr int u = decltype(U_)::value, t = u >> 1, base = 8 * (u & 1);
+      if (t ? hide1 : hide0) return;
+      v8bf vt[NDB];
+      constexpr int OFF = 16 * u * ROW, OFF8 = OFF + 8 * ROW;
+      if constexpr (NDB == 4) vt_read4<OFF, OFF8>(va, va ^ 64, va ^ 128, va ^ 192, vt[0], vt[1], vt[2], vt[3]);
+      else vt_read2<OFF, OFF8>(va, va ^ 64, vt[0], vt[1]);
+      v4i pk;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][base + 2 * i], a.c2, -mp));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][base + 2 * i + 1], a.c2, -mp));
+        ps[i & 1] += p0;
+        ps[i & 1] += p1;
+        pk[i] = (int)pack16<BF16>(p0, p1);
+      }
+      if constexpr (CAREFUL) {
+        v4i see;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          see[i] = (int)pack16<BF16>(sacc[t][base + 2 * i] == -INFINITY ? 0.0f : 1.0f, sacc[t][base + 2 * i + 1] == -INFINITY ? 0.0f : 1.0f);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          v4i fin, pos, neg;
+          __builtin_amdgcn_sched_barrier(0);             // one block's operands at a time: registers
+          split_nonfinite<BF16>(__builtin_bit_cast(v4i, vt[db]), fin, pos, neg);
+          oacc[db] = mma32<BF16>(fin, pk, oacc[db]);
+          v16f c = mma32<BF16>(pos, see, v16f{});
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[db][e] += c[e] > 0.0f ? INFINITY : 0.0f;
+          c = mma32<BF16>(neg, see, v16f{});
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[db][e] -= c[e] > 0.0f ? INFINITY : 0.0f;
+        }
+      } else {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) oacc[db] = mma32<BF16>(__builtin_bit_cast(v4i, vt[db]), pk, oacc[db]);
+      }
+    });
+    l += ps[0] + ps[1];
+  };
+  auto attend = [&](auto CAREFUL_) {
 #pragma unroll
     for (int db = 0; db < NDB; ++db) oacc[db] = v16f{};
     m = -INFINITY, l = 0.0f;
@@ -125,97 +230,22 @@ __global__ __launch_bounds__(64 * WW, 2) void window_fwd_kernel(const WindowFwd 
       __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): this wave's loads of tile j have landed
       __syncthreads();                                   // everyone's; every wave is past tile j - 1
       if (j + 1 < tl.count) issue(tl.tile(j + 1) * WK, (j + 1) & 1);
-      const uint8_t* L = lds + (j & 1) * 2 * TB;
       const int kb = tl.tile(j) * WK;
-      // keys past the wave's last query, or before its first query's window and behind the sinks
-      if (kb > qw + 31 || (kb + WK <= qw - W + 1 && kb >= sinks)) continue;
-      v16f sacc[NSUB];
-#pragma unroll
-      for (int t = 0; t < NSUB; ++t) {
-        const int row = 32 * t + col;
-        v16f acc = v16f{};
-#pragma unroll
-        for (int s = 0; s < NKS; ++s) {
-          const v4i x = *reinterpret_cast<const v4i*>(L + row * ROW + bswz<CH>(row, 2 * s + hi) * 16);
-          acc = mma32<BF16>(x, qreg[s], acc);
-        }
-        sacc[t] = acc;
+      // a half is hidden if it lies past the wave's last query, or before its first query's window
+      // and behind the sinks
+      const bool hide0 = kb > qw + 31 || (kb + 32 <= qw - W + 1 && kb >= sinks);
+      const bool hide1 = kb + 32 > qw + 31 || (kb + 64 <= qw - W + 1 && kb + 32 >= sinks);
+      if (hide0 && hide1) continue;
+      // D = 128: both halves in one softmax step, their scores computed in turn (2.29 -> 2.23 ms on
+      // 32768 tokens, window 4096, against a half after the other).  D = 64: a step for each, as
+      // 40 registers less are worth more than the shared step (54 -> 50 us on 8192 tokens, window 256).
+      if constexpr (D == 64) {
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t)
+          if (!(t ? hide1 : hide0)) piece(ic<1>{}, CAREFUL_, j & 1, 32 * t, kb + 32 * t, false, false);
+      } else {
+        piece(ic<2>{}, CAREFUL_, j & 1, 0, kb, hide0, hide1);
       }
-      if (kb + WK - 1 > qw || kb + WK > n || (kb <= qw + 31 - W && kb + WK > sinks)) {
-        // element (t, e) is key kb + 4 hi + c with c = 32t + 8 (e >> 2) + (e & 3), kept iff
-        // c < rem and (c >= low or c < sk): a sign mask selects its bits or those of -inf
-        // (a minimum with -inf would let the NaN of a masked key through)
-        const int base = kb + 4 * hi, rem = min(n, qi + 1) - base, low = qi - W + 1 - base, sk = sinks - base;
-#pragma unroll
-        for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int c = 32 * t + 8 * (e >> 2) + (e & 3);
-            const uint32_t keep = (uint32_t)(((c - rem) & ~((c - low) & ~(c - sk))) >> 31);
-            sacc[t][e] = __uint_as_float((__float_as_uint(sacc[t][e]) & keep) | (0xFF800000u & ~keep));
-          }
-      }
-      float x = sacc[0][0];
-#pragma unroll
-      for (int t = 0; t < NSUB; ++t)
-#pragma unroll
-        for (int e = (t == 0 ? 1 : 0); e < 16; ++e) x = smax(x, sacc[t][e]);
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      const float m_new = smax(m, smax(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
-      // a row that has seen no key yet keeps m = -inf: against 0 its probabilities are 0, not NaN
-      const float mc = m_new == -INFINITY ? 0.0f : m_new * a.c2;
-      const float alpha = __builtin_amdgcn_exp2f(m * a.c2 - mc);    // 0 on the first tile
-      m = m_new;
-      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-        for (int db = 0; db < NDB; ++db)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
-      }
-      const float mp = mc - kPShift<BF16>;
-      uint32_t va[NDB];
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) va[db] = vo[db] + (uint32_t)((j & 1) * 2 * TB);
-      float ps[2] = {0.0f, 0.0f};
-      static_for<NPK>([&](auto U_) {
-        constexpr int u = decltype(U_)::value, t = u >> 1, base = 8 * (u & 1);
-        v8bf vt[NDB];
-        constexpr int OFF = 16 * u * ROW, OFF8 = OFF + 8 * ROW;
-        if constexpr (NDB == 4) vt_read4<OFF, OFF8>(va[0], va[1], va[2], va[3], vt[0], vt[1], vt[2], vt[3]);
-        else vt_read2<OFF, OFF8>(va[0], va[1], vt[0], vt[1]);
-        v4i pk;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][base + 2 * i], a.c2, -mp));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[t][base + 2 * i + 1], a.c2, -mp));
-          ps[i & 1] += p0;
-          ps[i & 1] += p1;
-          pk[i] = (int)pack16<BF16>(p0, p1);
-        }
-        if constexpr (CAREFUL) {
-          v4i see;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            see[i] = (int)pack16<BF16>(sacc[t][base + 2 * i] == -INFINITY ? 0.0f : 1.0f, sacc[t][base + 2 * i + 1] == -INFINITY ? 0.0f : 1.0f);
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) {
-            v4i fin, pos, neg;
-            __builtin_amdgcn_sched_barrier(0);           // one block's operands at a time: registers
-            split_nonfinite<BF16>(__builtin_bit_cast(v4i, vt[db]), fin, pos, neg);
-            oacc[db] = mma32<BF16>(fin, pk, oacc[db]);
-            v16f c = mma32<BF16>(pos, see, v16f{});
-#pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[db][e] += c[e] > 0.0f ? INFINITY : 0.0f;
-            c = mma32<BF16>(neg, see, v16f{});
-#pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[db][e] -= c[e] > 0.0f ? INFINITY : 0.0f;
-          }
-        } else {
-#pragma unroll
-          for (int db = 0; db < NDB; ++db) oacc[db] = mma32<BF16>(__builtin_bit_cast(v4i, vt[db]), pk, oacc[db]);
-        }
-      });
-      l = l * alpha + (ps[0] + ps[1]);
     }
   };
   attend(ic<0>{});
@@ -232,7 +262,7 @@ __global__ __launch_bounds__(64 * WW, 2) void window_fwd_kernel(const WindowFwd 
   const bool live = qi < n;
   const float inv = live ? 1.0f / ltot : 0.0f;
   if (lrow && hi == 0)
-    *lrow = live ? (m * a.c2 + (__builtin_log2f(ltot) - kPShift<BF16>)) * 0.69314718055994530942f : -INFINITY;
+    *lrow = live ? (m * a.c2 + (__builtin_log2f(ltot) - SHIFT)) * 0.69314718055994530942f : -INFINITY;
 #pragma unroll
   for (int db = 0; db < NDB; ++db)
 #pragma unroll

@@ -38,8 +38,8 @@ __device__ __forceinline__ int seq_len(const WindowBwd& a, int b) { return a.len
 // Rows of a sequence's lb and delta arrays.
 __device__ __forceinline__ int row_pad(int N) { return (N + BT - 1) / BT * BT; }
 
-// lb = L log2(e) (+inf behind the sequence's end: P = 0 there) and delta per query
-// row; in fp16 also the largest |dO_i| (and, from blockIdx.y >= B Hq on, |V_j|) of
+// lb = -L log2(e) (and P's power of two; -inf behind the sequence's end: P = 0 there)
+// and -delta per query row, as the kernels add them; in fp16 also the largest |dO_i| (and, from blockIdx.y >= B Hq on, |V_j|) of
 // every PR rows.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void rows_kernel(const WindowBwd a) {
@@ -76,8 +76,8 @@ __global__ __launch_bounds__(256) void rows_kernel(const WindowBwd a) {
     }
     if (!vrows && ch == 0) {                             // (the arrays hold whole tiles of rows)
       const size_t at = (size_t)bh * row_pad(a.N) + i;
-      a.delta[at] = dot;
-      a.lb[at] = i < n ? a.lse[(size_t)bh * a.N + i] * kLog2e : INFINITY;
+      a.delta[at] = -dot;
+      a.lb[at] = i < n ? kPShift<BF16> - a.lse[(size_t)bh * a.N + i] * kLog2e : -INFINITY;
     }
     most = __builtin_fmaxf(most, sq);
   }
@@ -116,51 +116,19 @@ __device__ __forceinline__ float ds_scale(const WindowBwd& a, int b, int hk) {
   return __builtin_ldexpf(1.0f, imax(-100, imin(100, 15 - e)));
 }
 
-// A lane's LDS addresses in a tile at offset 0 of LDS: rows start on multiples of
-// their size, so the swizzled chunk is or-ed in, and the other chunks follow by xor with
-// constants: row_at ^ 32 i is chunk 2 i + hi of row l % 32, tr_at ^ 64 db the piece of
-// channel block db of the transposing read (see attn_window.hip).  They are made
-// opaque where they are used, as the compiler would keep every one in a register.
-template <int D>
-__device__ __forceinline__ uint32_t row_at() {
-  const int lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
-  return col * (D * 2) + vswz<D>(col, hi) * 16;
-}
-template <int D>
-__device__ __forceinline__ uint32_t tr_at() {
-  const int lane = threadIdx.x & 63, hi = lane >> 5;
-  const int r = 4 * hi + (lane & 15) / 4, c0 = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-  return r * (D * 2) + vswz<D>(r, c0) * 16 + 8 * (lane & 1);
-}
-__device__ __forceinline__ uint32_t opaque(uint32_t x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-__device__ __forceinline__ v4i lds16(uint32_t at) { return *(const __attribute__((address_space(3))) v4i*)at; }
-__device__ __forceinline__ v4f lds4f(uint32_t at) { return *(const __attribute__((address_space(3))) v4f*)at; }
-
-// S and dP: the 32 rows at `at` and TB bytes behind times the 32 columns of b and c, the
+// S and dP - delta: the 32 rows at `at` and TB bytes behind times the 32 columns of b and
+// c, the second on top of g (-delta), the
 // two products in turn (each alone would wait for its own last result, and its rows,
 // all read ahead, would not leave enough registers for two waves per SIMD).
 template <int D, bool BF16, int TB>
 __device__ __forceinline__ void rows_times(uint32_t at, const v4i* b, const v4i* c, v16f& s, v16f& g) {
-  s = g = v16f{};
+  s = v16f{};
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     s = mma32<BF16>(lds16(at ^ (32 * i)), b[i], s);
     g = mma32<BF16>(lds16((at + TB) ^ (32 * i)), c[i], g);
   }
 }
-// acc (dims x columns) += the transpose of 16 rows OFF bytes behind `at` times b.
-template <int D, bool BF16, int OFF>
-__device__ __forceinline__ void cols_times(uint32_t at, const v4i b, v16f* acc) {
-  v8bf x[D / 32];
-  if constexpr (D == 128) vt_read4<OFF, OFF + 8 * D * 2>(at, at ^ 64, at ^ 128, at ^ 192, x[0], x[1], x[2], x[3]);
-  else vt_read2<OFF, OFF + 8 * D * 2>(at, at ^ 64, x[0], x[1]);
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db) acc[db] = mma32<BF16>(__builtin_bit_cast(v4i, x[db]), b, acc[db]);
-}
-
 // The query tiles [t0, t1) of which some query sees one of the keys [k0, k0 + keys).
 struct TileRange {
   int t0, t1;
@@ -180,10 +148,17 @@ __device__ __forceinline__ void dkv_block(uint32_t L, uint32_t rat, uint32_t tat
   constexpr int ROW = D * 2, TB = BT * ROW;
   const int hi = (threadIdx.x & 63) >> 5;
   const uint32_t ra = opaque(L + t * 32 * ROW + rat);
-  v16f s, g;
-  rows_times<D, BF16, TB>(ra, kreg, vreg, s, g);
   // element e is query 32 t + 8 (e >> 2) + 4 hi + (e & 3) of the tile, visible iff first <= it < past
   const int at = 32 * t + 4 * hi;
+  const uint32_t la = opaque(L + 2 * TB + 4 * at);
+  v16f s, g;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const v4f dl = lds4f(la + 4 * BT + 32 * q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) g[4 * q + e] = dl[e];
+  }
+  rows_times<D, BF16, TB>(ra, kreg, vreg, s, g);
   if (mask) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -191,23 +166,18 @@ __device__ __forceinline__ void dkv_block(uint32_t L, uint32_t rat, uint32_t tat
       s[e] = c >= first && c < past ? s[e] : -INFINITY;
     }
   }
-  const uint32_t la = opaque(L + 2 * TB + 4 * at);
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const v4f lb = lds4f(la + 32 * q);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[4 * q + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * q + e], c2, kPShift<BF16> - lb[e]));
+    for (int e = 0; e < 4; ++e) s[4 * q + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * q + e], c2, lb[e]));
   }
   uint32_t pw[8], dw[8];
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const v4f dl = lds4f(la + 4 * BT + 32 * q);
     float d[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = g[4 * q + e] - dl[e];
-      d[e] = s[4 * q + e] * (BF16 ? x : x * f15);
-    }
+    for (int e = 0; e < 4; ++e) d[e] = s[4 * q + e] * (BF16 ? g[4 * q + e] : g[4 * q + e] * f15);
     pw[2 * q] = pack16<BF16>(s[4 * q], s[4 * q + 1]); pw[2 * q + 1] = pack16<BF16>(s[4 * q + 2], s[4 * q + 3]);
     dw[2 * q] = pack16<BF16>(d[0], d[1]); dw[2 * q + 1] = pack16<BF16>(d[2], d[3]);
   }
@@ -451,7 +421,10 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
     }
   }
   const size_t at = ((size_t)b * a.Hq + h) * row_pad(a.N) + qr;
-  const float lb = a.lb[at] - kPShift<BF16>, dl = a.delta[at];
+  const float lb = a.lb[at];
+  v16f dl;                                               // -delta, where dP's sums start
+#pragma unroll
+  for (int e = 0; e < 16; ++e) dl[e] = a.delta[at];
   const float f = ds_scale<BF16>(a, b, hk), f15 = f * 0x1p-15f;
 
   constexpr int JR = 1024 / ROW, NJ = BT / JR, JW = NJ / W;
@@ -492,7 +465,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
       const int kt = kb + 32 * t;
       if (kt > qw + 31 || (kt + 32 <= qw - win + 1 && kt >= sinks)) return;
       const uint32_t ra = opaque(L + t * 32 * ROW + rat);
-      v16f s, g;
+      v16f s, g = dl;
       rows_times<D, BF16, TB>(ra, qreg, greg, s, g);
       uint32_t dw[8];
       const bool mask = kt + 31 > qw || kt + 32 > n || (kt <= qw + 31 - win && kt + 32 > sinks);
@@ -500,8 +473,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
       float d[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c2, -lb)), x = g[e] - dl;
-        d[e] = p * (BF16 ? x : x * f15);
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c2, lb));
+        d[e] = p * (BF16 ? g[e] : g[e] * f15);
       }
       if (mask) {
 #pragma unroll

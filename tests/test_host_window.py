@@ -35,7 +35,7 @@ static void lists(int lo, int hi, int sinks, int T) {
 }
 // the forward kernel's tile loop for the queries of one wave
 static void forward(int n, int N, int W, int sinks) {
-  constexpr int WK = 64, WW = 4, NSUB = 2;
+  constexpr int WK = 64, WW = 4;
   for (int q0 = 0; q0 < N && q0 < n; q0 += 32 * WW)
     for (int wave = 0; wave < WW; ++wave)
       for (int col = 0; col < 32; ++col) {
@@ -45,19 +45,23 @@ static void forward(int n, int N, int W, int sinks) {
         static unsigned char got[4096];
         for (int j = 0; j < n; ++j) got[j] = 0;
         for (int j = 0; j < tl.count; ++j) {
-          const int kb = tl.tile(j) * WK;
-          @SKIP@
-          bool masked = false;
-          @COND@ masked = true;
-          for (int hi = 0; hi < 2; ++hi)
-            for (int t = 0; t < NSUB; ++t)
-              for (int e = 0; e < 16; ++e) {
-                @BASE@
-                const int c = 32 * t + 8 * (e >> 2) + (e & 3);
-                uint32_t keep_ = ~0u;
-                if (masked) { @KEEP@ keep_ = keep; }
-                if (keep_) { if (base + c >= n) ++bad; else ++got[base + c]; }
-              }
+          @HALVES@
+          const auto piece = [&](int NS, int kb) {
+            bool masked = false;
+            @COND@ masked = true;
+            for (int hi = 0; hi < 2; ++hi)
+              for (int t = 0; t < NS; ++t)
+                for (int e = 0; e < 16; ++e) {
+                  @BASE@
+                  const int c = 32 * t + 8 * (e >> 2) + (e & 3);
+                  uint32_t keep_ = ~0u;
+                  if (masked) { @KEEP@ keep_ = keep; }
+                  if (keep_) { if (base + c >= n) ++bad; else ++got[base + c]; }
+                }
+          };
+          if (hide0 && hide1) continue;
+          if (!hide0 && !hide1) piece(2, kb);
+          else piece(1, hide0 ? kb + 32 : kb);
         }
         for (int j = 0; j < n; ++j) { bad += got[j] != (sees(qi, j, n, W, sinks) ? 1 : 0); ++seen; }
       }
@@ -102,14 +106,14 @@ def between(src, a, b):
 def program(planted=False):
     src = open(os.path.join(CSRC, "attn_window.hip")).read()
     tiles = between(src, "const int q1 = min(q0 + 32 * WW, n);", "TileList{0, 0, 0};")
-    skip = between(src, "if (kb > qw + 31 ||", "continue;")
-    cond = between(src, "if (kb + WK - 1 > qw ||", ") {")[:-1]
+    halves = between(src, "const int kb = tl.tile(j) * WK;", "if (hide0 && hide1)")[:-len("if (hide0 && hide1)")]
+    cond = between(src, "if (kb + 32 * NS - 1 > qw ||", ") {")[:-1]
     base = between(src, "const int base = kb + 4 * hi,", ";")
     keep = between(src, "const uint32_t keep = ", ";")
     if planted:
         cond = cond.replace("kb <= qw + 31 - W", "kb < qw + 31 - W")
     text = MAIN
-    for name, code in (("@TILES@", tiles), ("@SKIP@", skip), ("@COND@", cond), ("@BASE@", base), ("@KEEP@", keep)):
+    for name, code in (("@TILES@", tiles), ("@HALVES@", halves), ("@COND@", cond), ("@BASE@", base), ("@KEEP@", keep)):
         text = text.replace(name, code)
     return text
 
