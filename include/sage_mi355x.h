@@ -435,7 +435,8 @@ int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, con
                    const int32_t* counts, float* weights, int64_t weights_stride, int S, int N, unsigned flags,
                    hipStream_t stream);
 
-/* Workspace bytes for sage_attn_paged_decode; 0 for invalid arguments.  Host only. */
+/* Workspace bytes for sage_attn_paged_decode; 0 where it needs none (short
+ * capacities, no weights) and for invalid arguments.  Host only. */
 size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int max_pages, int page_size, int with_weights);
 
 /*
@@ -450,14 +451,15 @@ size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int 
  *           token j, summed over the group's query heads, is added to
  *           weights[s][head][j]; weights_stride >= max_pages * page_size
  *  workspace: at least sage_attn_paged_decode_workspace_size() bytes, 256-byte
- *           aligned; calls that may overlap need one each
+ *           aligned (NULL if that is 0); calls that may overlap need one each
  */
 int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
                            float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,
                            int sinks, float* weights, int64_t weights_stride, unsigned flags, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);
 
-/* Workspace bytes for sage_kv_evict; 0 for invalid arguments.  Host only. */
+/* Workspace bytes for sage_kv_evict; 0 where it needs none (many sequences and
+ * heads, short capacities) and for invalid arguments.  Host only. */
 size_t sage_kv_evict_workspace_size(int S, int Hkv, int max_pages, int page_size);
 
 /*
@@ -475,6 +477,7 @@ size_t sage_kv_evict_workspace_size(int S, int Hkv, int max_pages, int page_size
  *               new_max_pages * page_size], their weights, 0 behind the last.
  *               None of them overlaps an input
  *  workspace  : at least sage_kv_evict_workspace_size() bytes, 256-byte aligned
+ *               (NULL if that is 0)
  * keep_first + keep_last <= budget.  Source pages are left as they were.
  */
 int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,

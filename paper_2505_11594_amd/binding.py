@@ -412,7 +412,7 @@ def _call(fn: str, device, *args):
     import torch
     index = device.index
     stream = torch._C._cuda_getCurrentRawStream(index)
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         rc = getattr(lib(), fn)(*args, stream)
     else:
         with torch.cuda.device(device):
@@ -428,16 +428,17 @@ def _adr(t):
 def _rows(t, what: str, ndim: int = 4):
     """A strided tensor with contiguous channels whose rows start on 16 bytes: its strides but the
     last (of a dimension of size 1, whose stride is never used, 0)."""
-    if t.dim() != ndim or not t.is_cuda or t.numel() == 0:
+    n, s = t.shape, t.stride()
+    if len(n) != ndim or not t.is_cuda or 0 in n:
         raise ValueError("%s must be a non-empty %d-d device tensor, got shape %s on %s"
-                         % (what, ndim, tuple(t.shape), t.device))
-    s, n = t.stride(), t.shape
-    s, last = [x if y > 1 else 0 for x, y in zip(s, n[:-1])], s[-1]
-    mask = 16 // t.element_size() - 1
-    if last != 1 or t.data_ptr() & 15 or any([x & mask for x in s]):
+                         % (what, ndim, tuple(n), t.device))
+    x = s[0] if n[0] > 1 else 0
+    y = s[1] if n[1] > 1 else 0
+    z = s[2] if ndim == 4 and n[2] > 1 else 0
+    if s[-1] != 1 or t.data_ptr() & 15 or (x | y | z) & (16 // t.element_size() - 1):
         raise ValueError("%s must have contiguous channels and rows on 16-byte addresses, got strides %s"
-                         % (what, tuple(t.stride())))
-    return s
+                         % (what, tuple(s)))
+    return (x, y, z) if ndim == 4 else (x, y)
 
 
 def _same(t, like, what: str, shape):
@@ -607,11 +608,12 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
         _check_tensor(L, "lse_out", (S, Hq), torch.float32, dev)
     if workspace is None:
         n = attn_paged_decode_workspace_size(S, Hq, Hkv, D, M, page, weights is not None)
-        workspace = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
-    _check_workspace(workspace, dev)
+        workspace = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    else:
+        _check_workspace(workspace, dev)
     _call("sage_attn_paged_decode", dev, c, _adr(q), qs[0], qs[1], _adr(o), _adr(L), _adr(table), M, _adr(lens),
           S, Hq, window, sinks, _adr(weights), weights.shape[2] if weights is not None else 0, flags, _adr(workspace),
-          workspace.numel())
+          workspace.numel() if workspace is not None else 0)
     return o, L
 
 
@@ -644,11 +646,13 @@ def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int
     for t, n, d, what in zip((new_lens, new_weights, kept), shapes, types, ("new_lens", "new_weights", "kept")):
         _check_tensor(t, what, n, d, dev)
     if workspace is None:
-        workspace = torch.empty(max(kv_evict_workspace_size(S, Hkv, M, page), 1), dtype=torch.uint8, device=dev)
-    _check_workspace(workspace, dev)
+        n = kv_evict_workspace_size(S, Hkv, M, page)
+        workspace = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    else:
+        _check_workspace(workspace, dev)
     _call("sage_kv_evict", dev, c, _adr(table), M, _adr(lens), _adr(weights), weights.shape[2], _adr(new_table),
           M2, budget, keep_first, keep_last, _adr(new_lens), _adr(new_weights), _adr(kept), S, _adr(workspace),
-          workspace.numel())
+          workspace.numel() if workspace is not None else 0)
     return new_lens, new_weights, kept
 
 

@@ -431,21 +431,32 @@ __global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) 
   }
 }
 
-// weights[j] += sum over the group's heads of exp(S - L), one thread per cached token.
+// weights[j] += sum over the group's heads of exp(S - L), four cached tokens per thread.
 __global__ __launch_bounds__(256) void add_weights_kernel(const Decode a) {
   const int s = blockIdx.z, hk = blockIdx.y, G = a.Hq / a.c.Hkv;
   const int n = cached_len(a.lens[s], a.c.max_pages * a.c.page_size);
   float* w = a.weights + ((size_t)s * a.c.Hkv + hk) * a.wstride;
   const float* sc = a.scores + ((size_t)s * a.Hq + (size_t)hk * G) * a.score_stride;
   const float* l2 = a.lse2 + (size_t)s * a.Hq + hk * G;
-  for (int j = blockIdx.x * 256 + threadIdx.x; j < n; j += gridDim.x * 256) {
-    if (!decode_sees(j, n, a.window, a.sinks)) continue;
-    float x = 0.0f;
+  for (int j = (blockIdx.x * 256 + threadIdx.x) * 4; j < n; j += gridDim.x * 1024) {
+    // (the scores of a tile of 32 are written together, those of unseen keys as -inf; other tiles hold nothing)
+    bool see[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) see[e] = decode_sees(j + e, n, a.window, a.sinks);
+    if (!(see[0] || see[1] || see[2] || see[3])) continue;
+    float old[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) old[e] = see[e] ? w[j + e] : 0.0f;
+    v4f x = v4f{};
+#pragma unroll 8
     for (int g = 0; g < G; ++g) {
-      const float y = sc[g * a.score_stride + j];
-      if (y != -INFINITY) x += __builtin_amdgcn_exp2f(y - l2[g]);
+      const v4f y = *reinterpret_cast<const v4f*>(sc + g * a.score_stride + j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(y[e] - l2[g]);
     }
-    w[j] += x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (see[e]) w[j + e] = old[e] + x[e];
   }
 }
 
@@ -478,7 +489,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   if (e == hipSuccess && a.weights) {
     const int capacity = a.c.max_pages * a.c.page_size;
     const int want = imax(1, 2048 / imax(1, imin(2048, a.c.S * a.c.Hkv)));
-    hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)imin(cdiv(capacity, 256), want), (unsigned)a.c.Hkv, (unsigned)a.c.S),
+    hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)imin(cdiv(capacity, 1024), want), (unsigned)a.c.Hkv, (unsigned)a.c.S),
                        dim3(256), 0, st, a);
     e = hipGetLastError();
   }

@@ -221,7 +221,7 @@ size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int 
   if (check_heads(Hq, Hkv, D) != SAGE_OK || S <= 0 || S > kMaxSeqs || max_pages <= 0 || page_size <= 0 ||
       (long long)max_pages * page_size > kMaxCapacity)
     return 0;
-  return std::max<size_t>(256, decode_ws(S, Hq, Hkv, D, max_pages * page_size, with_weights != 0).total);
+  return decode_ws(S, Hq, Hkv, D, max_pages * page_size, with_weights != 0).total;
 }
 
 int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
@@ -239,9 +239,11 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   if (!strides_ok(Strides{q_stride_s, q_stride_h, 0}, 8, 0)) return SAGE_ERR_INVALID_ARG;
   const int capacity = max_pages * cache->page_size;
   if (weights && weights_stride < capacity) return SAGE_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
   const DecodeWs w = decode_ws(S, Hq, cache->Hkv, cache->D, capacity, weights != nullptr);
-  if (workspace_bytes < w.total) return SAGE_ERR_WORKSPACE;
+  if (w.total > 0) {
+    if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
+    if (workspace_bytes < w.total) return SAGE_ERR_WORKSPACE;
+  }
   uint8_t* base = static_cast<uint8_t*>(workspace);
   sage::Decode a;
   a.c = cache_of(cache, table, max_pages, S);
@@ -263,7 +265,7 @@ size_t sage_kv_evict_workspace_size(int S, int Hkv, int max_pages, int page_size
   if (S <= 0 || S > kMaxSeqs || Hkv <= 0 || Hkv > kMaxHeads || max_pages <= 0 || page_size <= 0 ||
       (long long)max_pages * page_size > kMaxCapacity)
     return 0;
-  return std::max<size_t>(256, up256(sage::evict_hist_ints(S, Hkv, max_pages * page_size) * sizeof(int)));
+  return up256(sage::evict_hist_ints(S, Hkv, max_pages * page_size) * sizeof(int));
 }
 
 int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
@@ -282,8 +284,11 @@ int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_page
     return SAGE_ERR_INVALID_ARG;
   // outputs that other workgroups still read would change under them
   if (new_lens == lens || new_weights == weights) return SAGE_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
-  if (workspace_bytes < sage_kv_evict_workspace_size(S, cache->Hkv, max_pages, cache->page_size)) return SAGE_ERR_WORKSPACE;
+  const size_t need = sage_kv_evict_workspace_size(S, cache->Hkv, max_pages, cache->page_size);
+  if (need > 0) {
+    if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return SAGE_ERR_WORKSPACE;
+  }
   sage::Evict a;
   a.hist = static_cast<int*>(workspace);
   a.c = cache_of(cache, table, max_pages, S);

@@ -119,7 +119,8 @@ def test_append_refusals(L, bad):
 
 @pytest.mark.parametrize("bad", [dict(q=None), dict(q=FAKE + 8), dict(qsh=4), dict(qss=-8), dict(o=None), dict(lse=FAKE + 2),
                                  dict(lens=None), dict(S=0), dict(Hq=3), dict(Hq=0), dict(window=0), dict(sinks=-1), dict(flags=0x20),
-                                 dict(weights=FAKE, wstride=63), dict(weights=FAKE + 1, wstride=64), dict(ws=None), dict(ws=FAKE + 8),
+                                 dict(weights=FAKE, wstride=63), dict(weights=FAKE + 1, wstride=64), dict(ws=None, M=400),
+                                 dict(ws=FAKE + 8, weights=FAKE, wstride=64),
                                  dict(table=FAKE + 2)])
 def test_decode_refusals(L, bad):
     assert decode(L, **bad) == INVALID
@@ -131,14 +132,15 @@ def test_decode_workspace(L):
     c = cache(page_size=64)
     kw = dict(S=3, Hq=16, M=100, weights=FAKE, wstride=6400)
     assert decode(L, c, size=need - 1, **kw) == WORKSPACE
-    assert 256 <= bd.attn_paged_decode_workspace_size(3, 16, 2, 128, 100, 64) < need
+    assert 0 < bd.attn_paged_decode_workspace_size(3, 16, 2, 128, 100, 64) < need
+    assert bd.attn_paged_decode_workspace_size(3, 16, 2, 128, 8, 64) == 0      # short: nothing is split
     for bad in ((0, 16, 2, 128, 1, 1), (1, 16, 3, 128, 1, 1), (1, 16, 2, 100, 1, 1), (1, 16, 2, 128, 0, 1), (1, 16, 2, 128, 1 << 16, 1 << 16)):
         assert bd.attn_paged_decode_workspace_size(*bad) == 0
 
 
 @pytest.mark.parametrize("bad", [dict(lens=None), dict(weights=None), dict(new_table=None), dict(new_lens=None), dict(new_weights=None),
                                  dict(kept=FAKE + 2), dict(budget=0), dict(budget=33), dict(first=-1), dict(first=18), dict(last=-1),
-                                 dict(M2=0), dict(wstride=63), dict(new_lens=FAKE), dict(new_weights=FAKE), dict(S=70000), dict(ws=None), dict(ws=FAKE + 64)])
+                                 dict(M2=0), dict(wstride=63), dict(new_lens=FAKE), dict(new_weights=FAKE), dict(S=70000), dict(ws=None, M=2000, wstride=32000), dict(ws=FAKE + 64, M=2000, wstride=32000)])
 def test_evict_refusals(L, bad):
     assert evict(L, **bad) == INVALID
 
@@ -148,7 +150,7 @@ def test_evict_workspace(L):
     assert need >= 2 * 2 * 13 * 3 * 2048 * 4
     big = cache(page_size=1000, ks=(256000, 128000, 128), vs=(256000, 128000, 128))
     assert evict(L, big, M=100, wstride=100000, size=need - 1) == WORKSPACE
-    assert evict(L, size=255) == WORKSPACE
+    assert bd.kv_evict_workspace_size(64, 2, 100, 1000) == 0 == bd.kv_evict_workspace_size(1, 1, 100, 100)
     for bad in ((0, 2, 1, 1), (2, 0, 1, 1), (2, 2, 0, 1), (2, 2, 1 << 16, 1 << 16)):
         assert bd.kv_evict_workspace_size(*bad) == 0
 
