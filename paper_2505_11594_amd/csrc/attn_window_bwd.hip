@@ -395,11 +395,13 @@ __global__ __launch_bounds__(256) void join_keys_kernel(const WindowBwd a) {
 // where the second sum holds the rounded dS that the product took.  c is the mean
 // of the workgroup's last key tile.  (Error of dQ for keys N(0,1) with an N(0,1)
 // offset per channel, 8192 tokens, window 1024, bf16: 3.7e-3 without c.)
-template <int D, bool BF16>
-__global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
+// KG: groups of 4 waves that take the tiles in turn and are added at the end.
+template <int D, bool BF16, int KG>
+__global__ __launch_bounds__(256 * KG, 2 / KG) void dq_kernel(const WindowBwd a) {
   constexpr int W = 4, ROW = D * 2, CH = ROW / 16, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
-  __shared__ __attribute__((aligned(256))) uint8_t lds[4 * TB];  // two stages of a K tile and a V tile
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ __attribute__((aligned(256))) uint8_t lds[KG * 4 * TB];   // two stages of a K tile and a V tile per group
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = KG == 1 ? wid : wid % W, kg = KG == 1 ? 0 : wid / W, lgroup = kg * 4 * TB;
   const int col = lane & 31, hi = lane >> 5;
   const int nqt = cdiv(a.N, 32 * W);
   const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
   const uint8_t* kbase = (const uint8_t*)a.k + 2 * (b * a.ks.b + hk * a.ks.h);
   const uint8_t* vbase = (const uint8_t*)a.v + 2 * (b * a.vs.b + hk * a.vs.h);
   auto issue = [&](int kb, int stage) {
-    uint8_t* L = lds + stage * 2 * TB;
+    uint8_t* L = lds + lgroup + stage * 2 * TB;
     const uint32_t rows = (uint32_t)imin(n - kb, BT);
     const __amdgpu_buffer_rsrc_t rk = make_rsrc(kbase + (size_t)kb * kst, (rows - 1) * kst + ROW);
     const __amdgpu_buffer_rsrc_t rv = make_rsrc(vbase + (size_t)kb * vst, (rows - 1) * vst + ROW);
@@ -453,12 +455,14 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
   for (int db = 0; db < NDB; ++db) dq[db] = v16f{};
   float dsum = 0.0f;
 
-  if (tl.count > 0) issue(tl.tile(0) * BT, 0);
-  for (int j = 0; j < tl.count; ++j) {
+  if (kg < tl.count) issue(tl.tile(kg) * BT, 0);
+  for (int i = 0; i * KG < tl.count; ++i) {
     __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
-    if (j + 1 < tl.count) issue(tl.tile(j + 1) * BT, (j + 1) & 1);
-    const uint32_t L = l0 + (j & 1) * 2 * TB;
+    const int j = i * KG + kg;
+    if (j + KG < tl.count) issue(tl.tile(j + KG) * BT, (i + 1) & 1);
+    if (KG > 1 && j >= tl.count) continue;
+    const uint32_t L = l0 + lgroup + (i & 1) * 2 * TB;
     const int kb = tl.tile(j) * BT;
     static_for<2>([&](auto T_) {
       constexpr int t = decltype(T_)::value;
@@ -495,12 +499,14 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
       });
     });
   }
-  // c: the mean of the last tile's keys, summed in 256 / (D / 2) groups of rows
+  // c: the mean of the last tile's keys, summed in 256 / (D / 2) groups of rows.  It lies in
+  // its group's stage `last`; the sums go to that group's other stage.
   constexpr int NG = 512 / D;
-  float* const sums = reinterpret_cast<float*>(lds + (tl.count & 1) * 2 * TB);   // the stage that the last tile does not use
+  const int li = (tl.count - 1) / KG, lg = KG == 1 ? 0 : imax(0, tl.count - 1) % KG, last = li & 1;
+  float* const sums = reinterpret_cast<float*>(lds + lg * 4 * TB + (last ^ 1) * 2 * TB);
   const int kl = tl.count > 0 ? tl.tile(tl.count - 1) * BT : 0;
-  if (tl.count > 0) {
-    const uint8_t* L = lds + ((tl.count - 1) & 1) * 2 * TB;
+  if (tl.count > 0 && tid < 256) {
+    const uint8_t* L = lds + lg * 4 * TB + last * 2 * TB;
     const int ch = tid % (D / 2), g = tid / (D / 2);
     float x = 0.0f, y = 0.0f;
     for (int r = g; r < imin(n - kl, BT); r += NG) {
@@ -512,6 +518,32 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const WindowBwd a) {
     sums[g * D + 2 * ch + 1] = y;
   }
   __syncthreads();
+  if constexpr (KG == 2) {
+    // (behind the sums and the last tile's K, whose reads are over)
+    float* const x = reinterpret_cast<float*>(lds + (lg ^ 1) * 4 * TB) + wave * (NDB * 8 + 1) * 64 + lane;
+    for (int half = 0; half < 2; ++half) {               // half of the channel blocks at a time
+      if (kg == 1) {
+        if (half == 0) x[0] = dsum;
+#pragma unroll
+        for (int db = 0; db < NDB / 2; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[(1 + db * 16 + e) * 64] = half ? dq[NDB / 2 + db][e] : dq[db][e];
+      }
+      __syncthreads();
+      if (kg == 0) {
+        if (half == 0) dsum += x[0];
+#pragma unroll
+        for (int db = 0; db < NDB / 2; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            if (half) dq[NDB / 2 + db][e] += x[(1 + db * 16 + e) * 64];
+            else dq[db][e] += x[(1 + db * 16 + e) * 64];
+          }
+      }
+      __syncthreads();
+    }
+    if (kg == 1) return;
+  }
   if (qi >= a.N) return;
   dsum += __shfl_xor(dsum, 32, 64);
   dsum *= 1.0f / (float)imax(1, imin(n - kl, BT));
@@ -586,7 +618,10 @@ static hipError_t launch_window_bwd_t(const WindowBwd& a, hipStream_t st) {
     hipLaunchKernelGGL((join_sinks_kernel<D, BF16>), dim3((unsigned)a.sinks, heads), dim3(2 * D), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((dq_kernel<D, BF16>), dim3((unsigned)(a.B * a.Hq) * cdiv(a.N, 128)), dim3(256), 0, st, a);
+  // as in the forward: two groups of waves where there is a workgroup per CU or less
+  const unsigned blocks = (unsigned)(a.B * a.Hq) * cdiv(a.N, 128);
+  if (blocks <= 256) hipLaunchKernelGGL((dq_kernel<D, BF16, 2>), dim3(blocks), dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((dq_kernel<D, BF16, 1>), dim3(blocks), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

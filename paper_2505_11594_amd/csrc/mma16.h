@@ -65,8 +65,8 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x) {
   asm volatile("" : "+v"(x));
   return x;
 }
-__device__ __forceinline__ v4i lds16(uint32_t at) { return *(const __attribute__((address_space(3))) v4i*)at; }
-__device__ __forceinline__ v4f lds4f(uint32_t at) { return *(const __attribute__((address_space(3))) v4f*)at; }
+__device__ __forceinline__ v4i lds16(uint32_t at) { return *(const __attribute__((address_space(3))) v4i*)(uintptr_t)at; }
+__device__ __forceinline__ v4f lds4f(uint32_t at) { return *(const __attribute__((address_space(3))) v4f*)(uintptr_t)at; }
 
 // acc (dims x columns) += the transpose of 16 rows OFF bytes behind `at` times b.
 template <int D, bool BF16, int OFF>

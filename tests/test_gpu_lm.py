@@ -72,6 +72,11 @@ WINDOWS = [
     (4, 4, 2, 200, 64, "fp16", 50, 4, [200, 0, 1, 129]),
     (5, 2, 1, 300, 128, "bf16", None, 0, [300, 64, -7, 255, 1000]),
     (3, 7, 1, 513, 128, "bf16", 257, 1, [513, 512, 128]),
+    # more than a workgroup per CU: one group of waves each (the others run two)
+    (2, 32, 8, 600, 128, "bf16", 200, 4, [600, 333]),
+    (2, 32, 16, 600, 64, "fp16", 200, 40, None),
+    (1, 64, 4, 650, 64, "bf16", None, 0, None),
+    (1, 64, 32, 550, 128, "fp16", None, 0, None),
 ]
 
 
