@@ -19,7 +19,6 @@
 // device knows.  A part that is a whole sequence is final; others leave their
 // (maximum, sum, O) for join_kernel.  A share has at most two of them: one that
 // began before it (slot 0) and one that goes on behind it (slot 1).
-#include "bf16_tile.h"
 #include "lm_args.h"
 #include "mma16.h"
 #include "window.h"
@@ -43,52 +42,77 @@ __device__ __forceinline__ TileList seq_tiles(const Decode& a, int s, int* n) {
   return decode_tiles(*n, a.window, a.sinks, DT);
 }
 
-// Where a share begins on the line of all sequences' steps: every wave adds up
-// the steps of 64 sequences at a time.
+// The line of all sequences' steps.  Up to 64 sequences each wave adds up their steps
+// itself, one per lane; of more, line_kernel has left the steps before each in
+// a.before.
+constexpr int LINE = 64;
 struct Line {
   long long total, share;               // steps in all, and per workgroup
 };
-__device__ __forceinline__ int wave_sum(int x) {
+__device__ __forceinline__ int steps_of_lane(const Decode& a) {
+  const int lane = threadIdx.x & 63;
+  int n;
+  return lane < a.c.S ? cdiv(seq_tiles(a, lane, &n).count, DW) : 0;
+}
+__device__ __forceinline__ int lanes_up_to(int x) {      // inclusive sum over the lanes
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
   return x;
 }
-__device__ __forceinline__ Line steps_line(const Decode& a) {
-  const int lane = threadIdx.x & 63;
-  long long total = 0;
-  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
-    int n, c = 0;
-    if (s0 + lane < a.c.S) c = cdiv(seq_tiles(a, s0 + lane, &n).count, DW);
-    total += wave_sum(c);
-  }
+__device__ __forceinline__ Line steps_line(const Decode& a, int sum) {
   Line l;
-  l.total = total;
-  l.share = (total + a.nw - 1) / a.nw;
+  l.total = a.before ? a.before[a.c.S] : __shfl(sum, 63, 64);
+  l.share = (l.total + a.nw - 1) / a.nw;
   return l;
 }
-// The sequence that holds step r (r < total) and the steps before it.
-__device__ __forceinline__ int find_step(const Decode& a, long long r, long long* before) {
+// The sequence that holds step r < total, and the steps before it (c: this lane's
+// steps, sum: up to it).
+__device__ __forceinline__ int find_step(const Decode& a, int c, int sum, long long r, long long* before) {
   const int lane = threadIdx.x & 63;
-  long long base = 0;
-  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
-    int n, c = 0;
-    if (s0 + lane < a.c.S) c = cdiv(seq_tiles(a, s0 + lane, &n).count, DW);
-    int inc = c;                                             // inclusive sum over the lanes
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(inc, o, 64);
-      if (lane >= o) inc += y;
-    }
-    const unsigned long long past = __builtin_amdgcn_ballot_w64(base + inc > r);
-    if (past) {
-      const int first = __builtin_ctzll(past);
-      *before = base + __shfl(inc - c, first, 64);
-      return s0 + first;
-    }
-    base += __shfl(inc, 63, 64);
+  if (!a.before) {
+    const int first = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > r));
+    *before = __shfl(sum - c, first, 64);
+    return first;
   }
-  *before = base;
-  return a.c.S;
+  // the first s with before[s + 1] > r: 64 places are looked at at a time
+  int lo = 0, len = a.c.S;                               // it is in [lo, lo + len)
+  while (len > 1) {
+    const int step = cdiv(len, 64), s = lo + (lane + 1) * step;   // up to s: before[s] > r?
+    const unsigned long long past = __builtin_amdgcn_ballot_w64(s >= lo + len || a.before[s] > r);
+    const int first = __builtin_ctzll(past);
+    len = imin(step, len - first * step);
+    lo += first * step;
+  }
+  *before = a.before[lo];
+  return lo;
+}
+
+// Steps before each of many sequences, and in all.  One workgroup.
+__global__ __launch_bounds__(1024) void line_kernel(const Decode a) {
+  __shared__ int red[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  long long base = 0;
+  for (int s0 = 0; s0 < a.c.S; s0 += 1024) {
+    int n, c = 0;
+    if (s0 + tid < a.c.S) c = cdiv(seq_tiles(a, s0 + tid, &n).count, DW);
+    const int sum = lanes_up_to(c);
+    __syncthreads();
+    if (lane == 63) red[wave] = sum;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) before += red[w];
+      all += red[w];
+    }
+    if (s0 + tid < a.c.S) a.before[s0 + tid] = base + before + sum - c;
+    base += all;
+  }
+  if (tid == 0) a.before[a.c.S] = base;
 }
 
 // 16 int8 codes as 16 values of the type (exact).
@@ -135,27 +159,29 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
   constexpr int NKS = D / 32, NDB = D / 16;
   constexpr int PADQ = D + 4;                            // floats per head in the waves' join
   constexpr int REG = DG * PADQ * 4;                     // LDS bytes per wave: V tile, then its O
-  static_assert(REG >= DT * ROW, "a V tile fits");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[DW * REG + DW * DG * 8];
+  static_assert(REG >= DT * ROW && REG % 256 == 0, "a V tile fits; addresses inside it are xor-ed");
+  __shared__ __attribute__((aligned(256))) uint8_t lds[DW * REG + DW * DG * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, grp = lane >> 4;
   const int hk = blockIdx.y, G = a.Hq / a.c.Hkv, g0 = blockIdx.z * DG, gn = min(DG, G - g0);
   const int h0 = hk * G + g0;                            // first query head
   uint8_t* const vt = lds + wave * REG;
   const uint32_t vbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)vt;
-  uint32_t va[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db)
-    va[db] = vbase + (4 * grp + c16 / 4) * ROW + vswz<D>(4 * grp + c16 / 4, 2 * db + (c16 & 3) / 2) * 16 + 8 * (c16 & 1);
+  // block db's transposing read: vat ^ 32 db (rows start on multiples of their size)
+  const uint32_t vat = vbase + (4 * grp + c16 / 4) * ROW + vswz<D>(4 * grp + c16 / 4, (c16 & 3) / 2) * 16 + 8 * (c16 & 1);
 
   long long r0 = 0, r1 = 0, before = 0;
-  int s = blockIdx.x;
+  int s = blockIdx.x, mine = 0, upto = 0;
   if (a.nw > 0) {
-    const Line line = steps_line(a);
+    if (!a.before) {
+      mine = steps_of_lane(a);
+      upto = lanes_up_to(mine);
+    }
+    const Line line = steps_line(a, upto);
     r0 = min(line.total, blockIdx.x * line.share);
     r1 = min(line.total, r0 + line.share);
     if (r0 >= r1) return;
-    s = find_step(a, r0, &before);
+    s = find_step(a, mine, upto, r0, &before);
   }
   const int ps = a.c.page_size;
   for (;;) {
@@ -299,10 +325,11 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
           *reinterpret_cast<v4i*>(vt + row * ROW + vswz<D>(row, ch) * 16) = v;
         }
       }
+      const uint32_t va = opaque(vat);
       static_for<NDB / 4>([&](auto B_) {
         constexpr int b4 = 4 * decltype(B_)::value;
         v4i vv[4];
-        v_read4<D>(va[b4], va[b4 + 1], va[b4 + 2], va[b4 + 3], vv);
+        v_read4<D>(va ^ (32 * b4), va ^ (32 * b4 + 32), va ^ (32 * b4 + 64), va ^ (32 * b4 + 96), vv);
 #pragma unroll
         for (int d = 0; d < 4; ++d) oacc[b4 + d] = mma16<PB>(vv[d], pk, oacc[b4 + d]);
       });
@@ -366,11 +393,8 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
     }
     if (a.nw == 0) return;
     r0 += cnt;
-    before += steps;
     if (r0 >= r1) return;
-    ++s;
-    // sequences that have no steps hold no place on the line
-    for (int nn; s < a.c.S && seq_tiles(a, s, &nn).count == 0; ++s) {}
+    s = find_step(a, mine, upto, r0, &before);           // the next one that has steps
     __syncthreads();                                     // the next sequence's V tiles overwrite the join's LDS
   }
 }
@@ -382,15 +406,10 @@ __global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) 
   constexpr int CL = D / 64;                             // channels per lane
   __shared__ float sums[4][D + 1];
   const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Line line = steps_line(a);
-  int n;
-  const int steps = cdiv(seq_tiles(a, s, &n).count, DW);
-  long long before = 0;
-  for (int s0 = 0; s0 < s; s0 += 64) {
-    int nn, c = 0;
-    if (s0 + lane < s) c = cdiv(seq_tiles(a, s0 + lane, &nn).count, DW);
-    before += wave_sum(c);
-  }
+  const int mine = a.before ? 0 : steps_of_lane(a), upto = a.before ? 0 : lanes_up_to(mine);
+  const Line line = steps_line(a, upto);
+  const long long before = a.before ? a.before[s] : __shfl(upto - mine, s, 64);
+  const int steps = a.before ? (int)(a.before[s + 1] - before) : __shfl(mine, s, 64);
   const int w0 = steps > 0 ? (int)(before / line.share) : 0, w1 = steps > 0 ? (int)((before + steps - 1) / line.share) : -1;
   if (w0 == w1) return;                                  // final already
   const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
@@ -474,13 +493,22 @@ size_t decode_part_floats(int S, int Hq, int Hkv, int D, int capacity) {
   return (size_t)decode_workgroups(S, Hq, Hkv, capacity) * 2 * Hq * (D + 2);
 }
 
+size_t decode_line_longs(int S, int Hq, int Hkv, int capacity) {
+  return S > LINE && decode_workgroups(S, Hq, Hkv, capacity) > 0 ? (size_t)S + 1 : 0;
+}
+
 template <int D, bool BF16>
 static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   const int G = a.Hq / a.c.Hkv;
   const dim3 grid((unsigned)(a.nw > 0 ? a.nw : a.c.S), (unsigned)a.c.Hkv, (unsigned)cdiv(G, DG)), block(64 * DW);
+  hipError_t e = hipSuccess;
+  if (a.before) {
+    hipLaunchKernelGGL(line_kernel, dim3(1), dim3(1024), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   if (a.c.k_scale) hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((paged_decode_kernel<D, BF16, false>), grid, block, 0, st, a);
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
     const float shift = a.c.k_scale ? 0.0f : kPShift<BF16>;
     hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);

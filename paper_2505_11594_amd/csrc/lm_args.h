@@ -73,10 +73,12 @@ struct Decode {
   int Hq, window, sinks, nw;             // nw: workgroups that share the batch's steps (0: one per sequence)
   float c2;
   float* part;                           // per (workgroup, end, head): D sums, then (log2 maximum, sum)
+  long long* before;                     // steps before each of more than 64 sequences, or null
   float *lse2, *scores;                  // for weights: [S, Hq], [S, Hq, score_stride]
   long long score_stride;
 };
 int decode_workgroups(int S, int Hq, int Hkv, int capacity);
+size_t decode_line_longs(int S, int Hq, int Hkv, int capacity);
 size_t decode_part_floats(int S, int Hq, int Hkv, int D, int capacity);
 hipError_t launch_paged_decode(const Decode& a, int D, bool bf16, hipStream_t st);
 

@@ -112,7 +112,7 @@ BwdWs bwd_ws(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
 }
 
 struct DecodeWs {
-  size_t part, lse2, scores, total;
+  size_t part, line, lse2, scores, total;
   long long score_stride;
 };
 DecodeWs decode_ws(int S, int Hq, int Hkv, int D, int capacity, bool weights) {
@@ -120,6 +120,7 @@ DecodeWs decode_ws(int S, int Hq, int Hkv, int D, int capacity, bool weights) {
   size_t off = 0;
   w.score_stride = (capacity + 31LL) / 32 * 32;
   w.part = off; off += up256(sage::decode_part_floats(S, Hq, Hkv, D, capacity) * sizeof(float));
+  w.line = off; off += up256(sage::decode_line_longs(S, Hq, Hkv, capacity) * sizeof(long long));
   w.lse2 = off; off += weights ? up256((size_t)S * Hq * sizeof(float)) : 0;
   w.scores = off; off += weights ? up256((size_t)S * Hq * w.score_stride * sizeof(float)) : 0;
   w.total = off;
@@ -255,6 +256,7 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   a.nw = sage::decode_workgroups(S, Hq, cache->Hkv, capacity);
   a.c2 = softmax_c2(cache->D);
   a.part = reinterpret_cast<float*>(base + w.part);
+  a.before = w.lse2 > w.line ? reinterpret_cast<long long*>(base + w.line) : nullptr;
   a.lse2 = weights ? reinterpret_cast<float*>(base + w.lse2) : nullptr;
   a.scores = weights ? reinterpret_cast<float*>(base + w.scores) : nullptr;
   a.score_stride = w.score_stride;

@@ -409,22 +409,26 @@ def test_paged_decode(case):
     assert torch.equal(o, o2) and torch.equal(lse, lse2) and (w1 is None or torch.equal(w1, w2))
 
 
-def test_paged_decode_many_ragged_sequences():
-    """More sequences than a wave counts at a time, empty ones among them: every one as if it were alone
-    (up to the rounding of the split)."""
+@pytest.mark.parametrize("S,Hkv,empty", [(64, 4, False), (65, 1, False), (150, 2, True), (5000, 1, True)])
+def test_paged_decode_many_ragged_sequences(S, Hkv, empty):
+    """More sequences than a wave counts at a time, runs of empty ones among them: every one as if it
+    were alone (up to the rounding of the split)."""
     import torch
     g = gen(3)
-    S, Hkv, page, D = 150, 2, 16, 64
+    page, D = 16, 64
     lens = [int(x) for x in np.random.default_rng(4).integers(0, 900, S)]
-    lens[0], lens[63], lens[64], lens[149] = 0, 0, 899, 0
+    lens[0], lens[62], lens[-1] = 0, 899, 0
+    if empty:
+        lens[64:130] = [0] * 66
+        lens[1:3] = [0, 0]
     c, table, _ = make_cache(g, S, Hkv, page, D, lens, "bf16", False)
     q = randn(g, S, 4, D).to(torch.bfloat16)
     ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
     o, lse = bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], table, ln)
     torch.cuda.synchronize()
-    pick = [0, 1, 2, 62, 63, 64, 65, 127, 128, 147, 148, 149]
+    pick = sorted({i % S for i in (0, 1, 2, 3, 31, 62, 63, 64, 65, 127, 128, 129, 130, 131, S // 2, -3, -2, -1)})
     sub = torch.tensor(pick, device="cuda")
-    check_decode(q[sub], c, table[sub], [lens[i] for i in pick], None, 0, o[sub], lse[sub], None, None, "150 sequences")
+    check_decode(q[sub], c, table[sub], [lens[i] for i in pick], None, 0, o[sub], lse[sub], None, None, "%d sequences" % S)
 
 
 @pytest.mark.parametrize("int8", [False, True])
@@ -633,6 +637,103 @@ def test_evict_in_place_for_short_sequences_and_bad_pages():
     bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, ln, w, new_table, 32, 16, 16)
     torch.cuda.synchronize()
     assert all(torch.equal(c[x], again[x]) for x in again)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_caches_beyond_32_bit_offsets(int8):
+    """Pages behind 2^32 elements of the cache: stored, read and moved as in a small one."""
+    import torch
+    g = gen(51)
+    S, Hkv, page, D, lens = 2, 16, 256, 128, [700, 513]
+    c, table, spare = make_cache(g, S, Hkv, page, D, lens, "bf16", int8)
+    q = randn(g, S, 32, D).to(torch.bfloat16)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    kn, vn = (randn(g, S, Hkv, 1, D).to(torch.bfloat16) for _ in range(2))
+    w = torch.rand((S, Hkv, table.shape[1] * page), generator=g, device="cuda")
+    new_table = spare[:2].view(2, 1).contiguous()
+    P, n = c["k_cache"].shape[0], 2 ** 32 // (Hkv * page * D)
+    big = {}
+    for x, t in c.items():
+        big[x] = None
+        if t is not None:                                # the same pages, n places further on
+            big[x] = torch.empty((n + P,) + tuple(t.shape[1:]), dtype=t.dtype, device="cuda")
+            big[x][n:] = t
+    outs = []
+    for cc, off in ((c, 0), (big, n)):
+        tb, nt, ww = table + off, new_table + off, w.clone()
+        kw = dict(k_scale=cc["k_scale"], v_scale=cc["v_scale"])
+        args = (cc["k_cache"], cc["v_cache"], tb)
+        bd.sage_kv_append(kn, vn, *args, ln - 1, weights=ww, **kw)
+        o, lse = bd.sage_attn_paged_decode(q, *args, ln, weights=ww, **kw)
+        ev = bd.sage_kv_evict(*args, ln, ww, nt, 200, 3, 50, **kw)
+        o2, lse2 = bd.sage_attn_paged_decode(q, cc["k_cache"], cc["v_cache"], nt, ev[0], **kw)
+        torch.cuda.synchronize()
+        outs.append((o, lse, ww, *ev, o2, lse2))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    for x in c:
+        assert c[x] is None or torch.equal(big[x][n:], c[x])
+    del big
+
+
+def test_binding_refuses_mismatched_tensors():
+    import torch
+    q, k, v = qkv(1, 2, 4, 2, 64, 64, "bf16")
+    g = gen(1)
+    c, table, _ = make_cache(g, 2, 2, 16, 64, [40, 20], "bf16", False)
+    c8, _, _ = make_cache(g, 2, 2, 16, 64, [40, 20], "bf16", True)
+    kc, vc = c["k_cache"], c["v_cache"]
+    ln = torch.tensor([40, 20], dtype=torch.int32, device="cuda")
+    o, lse = bd.sage_attn_window_fwd(q, k, v)
+    w = torch.zeros((2, 2, 48), device="cuda")
+    bad = [
+        lambda: bd.sage_attn_window_fwd(q, k.half(), v),
+        lambda: bd.sage_attn_window_fwd(q, k[:, :, :-1], v),
+        lambda: bd.sage_attn_window_fwd(q, torch.cat([k, k[:, :1]], 1), torch.cat([v, v[:, :1]], 1)),
+        lambda: bd.sage_attn_window_fwd(q[..., 1:], k[..., 1:], v[..., 1:]),
+        lambda: bd.sage_attn_window_fwd(q, k, v, window=0),
+        lambda: bd.sage_attn_window_fwd(q, k, v, sinks=-1),
+        lambda: bd.sage_attn_window_fwd(q, k, v, lens=ln.long()),
+        lambda: bd.sage_attn_window_fwd(q, k, v, lens=ln[:1]),
+        lambda: bd.sage_attn_window_fwd(q, k, v, out=torch.empty_like(q).float()),
+        lambda: bd.sage_attn_window_fwd(q, k, v, lse_out=lse[:, :1]),
+        lambda: bd.sage_attn_window_bwd(q, k, v, o, lse.half(), q),
+        lambda: bd.sage_attn_window_bwd(q, k, v, o.float(), lse, q),
+        lambda: bd.sage_attn_window_bwd(q, k, v, o, lse, k),
+        lambda: bd.sage_attn_window_bwd(q, k, v, o, lse, q, out=(q, k, v.float())),
+        lambda: bd.sage_attn_window_bwd(q, k, v, o, lse, q, workspace=torch.empty(9, device="cuda")),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0].half(), kc, vc, table, ln),
+        lambda: bd.sage_attn_paged_decode(q[:, :3, 0], kc, vc, table, ln),
+        lambda: bd.sage_attn_paged_decode(q[:1, :, 0], kc, vc, table, ln),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc[:-1], table, ln),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc, table.long(), ln),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc, table.t(), ln),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc, table, ln.cpu()),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc, table, ln, weights=w[:, :, :47]),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc, table, ln, weights=w.double()),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], c8["k_cache"], c8["v_cache"], table, ln),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], kc, vc, table, ln, k_scale=c8["k_scale"], v_scale=c8["v_scale"]),
+        lambda: bd.sage_attn_paged_decode(q[:, :, 0], c8["k_cache"], c8["v_cache"], table, ln, k_scale=c8["k_scale"], v_scale=c8["v_scale"].half()),
+        lambda: bd.sage_kv_append(k.half(), v.half(), kc, vc, table, ln),
+        lambda: bd.sage_kv_append(k, v[:, :, 1:], kc, vc, table, ln),
+        lambda: bd.sage_kv_append(k[:1], v[:1], kc, vc, table, ln),
+        lambda: bd.sage_kv_append(k, v, kc, vc, table, ln[:1]),
+        lambda: bd.sage_kv_append(k, v, kc, vc, table, ln, counts=ln.float()),
+        lambda: bd.sage_kv_evict(kc, vc, table, ln, w, table[:, :1].contiguous(), 17),
+        lambda: bd.sage_kv_evict(kc, vc, table, ln, w, table[:1], 16),
+        lambda: bd.sage_kv_evict(kc, vc, table, ln, w[:, :1], table, 16),
+        lambda: bd.sage_kv_evict(kc, vc, table, ln, w, table, 16, 9, 8),
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises((ValueError, TypeError)):
+            f()
+            raise AssertionError(i)
+    # the library's own refusals come through as SageError
+    with pytest.raises(bd.SageError):
+        bd.sage_kv_append(k, v, kc[:1].expand(kc.shape), vc, table, ln)      # pages that are one and the same
+    with pytest.raises(bd.SageError):
+        bd.sage_attn_window_fwd(q, k, v, out=q[:, :1].expand(q.shape))
+    with pytest.raises(bd.SageError):
+        bd.sage_attn_window_bwd(q, k, v, o, lse, q, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
 
 
 # ---------------------------------------------------------------- together
