@@ -149,7 +149,9 @@ __device__ __forceinline__ void v_read4(uint32_t b0, uint32_t b1, uint32_t b2, u
 }
 
 // BF16: the type of q and o.  I8: 8-bit cache; its codes are exact in either type,
-// and P times V's scale, whose size nothing bounds, is rounded to bf16.
+// and P times V's scale, whose size nothing bounds, is taken in bf16.  P enters its
+// product with V in two parts, rounded and rest (together 2^-16 of it in bf16, 2^-22 in
+// fp16): the matrix instructions have the time.
 template <int D, bool BF16, bool I8>
 __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a) {
   constexpr bool PB = BF16 || I8;                        // type of P and V in the second product
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
       m = m_new;
       const float mp = mc - kPShift<PB>;
       float sum = 0.0f;
-      v4i pk;
+      v4i pk, pl;                                        // P's upper part, and what its rounding left
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         float p0 = __builtin_amdgcn_exp2f(sc[e >> 2][e & 3] - mp), p1 = __builtin_amdgcn_exp2f(sc[e >> 2][(e & 3) + 1] - mp);
@@ -301,7 +303,9 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
           p0 *= __shfl(cur.vs, key, 64);
           p1 *= __shfl(cur.vs, key + 1, 64);
         }
-        pk[e / 2] = (int)pack16<PB>(p0, p1);
+        const uint32_t hw = pack16<PB>(p0, p1);
+        pk[e / 2] = (int)hw;
+        pl[e / 2] = (int)pack16<PB>(p0 - widen<PB>((uint16_t)hw), p1 - widen<PB>((uint16_t)(hw >> 16)));
       }
       l = l * alpha + sum;
       if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
         v4i vv[4];
         v_read4<D>(va ^ (32 * b4), va ^ (32 * b4 + 32), va ^ (32 * b4 + 64), va ^ (32 * b4 + 96), vv);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) oacc[b4 + d] = mma16<PB>(vv[d], pk, oacc[b4 + d]);
+        for (int d = 0; d < 4; ++d) oacc[b4 + d] = mma16<PB>(vv[d], pl, mma16<PB>(vv[d], pk, oacc[b4 + d]));
       });
       id = id1;
       id1 = id2;

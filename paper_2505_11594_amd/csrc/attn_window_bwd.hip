@@ -396,6 +396,16 @@ __global__ __launch_bounds__(256) void join_keys_kernel(const WindowBwd a) {
 // of the workgroup's last key tile.  (Error of dQ for keys N(0,1) with an N(0,1)
 // offset per channel, 8192 tokens, window 1024, bf16: 3.7e-3 without c.)
 // KG: groups of 4 waves that take the tiles in turn and are added at the end.
+//
+// Where a row sees few keys, |O| is as large as |V| and d_i as large as the rounding of
+// dS itself.  Workgroups whose first row sees no more than EXACT keys (the first rows of
+// a sequence; all under a short window) walk their tiles twice: the first time (2
+// products) they add up sum_j P_ij (dP_ij - delta_i) in fp32, which is what delta is off
+// by, and put it right for themselves and for dK and dV behind them.  (15 tokens, bf16:
+// errors of dQ and dK 3.3e-3 -> 2.4e-3; their roundings alone give 2.3e-3.)  With more
+// keys of like weight d_i is small against dS's rounding.
+constexpr int EXACT = 256;
+
 template <int D, bool BF16, int KG>
 __global__ __launch_bounds__(256 * KG, 2 / KG) void dq_kernel(const WindowBwd a) {
   constexpr int W = 4, ROW = D * 2, CH = ROW / 16, TB = BT * ROW, NKS = D / 16, NDB = D / 32;
@@ -455,50 +465,76 @@ __global__ __launch_bounds__(256 * KG, 2 / KG) void dq_kernel(const WindowBwd a)
   for (int db = 0; db < NDB; ++db) dq[db] = v16f{};
   float dsum = 0.0f;
 
-  if (kg < tl.count) issue(tl.tile(kg) * BT, 0);
-  for (int i = 0; i * KG < tl.count; ++i) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);
-    __syncthreads();
-    const int j = i * KG + kg;
-    if (j + KG < tl.count) issue(tl.tile(j + KG) * BT, (i + 1) & 1);
-    if (KG > 1 && j >= tl.count) continue;
-    const uint32_t L = l0 + lgroup + (i & 1) * 2 * TB;
-    const int kb = tl.tile(j) * BT;
-    static_for<2>([&](auto T_) {
-      constexpr int t = decltype(T_)::value;
-      const int kt = kb + 32 * t;
-      if (kt > qw + 31 || (kt + 32 <= qw - win + 1 && kt >= sinks)) return;
-      const uint32_t ra = opaque(L + t * 32 * ROW + rat);
-      v16f s, g = dl;
-      rows_times<D, BF16, TB>(ra, qreg, greg, s, g);
-      uint32_t dw[8];
-      const bool mask = kt + 31 > qw || kt + 32 > n || (kt <= qw + 31 - win && kt + 32 > sinks);
-      const int base = kt + 4 * hi, rem = imin(n, qi + 1) - base, low = qi - win + 1 - base, sk = sinks - base;
-      float d[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c2, lb));
-        d[e] = p * (BF16 ? g[e] : g[e] * f15);
-      }
-      if (mask) {
+  auto walk = [&](auto FIRST_) {
+    constexpr bool FIRST = decltype(FIRST_)::value != 0;
+    if (kg < tl.count) issue(tl.tile(kg) * BT, 0);
+    for (int i = 0; i * KG < tl.count; ++i) {
+      __builtin_amdgcn_s_waitcnt(0x0F70);
+      __syncthreads();
+      const int j = i * KG + kg;
+      if (j + KG < tl.count) issue(tl.tile(j + KG) * BT, (i + 1) & 1);
+      if (KG > 1 && j >= tl.count) continue;
+      const uint32_t L = l0 + lgroup + (i & 1) * 2 * TB;
+      const int kb = tl.tile(j) * BT;
+      static_for<2>([&](auto T_) {
+        constexpr int t = decltype(T_)::value;
+        const int kt = kb + 32 * t;
+        if (kt > qw + 31 || (kt + 32 <= qw - win + 1 && kt >= sinks)) return;
+        const uint32_t ra = opaque(L + t * 32 * ROW + rat);
+        v16f s, g = dl;
+        rows_times<D, BF16, TB>(ra, qreg, greg, s, g);
+        uint32_t dw[8];
+        const bool mask = kt + 31 > qw || kt + 32 > n || (kt <= qw + 31 - win && kt + 32 > sinks);
+        const int base = kt + 4 * hi, rem = imin(n, qi + 1) - base, low = qi - win + 1 - base, sk = sinks - base;
+        float d[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int c = 8 * (e >> 2) + (e & 3);
-          d[e] = __uint_as_float(__float_as_uint(d[e]) & (uint32_t)(((c - rem) & ~((c - low) & ~(c - sk))) >> 31));
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.c2, lb));
+          d[e] = p * (BF16 ? g[e] : g[e] * f15);
         }
-      }
+        if (mask) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        dw[e] = pack16<BF16>(d[2 * e], d[2 * e + 1]);
-        dsum = add_pair<BF16>(dw[e], dsum);
-      }
-      const uint32_t ta = opaque(L + tat);
-      static_for<2>([&](auto U_) {
-        constexpr int u = decltype(U_)::value;
-        cols_times<D, BF16, (32 * t + 16 * u) * ROW>(ta, v4i{(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]}, dq);
+          for (int e = 0; e < 16; ++e) {
+            const int c = 8 * (e >> 2) + (e & 3);
+            d[e] = __uint_as_float(__float_as_uint(d[e]) & (uint32_t)(((c - rem) & ~((c - low) & ~(c - sk))) >> 31));
+          }
+        }
+        if constexpr (FIRST) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) dsum += d[e];
+          return;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          dw[e] = pack16<BF16>(d[2 * e], d[2 * e + 1]);
+          dsum = add_pair<BF16>(dw[e], dsum);
+        }
+        const uint32_t ta = opaque(L + tat);
+        static_for<2>([&](auto U_) {
+          constexpr int u = decltype(U_)::value;
+          cols_times<D, BF16, (32 * t + 16 * u) * ROW>(ta, v4i{(int)dw[4 * u], (int)dw[4 * u + 1], (int)dw[4 * u + 2], (int)dw[4 * u + 3]}, dq);
+        });
       });
-    });
+    }
+  };
+  if (imin(q0 + 1, win) <= EXACT) {
+    walk(ic<1>{});
+    dsum += __shfl_xor(dsum, 32, 64);
+    if constexpr (KG == 2) {
+      float* const x = reinterpret_cast<float*>(lds) + wave * 32 + col;
+      __syncthreads();
+      if (hi == 0) x[kg * 128] = dsum;
+      __syncthreads();
+      dsum = x[0] + x[128];
+    }
+    __syncthreads();                                     // the tiles' LDS is free again
+    dsum /= f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dl[e] -= dsum;
+    if (kg == 0 && hi == 0 && qi < n) a.delta[at] = dl[0];
+    dsum = 0.0f;
   }
+  walk(ic<0>{});
   // c: the mean of the last tile's keys, summed in 256 / (D / 2) groups of rows.  It lies in
   // its group's stage `last`; the sums go to that group's other stage.
   constexpr int NG = 512 / D;
@@ -605,6 +641,12 @@ static hipError_t launch_window_bwd_t(const WindowBwd& a, hipStream_t st) {
                      st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // dQ first, as it may put delta right.  As in the forward: two groups of waves where
+  // there is a workgroup per CU or less.
+  const unsigned blocks = (unsigned)(a.B * a.Hq) * cdiv(a.N, 128);
+  if (blocks <= 256) hipLaunchKernelGGL((dq_kernel<D, BF16, 2>), dim3(blocks), dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((dq_kernel<D, BF16, 1>), dim3(blocks), dim3(256), 0, st, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   const unsigned heads = (unsigned)(a.B * a.Hkv);
   hipLaunchKernelGGL((dkv_kernel<D, BF16, false>), dim3(heads * cdiv(a.N, 128) * a.mchunks), dim3(256), 0, st, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -618,11 +660,7 @@ static hipError_t launch_window_bwd_t(const WindowBwd& a, hipStream_t st) {
     hipLaunchKernelGGL((join_sinks_kernel<D, BF16>), dim3((unsigned)a.sinks, heads), dim3(2 * D), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  // as in the forward: two groups of waves where there is a workgroup per CU or less
-  const unsigned blocks = (unsigned)(a.B * a.Hq) * cdiv(a.N, 128);
-  if (blocks <= 256) hipLaunchKernelGGL((dq_kernel<D, BF16, 2>), dim3(blocks), dim3(512), 0, st, a);
-  else hipLaunchKernelGGL((dq_kernel<D, BF16, 1>), dim3(blocks), dim3(256), 0, st, a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 hipError_t launch_window_bwd(const WindowBwd& a, int D, bool bf16, hipStream_t st) {

@@ -339,7 +339,7 @@ def check_decode(q, c, table, lens, window, sinks, o, lse, w0, w1, label):
     S, Hq, D = q.shape
     Hkv, page = c["k_cache"].shape[1:3]
     G, u = Hq // Hkv, _lm.unit(q.dtype)
-    up = _lm.unit(torch.bfloat16) if c["k_scale"] is not None else u
+    up = (_lm.unit(torch.bfloat16) if c["k_scale"] is not None else u) ** 2   # P in two parts
     tab = table.cpu()
     worst = [0.0, 0.0, 0.0]
     for s in range(S):
