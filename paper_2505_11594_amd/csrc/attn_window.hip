@@ -131,6 +131,14 @@ __global__ __launch_bounds__(64 * WW * KG, 2 / KG) void window_fwd_kernel(const 
           sacc[0] = mma32<BF16>(lds16(ra ^ (32 * s)), qreg[s], sacc[0]);
           sacc[NS - 1] = mma32<BF16>(lds16((ra ^ (32 * s)) + 32 * ROW), qreg[s], sacc[NS - 1]);
         }
+        // four reads in front of the product that takes the first of them (the compiler alone reads,
+        // waits and multiplies in turn; 681 -> 668 us on 4 x 4096 tokens)
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int s = 0; s < 2 * NKS; ++s) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          if (s + 4 < 2 * NKS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
       } else {
 #pragma unroll
         for (int t = 0; t < NS; ++t) {
@@ -138,6 +146,12 @@ __global__ __launch_bounds__(64 * WW * KG, 2 / KG) void window_fwd_kernel(const 
           if (!(t ? hide1 : hide0)) {
 #pragma unroll
             for (int s = 0; s < NKS; ++s) acc = mma32<BF16>(lds16((ra ^ (32 * s)) + 32 * t * ROW), qreg[s], acc);
+            __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+            for (int s = 0; s < NKS; ++s) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              if (s + 3 < NKS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
           }
           sacc[t] = acc;
         }
