@@ -59,15 +59,14 @@ __global__ __launch_bounds__(64 * WW * KG, 2 / KG) void window_fwd_kernel(const 
   constexpr float LAZY = 8.0f, SHIFT = BF16 ? 0.0f : kPShift<false> - LAZY;   // fp16: P at most 2^15 all the same
   static_assert(WK == 64, "a tile is two 32-key pieces");
   constexpr int ROW = D * 2, CH = ROW / 16, TB = WK * ROW;
-  __shared__ __attribute__((aligned(256))) uint8_t lds[KG * 4 * TB];   // two stages of a K tile and a V tile per group
+  constexpr int GROUP = 4 * TB;                          // two stages of a K tile and a V tile per group of waves
+  __shared__ __attribute__((aligned(256))) uint8_t lds[KG * GROUP];
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wave = KG == 1 ? wid : wid % WW, kg = KG == 1 ? 0 : wid / WW, lgroup = kg * 4 * TB;
+  const int wave = KG == 1 ? wid : wid % WW, kg = KG == 1 ? 0 : wid / WW, lgroup = kg * GROUP;
   const int col = lane & 31, hi = lane >> 5;
   const int nqt = cdiv(a.N, 32 * WW);
 
-  // Each XCD takes a run of neighbouring tiles: they share keys, and heads of a group follow each other.
-  const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
-  const unsigned lin = xcd * (total >> 3) + min(xcd, total & 7u) + (blockIdx.x >> 3);
+  const unsigned lin = xcd_order(blockIdx.x, gridDim.x, a.B * a.Hkv);
   const int bh = (int)(lin / nqt), b = bh / a.Hq, h = bh - b * a.Hq, hk = h / (a.Hq / a.Hkv);
   const int qt = nqt - 1 - (int)(lin % nqt);                     // the longest rows first
   const int q0 = qt * (32 * WW), qw = q0 + wave * 32, qi = qw + col;
@@ -242,11 +241,16 @@ __global__ __launch_bounds__(64 * WW * KG, 2 / KG) void window_fwd_kernel(const 
     m = -INFINITY, l = 0.0f;
 
     if (kg < tl.count) issue(tl.tile(kg) * WK, 0);
+    // The queries' registers are waited for here, behind the first tile's loads: left to their first
+    // use, the compiler waits inside the loop, and for the tile in flight too (4 x 32 heads of 4096
+    // tokens: 667 -> 630 us).
+#pragma unroll
+    for (int s = 0; s < NKS; ++s) asm volatile("" : "+v"(qreg[s]));
     for (int i = 0; i * KG < tl.count; ++i) {
+      const int j = i * KG + kg, stage = i & 1;
       __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): this wave's loads of tile j have landed
-      __syncthreads();                                   // everyone's; every wave is past the tile before
-      const int j = i * KG + kg;
-      if (j + KG < tl.count) issue(tl.tile(j + KG) * WK, (i + 1) & 1);
+      lds_barrier();                                     // everyone's; every wave is past the tile before
+      if (j + KG < tl.count) issue(tl.tile(j + KG) * WK, stage ^ 1);
       if (KG > 1 && j >= tl.count) continue;
       const int kb = tl.tile(j) * WK;
       // a half is hidden if it lies past the wave's last query, or before its first query's window
@@ -260,9 +264,9 @@ __global__ __launch_bounds__(64 * WW * KG, 2 / KG) void window_fwd_kernel(const 
       if constexpr (D == 64) {
 #pragma unroll 1
         for (int t = 0; t < 2; ++t)
-          if (!(t ? hide1 : hide0)) piece(ic<1>{}, CAREFUL_, i & 1, 32 * t, kb + 32 * t, false, false);
+          if (!(t ? hide1 : hide0)) piece(ic<1>{}, CAREFUL_, stage, 32 * t, kb + 32 * t, false, false);
       } else {
-        piece(ic<2>{}, CAREFUL_, i & 1, 0, kb, hide0, hide1);
+        piece(ic<2>{}, CAREFUL_, stage, 0, kb, hide0, hide1);
       }
     }
   };

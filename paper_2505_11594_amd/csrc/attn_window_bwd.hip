@@ -214,8 +214,7 @@ __global__ __launch_bounds__(SINK ? 128 : 256, SINK ? 1 : 2) void dkv_kernel(con
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5;
   const int nkb = SINK ? cdiv(a.sinks, KB) : cdiv(a.N, KB);
-  const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
-  unsigned lin = xcd * (total >> 3) + min(xcd, total & 7u) + (blockIdx.x >> 3);
+  unsigned lin = xcd_order(blockIdx.x, gridDim.x, a.B * a.Hkv);
   const int chunks = SINK ? a.chunks : a.mchunks, chunk = (int)(lin % chunks);
   lin /= chunks;
   const int bh = (int)(lin / nkb), b = bh / a.Hkv, hk = bh - b * a.Hkv, G = a.Hq / a.Hkv;
@@ -422,8 +421,7 @@ __global__ __launch_bounds__(256 * KG, 2 / KG) void dq_kernel(const WindowBwd a)
   const int wave = KG == 1 ? wid : wid % W, kg = KG == 1 ? 0 : wid / W, lgroup = kg * 4 * TB;
   const int col = lane & 31, hi = lane >> 5;
   const int nqt = cdiv(a.N, 32 * W);
-  const unsigned total = gridDim.x, xcd = blockIdx.x & 7;
-  const unsigned lin = xcd * (total >> 3) + min(xcd, total & 7u) + (blockIdx.x >> 3);
+  const unsigned lin = xcd_order(blockIdx.x, gridDim.x, a.B * a.Hkv);
   const int bh = (int)(lin / nqt), b = bh / a.Hq, h = bh - b * a.Hq, hk = h / (a.Hq / a.Hkv);
   const int qt = nqt - 1 - (int)(lin % nqt), q0 = qt * (32 * W), qw = q0 + wave * 32, qi = qw + col;
   const int n = seq_len(a, b), win = a.window, sinks = a.sinks;

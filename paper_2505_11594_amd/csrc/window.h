@@ -46,7 +46,18 @@ SAGE_HD int cached_len(int n, int capacity) { return imax(0, imin(n, capacity));
 // A page id is used only if the cache has that page.
 SAGE_HD bool page_ok(int id, int pages) { return (unsigned)id < (unsigned)pages; }
 
-// Workgroup w of nw takes the steps [first, last) of `total`, equal shares.
-SAGE_HD int share_of(long long total, int nw) { return (int)((total + nw - 1) / nw); }
+// Which of `total` pieces of work, `groups` equal runs that share keys, a block takes.
+// Blocks go to the 8 XCDs in turn; every run stays on one (its keys in one L2).  Runs
+// are dealt out in turn where 8 divides them, so that sequences of differing lengths
+// spread over the XCDs; else each XCD takes an equal part of the line.
+SAGE_HD unsigned xcd_order(unsigned block, unsigned total, unsigned groups) {
+  const unsigned x = block & 7, i = block >> 3;
+  if (groups % 8 == 0) {
+    const unsigned per = total / groups, run = i / per;
+    return (run * 8 + x) * per + (i - run * per);
+  }
+  const unsigned more = total & 7;
+  return x * (total >> 3) + (x < more ? x : more) + i;
+}
 
 }  // namespace sage

@@ -90,6 +90,19 @@ int main() {
           ++seen;
         }
       }
+  for (unsigned groups : {1u, 2u, 3u, 7u, 8u, 16u, 24u, 96u, 100u})       // every piece once, runs on one XCD
+    for (unsigned per : {1u, 2u, 5u, 10u, 257u}) {
+      static int who[1 << 15];
+      const unsigned total = groups * per;
+      for (unsigned i = 0; i < total; ++i) who[i] = -1;
+      for (unsigned b = 0; b < total; ++b) {
+        const unsigned l = xcd_order(b, total, groups);
+        if (l >= total || who[l] >= 0) { ++bad; continue; }
+        who[l] = (int)(b & 7);
+      }
+      if (groups % 8 == 0)
+        for (unsigned i = 0; i < total; ++i) bad += who[i] != who[i / per * per] || who[i] != (int)(i / per % 8);
+    }
   bad += cached_len(-5, 100) != 0 || cached_len(101, 100) != 100 || cached_len(7, 100) != 7;
   bad += page_ok(-1, 4) || page_ok(4, 4) || !page_ok(0, 4) || !page_ok(3, 4) || page_ok(INT32_MIN, 4);
   printf("%lld pairs, %lld wrong\n", seen, bad);
