@@ -1,7 +1,9 @@
 /*
  * sage_mi355x.h -- C ABI of the MI355X (gfx950) microscaled-FP4 attention
- * forward of SageAttention3 (arXiv 2505.11594), and of the paper's 8-bit
- * attention (SageBwd: the forward of Algorithm 2, the backward of Algorithm 3).
+ * forward of SageAttention3 (arXiv 2505.11594), of the paper's 8-bit
+ * attention (SageBwd: the forward of Algorithm 2, the backward of Algorithm 3),
+ * and of 16-bit attention of language models with a sliding window, forward and
+ * backward, and over a paged cache.
  *
  * Every function returns an int status (sage_status).  Arguments are checked
  * on the host before any HIP call, so invalid calls fail without touching the
@@ -33,7 +35,8 @@ typedef enum {
 } sage_status;
 
 /* ---- shapes ------------------------------------------------------------ */
-/* Every entry point takes B, H, N, D with B, H, N >= 1 and D in {64, 128}. */
+/* Every entry point takes B, H, N, D with B, H, N >= 1 and D in {64, 128}  */
+/* (those of language models, below, say so where theirs differ).           */
 /* Np = N rounded up to 128.  Per head, Np * D <= 2^31 (N <= 2^24 at        */
 /* D = 128, 2^25 at D = 64); in total, B * H * Np * D <= 2^40.  Larger      */
 /* shapes return SAGE_ERR_INVALID_ARG.                                      */
@@ -352,8 +355,10 @@ int sage_attn_int8_bwd_ws(const void* q, const void* k, const void* v, const flo
 /* Everything is 16-bit in the type that flags give (SAGE_IN_FP16 or        */
 /* SAGE_IN_BF16, the only accepted bits), o and gradients too; scores,      */
 /* softmax and sums are fp32.  Probabilities are rounded to 16 bits for     */
-/* their product with V.  D is 64 or 128.  `stream` must belong to the      */
-/* current device.  Results are the same bits from call to call.            */
+/* their product with V (over the cache in two 16-bit parts).  D is 64 or   */
+/* 128.  `stream` must belong to the current device.  No output overlaps an */
+/* input or another output.  Results are the same bits from call to call.   */
+/* Nothing is allocated inside.                                             */
 /* ======================================================================== */
 
 /* Element strides of a [B, H, N, D] tensor; its channels are contiguous and
