@@ -433,7 +433,8 @@ typedef struct {
  *  k, v   : [S, Hkv, N, D] 16-bit, any strides, 16-byte aligned
  *  pos    : int32 [S], cached tokens before the call; counts: int32 [S] or NULL (N)
  *  weights: fp32 [S, Hkv, weights_stride] or NULL: set to 0 for the new tokens
- * Two tokens of one call stored in the same slot leave either.
+ * Two tokens of one call stored in the same slot leave either.  For an INT8 cache
+ * k and v must be finite.
  */
 int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
                    const sage_strides* v_strides, const int32_t* table, int max_pages, const int32_t* pos,

@@ -77,6 +77,9 @@ WINDOWS = [
     (2, 32, 16, 600, 64, "fp16", 200, 40, None),
     (1, 64, 4, 650, 64, "bf16", None, 0, None),
     (1, 64, 32, 550, 128, "fp16", None, 0, None),
+    # enough key blocks of like length that none is cut into chunks in the backward
+    (4, 32, 32, 512, 64, "bf16", 64, 0, None),
+    (4, 32, 32, 512, 128, "fp16", 64, 4, [512, 511, 300, 0]),
 ]
 
 
@@ -794,6 +797,38 @@ def test_prompt_tokens_and_eviction_together(int8):
             b, _ = _lm.cache_rows(c["k_cache"], c["k_scale"], table[s].cpu(), h, int(lens[s]))
             assert torch.equal(a, b[kept[s, h, :m].long()])
             assert torch.equal(nw[s, h, :m], w[s, h][kept[s, h, :m].long()])
+
+
+def test_calls_on_two_streams_at_once():
+    """Training and decoding of different inputs interleaved on two streams: each as alone."""
+    import torch
+    jobs = []
+    for i in range(2):
+        q, k, v = qkv(300 + i, 2, 8, 2, 400, 64, "bf16")
+        dout = randn(gen(310 + i), *q.shape).to(q.dtype)
+        g = gen(320 + i)
+        c, table, _ = make_cache(g, 3, 2, 16, 128, [900, 700, 800], "bf16", bool(i))
+        qd = randn(g, 3, 8, 128).to(torch.bfloat16)
+        ln = torch.tensor([900, 700 - 300 * i, 800], dtype=torch.int32, device="cuda")
+
+        def job(q=q, k=k, v=v, dout=dout, c=c, table=table, qd=qd, ln=ln):
+            o, lse = bd.sage_attn_window_fwd(q, k, v, window=90, sinks=4)
+            grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=90, sinks=4)
+            w = torch.zeros((3, 2, table.shape[1] * 16), device="cuda")
+            d = bd.sage_attn_paged_decode(qd, c["k_cache"], c["v_cache"], table, ln, k_scale=c["k_scale"], v_scale=c["v_scale"], weights=w)
+            return (o, lse, *grads, *d, w)
+
+        jobs.append((job, job(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, (job, _, s) in enumerate(jobs):
+            with torch.cuda.stream(s):
+                got[i].append(job())
+    torch.cuda.synchronize()
+    for i, (_, ref, _) in enumerate(jobs):
+        for r in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(r, ref)), i
 
 
 def test_captured_steps_follow_the_lengths_and_streams():
