@@ -109,8 +109,8 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
 // fills half the GPU, or the sequences are short.  A single workgroup takes 74 us for
 // 65536 tokens (its LDS atomics and scattered stores bound it), so a few long
 // sequences are cut into chunks: a launch per digit leaves each chunk's histogram in
-// the workspace, from which the next ones add up all chunks' to pick the digit, and
-// the last finds its place behind the chunks before it (4 launches).
+// the workspace, from which the next adds up all chunks' to pick the digit, and those in
+// front of its own to find its place behind them (4 launches, 36 us).
 // ---------------------------------------------------------------------------
 constexpr int EV = 1024;                                 // threads of the selection
 constexpr int ER = 8;                                    // neighbouring tokens per thread and round of the writing
@@ -291,32 +291,40 @@ __global__ __launch_bounds__(EV) void evict_chunk_kernel(const Evict a, int pass
   if (pass == 3 && evict_ends(a, e, s, h, c, a.chunks)) return;
   if (e.n <= a.budget) return;
   const int b0 = imin(e.n, c * a.chunk), b1 = imin(e.n, b0 + a.chunk);
-  int* const mine = a.hist + (((size_t)s * a.c.Hkv + h) * a.chunks) * 3 * BINS;   // [chunk][digit][bin]
+  const size_t head = (size_t)s * a.c.Hkv + h;
+  int* const mine = a.hist + head * a.chunks * 3 * BINS;   // [chunk][digit][bin]
+  int* const state = a.hist + (size_t)a.c.S * a.c.Hkv * a.chunks * 3 * BINS + (head * a.chunks + c) * 4;   // this chunk's, from pass to pass
   Last last = {0u, 0u, e.need};
   int out = 0, ties = 0;
-  if (e.need > 0) {
-    for (int p = 0; p < pass; ++p) {
-      // this digit over all chunks, and over those before this one (bins BINS - 1 - 2 tid and the next)
-      int t0 = 0, t1 = 0, f0 = 0, f1 = 0;
-      const int* x = mine + p * BINS + BINS - 2 - 2 * tid;
-#pragma unroll 4
-      for (int k = 0; k < a.chunks; ++k) {
-        const int y1 = x[(size_t)k * 3 * BINS], y0 = x[(size_t)k * 3 * BINS + 1];
-        t0 += y0; t1 += y1;
-        if (k < c) { f0 += y0; f1 += y1; }
-      }
-      const int d = BINS - 1 - 2 * tid;
-      pick_digit(l, t0, t1, p, last);
-      if (pass == 3) {
-        const int at = (int)(last.prefix >> digit_shift(p) & digit_mask(p));
-        int total;
-        block_scan((d > at ? f0 : 0) + (d - 1 > at ? f1 : 0), l.red, &total);
-        out += total;
-        if (p == 2) {
-          block_scan((d == at ? f0 : 0) + (d - 1 == at ? f1 : 0), l.red, &total);
-          ties = total;
-        }
-      }
+  if (e.need > 0 && pass > 0) {
+    const int p = pass - 1;
+    if (pass > 1) {
+      last.prefix = (uint32_t)state[0];
+      last.need = state[1];
+      out = state[2];
+      for (int i = 0; i < p; ++i) last.mask |= digit_mask(i) << digit_shift(i);
+    }
+    // the digit before over all chunks, and over those in front of this one (bins BINS - 1 - 2 tid and the next)
+    int t0 = 0, t1 = 0, f0 = 0, f1 = 0;
+    const int* x = mine + p * BINS + BINS - 2 - 2 * tid;
+#pragma unroll 8
+    for (int k = 0; k < a.chunks; ++k) {
+      const v2u y = *reinterpret_cast<const v2u*>(x + (size_t)k * 3 * BINS);
+      t0 += (int)y[1]; t1 += (int)y[0];
+      if (k < c) { f0 += (int)y[1]; f1 += (int)y[0]; }
+    }
+    const int d = BINS - 1 - 2 * tid;
+    pick_digit(l, t0, t1, p, last);
+    const int at = (int)(last.prefix >> digit_shift(p) & digit_mask(p));
+    int total;
+    block_scan((d > at ? f0 : 0) + (d - 1 > at ? f1 : 0), l.red, &total);
+    out += total;
+    if (pass == 3) {
+      block_scan((d == at ? f0 : 0) + (d - 1 == at ? f1 : 0), l.red, &ties);
+    } else if (tid == 0) {                               // (all have read it: the scans' barriers)
+      state[0] = (int)last.prefix;
+      state[1] = last.need;
+      state[2] = out;
     }
   }
   if (pass == 3) {
@@ -361,7 +369,7 @@ int evict_chunks(int S, int Hkv, int capacity) {
 }
 size_t evict_hist_ints(int S, int Hkv, int capacity) {
   const int c = evict_chunks(S, Hkv, capacity);
-  return c > 1 ? (size_t)S * Hkv * c * 3 * BINS : 0;
+  return c > 1 ? (size_t)S * Hkv * c * (3 * BINS + 4) : 0;
 }
 
 hipError_t launch_kv_evict(const Evict& x, int D, hipStream_t st) {
