@@ -375,7 +375,8 @@ typedef struct {
  *  lse    : fp32 [B, Hq, N] or NULL: the natural-log log-sum-exp
  *  lens   : int32 [B] or NULL: tokens of each sequence of a padded batch (on the
  *           device; clamped to [0, N]).  Rows behind it are o = 0, L = -infinity
- * Shape limits as above, with Hq heads (at most 65535).  No workspace.
+ * Shape limits as above, with Hq heads (at most 65535), and fewer than 2^24 blocks
+ * of 128 queries in all (B * Hq * Np / 128).  No workspace.
  */
 int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* lens,
                          int B, int Hq, int Hkv, int N, int D, int window, int sinks, unsigned flags,

@@ -520,7 +520,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   }
   if (e == hipSuccess && a.weights) {
     const int capacity = a.c.max_pages * a.c.page_size;
-    const int want = imax(1, 2048 / imax(1, imin(2048, a.c.S * a.c.Hkv)));
+    const int want = imax(1, (int)(2048 / ((long long)a.c.S * a.c.Hkv)));
     hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)imin(cdiv(capacity, 1024), want), (unsigned)a.c.Hkv, (unsigned)a.c.S),
                        dim3(256), 0, st, a);
     e = hipGetLastError();

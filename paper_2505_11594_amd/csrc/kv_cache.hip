@@ -389,7 +389,7 @@ hipError_t launch_kv_evict(const Evict& x, int D, hipStream_t st) {
   }
   if (e != hipSuccess) return e;
   const int elem = a.c.k_scale ? 1 : 2, rb = D * elem, per = 256 / (rb / 16);
-  const dim3 grid((unsigned)imin(cdiv(a.budget, per), imax(1, 8192 / imax(1, imin(8192, a.c.S * a.c.Hkv)))),
+  const dim3 grid((unsigned)imin(cdiv(a.budget, per), imax(1, (int)(8192 / ((long long)a.c.S * a.c.Hkv)))),
                   (unsigned)a.c.Hkv, (unsigned)a.c.S);
   if (rb == 256) hipLaunchKernelGGL((evict_move_kernel<256>), grid, dim3(256), 0, st, a, elem);
   else if (rb == 128) hipLaunchKernelGGL((evict_move_kernel<128>), grid, dim3(256), 0, st, a, elem);

@@ -40,7 +40,7 @@ inline bool distinct_rows(const Strides& s, long long nb, long long nh, long lon
   long long extent = D;
   for (const Dim& x : d) {
     if (x.size <= 1) continue;
-    if (x.stride < extent) return false;
+    if (x.stride < extent || x.stride > (1LL << 62) / x.size) return false;
     extent += x.stride * (x.size - 1);
   }
   return true;
@@ -59,12 +59,15 @@ int check_window(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
   const long long Np = ((long long)N + 127) / 128 * 128;
   if (Np * D > (1LL << 31) || (long long)B * Hq > (1LL << 30) || (long long)B * Hq * Np * D > kMaxElems)
     return SAGE_ERR_INVALID_ARG;
+  if ((long long)B * Hq * (Np / 128) >= (1LL << 24)) return SAGE_ERR_INVALID_ARG;   // a workgroup of 256 each: 2^32 threads a launch
   return SAGE_OK;
 }
-// A window over everything makes the sinks ordinary keys.
+// Where even the last query's window begins among the sinks (or is everything), every
+// key is seen as without a window.
 inline void clamp_window(int n, int* window, int* sinks) {
-  *window = std::min(*window, n);
-  *sinks = *window >= n ? 0 : std::min(*sinks, n);
+  if ((long long)*window + *sinks < n) return;
+  *window = n;
+  *sinks = 0;
 }
 
 // `written`: rows are stored, so they may not overlap.

@@ -169,3 +169,22 @@ def test_binding_refuses_host_tensors_and_wrong_types():
         bd.sage_kv_append(q, q, q, q, t, t[0])
     with pytest.raises(ValueError):
         bd.sage_kv_evict(q, q, t, t[0], q, t, 4)
+
+
+def test_more_blocks_than_a_launch_takes(L):
+    big = dict(B=1 << 12, Hq=1 << 12, Hkv=1 << 12, N=1, D=64)            # 2^24 workgroups of 256
+    assert fwd(L, **big) == INVALID
+    assert bd.attn_window_bwd_workspace_size(*big.values()) == 0
+
+
+@pytest.mark.parametrize("window,sinks", [(900, 100), (1, 999), (1, 5000), (999, 1), (1000, 1000)])
+def test_window_that_reaches_the_sinks_is_no_window(L, window, sinks):
+    # query 999 sees all of the keys 0 .. sinks - 1 and 1000 - window .. 999
+    full = bd.attn_window_bwd_workspace_size(1, 4, 4, 1000, 128)
+    assert bd.attn_window_bwd_workspace_size(1, 4, 4, 1000, 128, window, sinks) == full
+
+
+def test_strides_whose_extent_overflows_are_refused(L):
+    c = cache(ks=(1 << 40, 2048, 128), pages=(1 << 31) - 1)
+    for f in (append, evict):
+        assert f(L, c) == INVALID, f.__name__
