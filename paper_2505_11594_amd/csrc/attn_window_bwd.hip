@@ -16,8 +16,8 @@
 // products of 32 x 32 x 16) bound both kernels.
 //
 // Sink keys are seen by every later query, 32768 / 1152 times as many as others of a
-// long sequence: dkv_kernel leaves them out, sink_kernel takes them in chunks of
-// queries and join_sinks_kernel adds the chunks.
+// long sequence: dkv_kernel leaves them out, a launch of its SINK form takes them in
+// chunks of queries and join_sinks_kernel adds the chunks.
 //
 // P and dS are rounded to the input's type for the second products.  In fp16 both
 // carry a power of two that keeps them normal numbers: P 2^15, and dS the largest
@@ -39,8 +39,8 @@ __device__ __forceinline__ int seq_len(const WindowBwd& a, int b) { return a.len
 __device__ __forceinline__ int row_pad(int N) { return (N + BT - 1) / BT * BT; }
 
 // lb = -L log2(e) (and P's power of two; -inf behind the sequence's end: P = 0 there)
-// and -delta per query row, as the kernels add them; in fp16 also the largest |dO_i| (and, from blockIdx.y >= B Hq on, |V_j|) of
-// every PR rows.
+// and -delta per query row, as the kernels add them; in fp16 also the largest |dO_i|
+// (and, from blockIdx.y >= B Hq on, |V_j|) of every PR rows.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void rows_kernel(const WindowBwd a) {
   constexpr int LPR = D / 8, RPP = 256 / LPR, PASSES = PR / RPP;   // lanes per row, rows per pass
@@ -125,8 +125,7 @@ __device__ __forceinline__ float ds_scale(const WindowBwd& a, int b, int hk) {
 }
 
 // S and dP - delta: the 32 rows at `at` and TB bytes behind times the 32 columns of b and
-// c, the second on top of g (-delta), the
-// two products in turn (each alone would wait for its own last result, and its rows,
+// c, the second on top of g (-delta), the two products in turn (each alone would wait for its own last result, and its rows,
 // all read ahead, would not leave enough registers for two waves per SIMD).
 template <int D, bool BF16, int TB, int AHEAD = 3>
 __device__ __forceinline__ void rows_times(uint32_t at, const v4i* b, const v4i* c, v16f& s, v16f& g) {
