@@ -351,7 +351,9 @@ int sage_attn_int8_bwd_ws(const void* q, const void* k, const void* v, const flo
 /* query head h reads key head h * Hkv / Hq.  Softmax scale 1/sqrt(D).  A   */
 /* row that sees no key has o = 0 and L = -infinity.  What lies in keys and */
 /* values that a row does not see -- behind a sequence's end, in unused     */
-/* cache slots -- does not change it, infinities and NaN included.          */
+/* cache slots -- does not change it, infinities and NaN included; an       */
+/* infinity or NaN in a value that it sees makes that channel of its o      */
+/* infinite or NaN, and no other.                                           */
 /* Everything is 16-bit in the type that flags give (SAGE_IN_FP16 or        */
 /* SAGE_IN_BF16, the only accepted bits), o and gradients too; scores,      */
 /* softmax and sums are fp32.  Probabilities are rounded to 16 bits for     */

@@ -19,6 +19,14 @@
 // device knows.  A part that is a whole sequence is final; others leave their
 // (maximum, sum, O) for join_kernel.  A share has at most two of them: one that
 // began before it (slot 0) and one that goes on behind it (slot 1).
+//
+// Infinities and NaN in values that the token sees: P enters its product in two parts, of
+// which the second may be 0 or negative, and an infinity times it would be NaN.  But a
+// channel's sums hold that channel's values only, and all heads see the same keys.  So a
+// wave that would store anything but finite numbers looks through the part's rows of V once
+// more for such values, and gives their channels what a sum with them is: an infinity, or
+// NaN.  (A look at the sums per sequence for everyone else.  The same look before the waves'
+// join took 14 registers of the tile loop.)
 #include "lm_args.h"
 #include "mma16.h"
 #include "window.h"
@@ -148,12 +156,24 @@ __device__ __forceinline__ void v_read4(uint32_t b0, uint32_t b1, uint32_t b2, u
   r[3] = __builtin_bit_cast(v4i, __builtin_shufflevector(x6, x7, 0, 1, 2, 3));
 }
 
+// Of 8 values, bit e of pos: value e is +infinity or NaN, of neg: -infinity or NaN.
+template <bool BF16>
+__device__ __forceinline__ void find_nonfinite(const v4i x, unsigned& pos, unsigned& neg) {
+  constexpr uint32_t INF = BF16 ? 0x7F80u : 0x7C00u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t h = (uint32_t)x[e / 2] >> (16 * (e & 1)) & 0xFFFFu, size = h & 0x7FFFu;
+    if (size > INF || h == INF) pos |= 1u << e;
+    if (size > INF || h == (INF | 0x8000u)) neg |= 1u << e;
+  }
+}
+
 // BF16: the type of q and o.  I8: 8-bit cache; its codes are exact in either type,
 // and P times V's scale, whose size nothing bounds, is taken in bf16.  P enters its
 // product with V in two parts, rounded and rest (together 2^-16 of it in bf16, 2^-22 in
 // fp16): the matrix instructions have the time.
 template <int D, bool BF16, bool I8>
-__global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a) {
+__global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(const Decode a) {
   constexpr bool PB = BF16 || I8;                        // type of P and V in the second product
   constexpr int EB = I8 ? 1 : 2, ROW = D * 2;
   constexpr int KL = D * EB / 64;                        // 16-byte K loads per lane and 16-key subtile
@@ -379,19 +399,56 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_kernel(const Decode a
     // thread: head tid / 16, 4 channels at a time
     const int qh = tid >> 4;
     const float lq = __shfl(ll, qh, 64);                 // lane qh (< 16) holds head qh's sum
+    v4f x[D / 64];
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+      x[c] = v4f{};
+#pragma unroll
+      for (int w = 0; w < DW; ++w) x[c] += *reinterpret_cast<const v4f*>(lds + w * REG + (qh * PADQ + 64 * c + 4 * (tid & 15)) * 4);
+    }
+    if constexpr (!I8) {
+      bool odd = false;
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= !(__builtin_fabsf(x[c][e]) < INFINITY);
+      if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+        unsigned pos = 0, neg = 0;                       // of channels 8 (lane % RC) + e
+#pragma unroll 1
+        for (int t = DW * off; t < tend; ++t) {
+          const int id = page_of(t), at = (tl.tile(t) * DT + (lane & 31)) % ps;
+#pragma unroll 1
+          for (int j = 0; j < VL; ++j) {
+            const int row = VR * j + lane / RC, p = __shfl(id, row, 64), sl = __shfl(at, row, 64);
+            const uint8_t* v = (const uint8_t*)a.c.v + EB * (max(p, 0) * a.c.vs.b + hk * a.c.vs.h + sl * a.c.vs.n) + 16 * (lane % RC);
+            if (p >= 0) find_nonfinite<BF16>(*reinterpret_cast<const v4i*>(v), pos, neg);
+          }
+        }
+#pragma unroll
+        for (int o = RC; o < 64; o <<= 1) {              // over the rows
+          pos |= __shfl_xor(pos, o, 64);
+          neg |= __shfl_xor(neg, o, 64);
+        }
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {               // channel 64 c + 4 (tid % 16) + e
+          const int from = 8 * c + (lane & 15) / 2, bit = 4 * (lane & 1);
+          const unsigned p = __shfl(pos, from, 64) >> bit, n = __shfl(neg, from, 64) >> bit;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if ((p | n) >> e & 1u) x[c][e] = (p >> e & 1u ? INFINITY : 0.0f) - (n >> e & 1u ? INFINITY : 0.0f);
+        }
+      }
+    }
     if (qh < gn) {
       const float inv = lq > 0.0f || lq != lq ? 1.0f / lq : 0.0f;
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         const int d = 64 * c + 4 * (tid & 15);
-        v4f x = v4f{};
-#pragma unroll
-        for (int w = 0; w < DW; ++w) x += *reinterpret_cast<const v4f*>(lds + w * REG + (qh * PADQ + d) * 4);
         if (whole) {
-          const v2u o = {pack16<BF16>(x[0] * inv, x[1] * inv), pack16<BF16>(x[2] * inv, x[3] * inv)};
+          const v2u o = {pack16<BF16>(x[c][0] * inv, x[c][1] * inv), pack16<BF16>(x[c][2] * inv, x[c][3] * inv)};
           *reinterpret_cast<v2u*>((uint16_t*)a.o + ((size_t)s * a.Hq + h0 + qh) * D + d) = o;
         } else {
-          *reinterpret_cast<v4f*>(a.part + (slot * a.Hq + h0 + qh) * D + d) = x;
+          *reinterpret_cast<v4f*>(a.part + (slot * a.Hq + h0 + qh) * D + d) = x[c];
         }
       }
     }
@@ -430,7 +487,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) 
     l += ml[at(w) * 2 + 1] * f;
     const float* p = a.part + at(w) * D + lane * CL;
 #pragma unroll
-    for (int i = 0; i < CL; ++i) x[i] += p[i] * f;
+    for (int i = 0; i < CL; ++i) x[i] += __builtin_fabsf(p[i]) < INFINITY ? p[i] * f : p[i];   // (an infinity stays one where f is 0)
   }
 #pragma unroll
   for (int i = 0; i < CL; ++i) sums[wave][lane * CL + i] = x[i];

@@ -1,0 +1,75 @@
+"""GPU checks of the language-model operators where their inputs or sizes are at an edge:
+infinities and NaN that a row does see, and calls far larger than those of test_gpu_lm.py."""
+import pytest
+
+from paper_2505_11594_amd import binding as bd
+
+from _gpu import say
+from test_gpu_lm import DT, gen, make_cache, randn
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = float("inf"), float("nan")
+
+
+# ---------------------------------------------------------------- values that are seen and not finite
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("D,page,lens", [(64, 16, [40, 7]), (128, 24, [300, 129]), (128, 64, [3000, 700]), (64, 16, [9000, 1])])
+def test_paged_decode_infinities_and_nan_that_are_seen(D, page, lens, dtype):
+    """A value that is no finite number, seen by every head of its key head: its channel is that
+    infinity, or NaN where there are both or a NaN; every other output keeps the bits that it has
+    with 0 in the value's place."""
+    import torch
+    g = gen(7 * D + lens[0])
+    Hq, Hkv, ch = 8, 2, D // 2 + 3
+    c, table, _ = make_cache(g, len(lens), Hkv, page, D, lens, dtype, False)
+    q = randn(g, len(lens), Hq, D).to(getattr(torch, DT[dtype]))
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    v = c["v_cache"]
+    run = lambda: bd.sage_attn_paged_decode(q, c["k_cache"], v, table, ln)
+    n = lens[0]
+    for puts, want in (([(0, INF)], INF), ([(n - 1, -INF)], -INF), ([(n // 2, NAN)], NAN), ([(3, INF), (n // 2, -INF)], NAN),
+                       ([(n // 3, INF), (n // 2, INF)], INF), ([(n // 3, -INF), (n - 1, NAN)], NAN)):
+        where = [(int(table[0, j // page]), 1, j % page, ch) for j, _ in puts]
+        old = [v[w].clone() for w in where]
+        for w in where:
+            v[w] = 0
+        o0, l0 = run()
+        for w, (_, x) in zip(where, puts):
+            v[w] = x
+        o, l = run()
+        torch.cuda.synchronize()
+        say("seen %s: %s" % (puts, o[0, :, ch].tolist()))
+        got = o[0, Hq // 2:, ch].float()
+        assert torch.equal(got.nan_to_num(7, 8, 9), torch.full_like(got, want).nan_to_num(7, 8, 9))
+        o[0, Hq // 2:, ch] = o0[0, Hq // 2:, ch]
+        assert torch.equal(o, o0) and torch.equal(l, l0)
+        for w, x in zip(where, old):
+            v[w] = x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("n", [200, 3000])
+def test_paged_decode_infinity_of_a_token_with_hardly_any_weight(n, dtype):
+    """The first half of the sequence has scores 512 below the other's: weights that are 0 in fp32, and
+    whole parts of the split whose factor is.  An infinity there is seen all the same."""
+    import torch
+    g = gen(n)
+    D, page = 64, 16
+    c, table, _ = make_cache(g, 1, 1, page, D, [n], dtype, False)
+    k, v = c["k_cache"], c["v_cache"]
+    ids = table[0].long()
+    half = -(-n // (2 * page))
+    k[ids[:half]], k[ids[half:]] = -8.0, 0.0             # scores -64 * 8 * 8 / 8 and 0
+    q = torch.full((1, 4, D), 8.0, dtype=k.dtype, device="cuda")
+    ln = torch.tensor([n], dtype=torch.int32, device="cuda")
+    o0, l0 = bd.sage_attn_paged_decode(q, k, v, table, ln)
+    for at, bad in ((5, INF), (page * (half - 1) + 1, -INF), (40, NAN)):
+        v2 = v.clone()
+        v2[int(ids[at // page]), 0, at % page, 9] = bad
+        o, l = bd.sage_attn_paged_decode(q, k, v2, table, ln)
+        torch.cuda.synchronize()
+        got = o[0, :, 9].float()
+        assert torch.equal(got.nan_to_num(7, 8, 9), torch.full_like(got, bad).nan_to_num(7, 8, 9)), (at, bad, got.tolist())
+        o[0, :, 9] = o0[0, :, 9]
+        assert torch.equal(o, o0) and torch.equal(l, l0)
