@@ -101,27 +101,46 @@ __global__ __launch_bounds__(256) void rows_kernel(const WindowBwd a) {
 }
 static_assert(PR == BT, "the row pass fills whole tiles of rows");
 
-// The power of two that dS of a (sequence, key head) carries in fp16.  Every lane
-// gets it.
-template <bool BF16>
-__device__ __forceinline__ float ds_scale(const WindowBwd& a, int b, int hk) {
-  if constexpr (BF16) return 1.0f;
-  const int lane = threadIdx.x & 63, nb = cdiv(a.N, PR), G = a.Hq / a.Hkv;
+// The power of two that dS of each (sequence, key head) carries in fp16, from the norms of
+// its row blocks: one workgroup each.  If every wave of the kernels behind looked through
+// the norms itself, G N / 64 of them, a window's constant work per workgroup would grow with N
+// (fp16 step of 16 / 1 heads, D = 64, window 64: 32768 tokens 488 -> 258 us with this
+// launch, 2048 tokens 59 -> 57.5, 2 x 12 / 4 heads of 1000 tokens 78 either way).
+constexpr int SW = 16;                  // waves
+__global__ __launch_bounds__(64 * SW) void scale_kernel(const WindowBwd a) {
+  __shared__ float red[2][SW];
+  const int b = blockIdx.x / a.Hkv, hk = blockIdx.x - b * a.Hkv, tid = threadIdx.x, nb = cdiv(a.N, PR), G = a.Hq / a.Hkv;
   const float* g = a.norms + ((size_t)b * a.Hq + hk * G) * nb;
   const float* v = a.norms + ((size_t)a.B * a.Hq + b * a.Hkv + hk) * nb;
   float gm = 0.0f, vm = 0.0f;
-  for (int i = lane; i < G * nb; i += 64) gm = __builtin_fmaxf(gm, g[i]);
-  for (int i = lane; i < nb; i += 64) vm = __builtin_fmaxf(vm, v[i]);
+#pragma unroll 4
+  for (int i = tid; i < G * nb; i += 64 * SW) gm = __builtin_fmaxf(gm, g[i]);
+#pragma unroll 4
+  for (int i = tid; i < nb; i += 64 * SW) vm = __builtin_fmaxf(vm, v[i]);
 #pragma unroll
   for (int s = 32; s >= 1; s >>= 1) {
     gm = __builtin_fmaxf(gm, __shfl_xor(gm, s, 64));
     vm = __builtin_fmaxf(vm, __shfl_xor(vm, s, 64));
   }
+  if ((tid & 63) == 0) {
+    red[0][tid >> 6] = gm;
+    red[1][tid >> 6] = vm;
+  }
+  __syncthreads();
+  if (tid > 0) return;
+#pragma unroll
+  for (int w = 1; w < SW; ++w) {
+    gm = __builtin_fmaxf(gm, red[0][w]);
+    vm = __builtin_fmaxf(vm, red[1][w]);
+  }
   const float bound = 2.0f * gm * vm;
-  if (!(bound > 0.0f) || bound == INFINITY) return 1.0f;
-  int e;
-  __builtin_frexpf(bound, &e);                           // bound < 2^e
-  return __builtin_ldexpf(1.0f, imax(-100, imin(100, 15 - e)));
+  int e = 15;
+  if (bound > 0.0f && bound < INFINITY) __builtin_frexpf(bound, &e);   // bound < 2^e
+  a.scales[blockIdx.x] = __builtin_ldexpf(1.0f, imax(-100, imin(100, 15 - e)));
+}
+template <bool BF16>
+__device__ __forceinline__ float ds_scale(const WindowBwd& a, int b, int hk) {
+  return BF16 ? 1.0f : a.scales[(size_t)b * a.Hkv + hk];
 }
 
 // S and dP - delta: the 32 rows at `at` and TB bytes behind times the 32 columns of b and
@@ -654,6 +673,10 @@ static hipError_t launch_window_bwd_t(const WindowBwd& a, hipStream_t st) {
                      st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  if (!BF16) {
+    hipLaunchKernelGGL(scale_kernel, dim3((unsigned)(a.B * a.Hkv)), dim3(64 * SW), 0, st, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   // dQ first, as it may put delta right.  As in the forward: two groups of waves where
   // there is a workgroup per CU or less.
   const unsigned blocks = (unsigned)(a.B * a.Hq) * cdiv(a.N, 128);

@@ -29,7 +29,7 @@ struct WindowBwd {
   int chunks, mchunks, mshare;           // of the sinks' query tiles, of the other keys', and tiles in one of these
   Strides qs, ks, vs, os, gs;            // gs: dout
   float c2, rsd;           // rsd = 1 / sqrt(D)
-  float *lb, *delta, *norms, *part, *mpart;   // workspace
+  float *lb, *delta, *norms, *scales, *part, *mpart;   // workspace
 };
 int window_bwd_chunks(int B, int Hq, int Hkv, int N, int sinks);
 int window_bwd_share(int B, int Hq, int Hkv, int N, int window, int* chunks);

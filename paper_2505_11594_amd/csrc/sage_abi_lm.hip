@@ -96,7 +96,7 @@ sage::Cache cache_of(const sage_kv_cache* c, const int32_t* table, int max_pages
 }
 
 struct BwdWs {
-  size_t lb, delta, norms, part, mpart, total;
+  size_t lb, delta, norms, scales, part, mpart, total;
   int chunks, mchunks, mshare;
 };
 BwdWs bwd_ws(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
@@ -108,6 +108,7 @@ BwdWs bwd_ws(int B, int Hq, int Hkv, int N, int D, int window, int sinks) {
   w.lb = off; off += rows;
   w.delta = off; off += rows;
   w.norms = off; off += up256(sage::window_bwd_norm_floats(B, Hq, Hkv, N) * sizeof(float));
+  w.scales = off; off += up256((size_t)B * Hkv * sizeof(float));
   w.part = off; off += up256(sage::window_bwd_part_floats(B, Hq, Hkv, N, D, sinks) * sizeof(float));
   w.mpart = off; off += up256(sage::window_bwd_mpart_floats(B, Hkv, N, D, w.mchunks) * sizeof(float));
   w.total = off;
@@ -192,6 +193,7 @@ int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void
   a.lb = reinterpret_cast<float*>(base + w.lb);
   a.delta = reinterpret_cast<float*>(base + w.delta);
   a.norms = reinterpret_cast<float*>(base + w.norms);
+  a.scales = reinterpret_cast<float*>(base + w.scales);
   a.part = reinterpret_cast<float*>(base + w.part);
   a.mpart = reinterpret_cast<float*>(base + w.mpart);
   a.chunks = w.chunks; a.mchunks = w.mchunks; a.mshare = w.mshare;

@@ -1,11 +1,13 @@
 """GPU checks of the language-model operators where their inputs or sizes are at an edge:
 infinities and NaN that a row does see, and calls far larger than those of test_gpu_lm.py."""
+import math
+
 import pytest
 
 from paper_2505_11594_amd import binding as bd
 
 from _gpu import say
-from test_gpu_lm import DT, gen, make_cache, randn
+from test_gpu_lm import DT, check_grads, gen, make_cache, qkv, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -73,3 +75,44 @@ def test_paged_decode_infinity_of_a_token_with_hardly_any_weight(n, dtype):
         assert torch.equal(got.nan_to_num(7, 8, 9), torch.full_like(got, bad).nan_to_num(7, 8, 9)), (at, bad, got.tolist())
         o[0, :, 9] = o0[0, :, 9]
         assert torch.equal(o, o0) and torch.equal(l, l0)
+
+
+# ---------------------------------------------------------------- the power of two of fp16's dS
+@pytest.mark.parametrize("at", [(0, 0), (7, 640), (15, 1099)])
+@pytest.mark.parametrize("what", ["dout", "v"])
+def test_window_backward_fp16_scale_knows_every_row(what, at):
+    """One row of dO or V is 2^9 times the others, in any block of any head of the group: dS of that
+    size would pass fp16's range if the bound had missed it."""
+    import torch
+    q, k, v = qkv(5, 1, 16, 1, 1100, 64, "fp16")
+    dout = randn(gen(6), 1, 16, 1100, 64).half()
+    (dout if what == "dout" else v)[0, at[0] if what == "dout" else 0, at[1]] *= 512
+    o, lse = bd.sage_attn_window_fwd(q, k, v, window=200, sinks=3)
+    grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=200, sinks=3)
+    torch.cuda.synchronize()
+    check_grads(q, k, v, dout, grads, 200, 3, None, "%s large at %s" % (what, at))
+
+
+def test_window_backward_fp16_takes_no_longer_than_bf16_as_lengths_grow():
+    """16 query heads of one key head under a short window: the work per workgroup is the same at any
+    length.  (fp16 took 2.2 times bf16's time here when every wave looked for the scale itself.)"""
+    import torch
+    N = 32768
+    times = []
+    for dt in (torch.float16, torch.bfloat16):
+        q, k, v, dout = (torch.randn((1, h, N, 64), device="cuda").to(dt) for h in (16, 1, 1, 16))
+        o, lse = bd.sage_attn_window_fwd(q, k, v, window=64)
+        ws = torch.empty(bd.attn_window_bwd_workspace_size(1, 16, 1, N, 64, 64), dtype=torch.uint8, device="cuda")
+        out = [torch.empty_like(x) for x in (q, k, v)]
+        best = math.inf
+        for _ in range(6):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(5):
+                bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=64, workspace=ws, out=out)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b) / 5 * 1e3)
+        times.append(best)
+    say("backward of 32768 tokens, window 64: fp16 %.0f us, bf16 %.0f us" % tuple(times))
+    assert times[0] < 1.5 * times[1]
