@@ -6,8 +6,10 @@ import pytest
 
 from paper_2505_11594_amd import binding as bd
 
+import _lm
+import _slopes
 from _gpu import say
-from test_gpu_lm import DT, check_grads, gen, make_cache, qkv, randn
+from test_gpu_lm import DT, WINDOWS, check_grads, gen, make_cache, qkv, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +118,25 @@ def test_window_backward_fp16_takes_no_longer_than_bf16_as_lengths_grow():
         times.append(best)
     say("backward of 32768 tokens, window 64: fp16 %.0f us, bf16 %.0f us" % tuple(times))
     assert times[0] < 1.5 * times[1]
+
+
+# ---------------------------------------------------------------- gradients against slopes
+@pytest.mark.parametrize("case", [c for c in WINDOWS if c[3] > 1])
+def test_window_gradients_are_slopes_of_the_definition(case):
+    """Each gradient against the slope of the definition along it (_slopes.py).  A gradient of zero is
+    off by the slope itself, so it would not pass where the tolerance is less than that."""
+    import torch
+    B, Hq, Hkv, N, D, dtype, window, sinks, lens = case
+    q, k, v = qkv(13 + N + D, B, Hq, Hkv, N, D, dtype)
+    dout = randn(gen(N + 1), B, Hq, N, D).to(q.dtype)
+    ln = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse = bd.sage_attn_window_fwd(q, k, v, window=window, sinks=sinks, lens=ln)
+    grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=window, sinks=sinks, lens=ln)
+    torch.cuda.synchronize()
+    want, bound = check_grads(q, k, v, dout, grads, window, sinks, lens, "slopes %s" % (case,))
+    u = _lm.unit(q.dtype)
+    bound = [t + u * (w.abs() + t) + torch.finfo(q.dtype).smallest_normal * 2.0 ** -10 for w, t in zip(want, bound)]
+    ratios, sizes = _slopes.slopes_agree([x.double() for x in (q, k, v)], dout.double(), grads, want, bound, window, sinks, lens)
+    say("slopes: %s of the tolerances, which are %s of the slopes" % (ratios, sizes))
+    first = 2 if window == 1 and sinks == 0 else 0       # (a query that sees one key: dQ and dK are 0)
+    assert max(ratios) <= 1 and max(sizes[first:]) < 1
