@@ -140,3 +140,66 @@ def test_window_gradients_are_slopes_of_the_definition(case):
     say("slopes: %s of the tolerances, which are %s of the slopes" % (ratios, sizes))
     first = 2 if window == 1 and sinks == 0 else 0       # (a query that sees one key: dQ and dK are 0)
     assert max(ratios) <= 1 and max(sizes[first:]) < 1
+
+
+# ---------------------------------------------------------------- large calls
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_window_tensors_of_more_than_2_31_elements(dtype):
+    """262181 tokens of 72 heads: the last group's last rows and keys against the definition over the
+    sinks and the last tokens, of which the first see less than they should and are left out."""
+    import torch
+    Hq, Hkv, N, D, window, sinks = 72, 8, 2 ** 18 + 37, 128, 100, 4
+    G, dt = Hq // Hkv, getattr(torch, DT[dtype])
+    assert Hq * N * D > 2 ** 31
+    g = gen(91)
+    rnd = lambda h: torch.randn((1, h, N, D), generator=g, device="cuda", dtype=dt)
+    q, k, v, dout = rnd(Hq), rnd(Hkv), rnd(Hkv), rnd(Hq)
+    say("window %d tokens %s" % (N, dtype))
+    o, lse = bd.sage_attn_window_fwd(q, k, v, window=window, sinks=sinks)
+    grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    first = N - sinks - (N - sinks) % 128 - 512          # tiles lie in the short sequence as in the long one
+    at = torch.cat([torch.arange(sinks), torch.arange(first + sinks, N)]).cuda()
+    n, whole, u = len(at), slice(sinks + window, None), _lm.unit(dt)
+    short = lambda x, h: x[0, h, at].double()
+    kk, vv = short(k, -1), short(v, -1)
+    sums = {x: torch.zeros_like(kk) for x in ("dk", "dv", "edk", "edv")}
+    worst = [0.0] * 5
+    over = lambda got, w, t: float(((got.double() - w).abs() / t)[whole].max())
+    for h in range(Hq - G, Hq):
+        r = _lm.window_attention(short(q, h), kk, vv, window, sinks, n, short(dout, h), u)
+        worst[0] = max(worst[0], over(o[0, h, at], r["o"], _lm.o_bound(r, n, u)))
+        worst[1] = max(worst[1], over(lse[0, h, at], r["lse"], _lm.lse_bound(r, n)))
+        t = r["edq"] + u * (r["dq"].abs() + r["edq"]) + 1e-9
+        worst[2] = max(worst[2], over(grads[0][0, h, at], r["dq"], t))
+        for x in sums:
+            sums[x] += r[x]
+    for i, x in ((3, "dk"), (4, "dv")):
+        t = sums["e" + x] + u * (sums[x].abs() + sums["e" + x]) + 1e-9
+        worst[i] = over(grads[i - 2][0, -1, at], sums[x], t)
+    say("O, L, dQ, dK, dV at %s of their bounds" % worst)
+    assert max(worst) <= 1
+
+
+def test_window_strides_of_more_than_2_31_elements():
+    """Rows 2^22 elements apart, the largest token stride that is taken: the bits of contiguous copies."""
+    import torch
+    B, Hq, Hkv, N, D = 2, 4, 2, 700, 128
+    q, k, v = qkv(92, B, Hq, Hkv, N, D, "bf16")
+    dout = randn(gen(93), B, Hq, N, D).to(q.dtype)
+    o, lse = bd.sage_attn_window_fwd(q, k, v, window=90, sinks=40)
+    grads = bd.sage_attn_window_bwd(q, k, v, o, lse, dout, window=90, sinks=40)
+    big = torch.empty((N, B, 2 ** 21 // 1024, 1024), dtype=q.dtype, device="cuda")
+    assert big.numel() > 2 ** 31
+    far = []
+    for i, x in enumerate((q, k, v, o, dout)):
+        y = big[:, :, -1 - i, :x.shape[1] * D].unflatten(-1, (x.shape[1], D)).permute(1, 2, 0, 3)
+        assert y.shape == x.shape and y.stride(2) == 2 ** 22
+        if x is not o:
+            y.copy_(x)
+        far.append(y)
+    say("window, rows 2^22 elements apart")
+    o2, lse2 = bd.sage_attn_window_fwd(*far[:3], window=90, sinks=40, out=far[3])
+    got = bd.sage_attn_window_bwd(*far[:4], lse2, far[4], window=90, sinks=40)
+    torch.cuda.synchronize()
+    assert torch.equal(o2, o) and torch.equal(lse2, lse) and all(torch.equal(a, b) for a, b in zip(got, grads))
