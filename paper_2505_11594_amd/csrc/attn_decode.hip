@@ -137,25 +137,6 @@ __device__ __forceinline__ void widen16(const v4i c, v4i& lo, v4i& hi) {
   hi = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
 }
 
-// The A operands of 4 channel blocks for 32 keys: two transposing reads each, 16 keys apart.
-template <int D>
-__device__ __forceinline__ void v_read4(uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3, v4i* r) {
-  v2u x0, x1, x2, x3, x4, x5, x6, x7;
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3), "=&v"(x4), "=&v"(x5), "=&v"(x6), "=&v"(x7)
-      : "v"(b0), "v"(b1), "v"(b2), "v"(b3), "n"(16 * D * 2)
-      : "memory");
-  r[0] = __builtin_bit_cast(v4i, __builtin_shufflevector(x0, x1, 0, 1, 2, 3));
-  r[1] = __builtin_bit_cast(v4i, __builtin_shufflevector(x2, x3, 0, 1, 2, 3));
-  r[2] = __builtin_bit_cast(v4i, __builtin_shufflevector(x4, x5, 0, 1, 2, 3));
-  r[3] = __builtin_bit_cast(v4i, __builtin_shufflevector(x6, x7, 0, 1, 2, 3));
-}
-
 // Of 8 values, bit e of pos: value e is +infinity or NaN, of neg: -infinity or NaN.
 template <bool BF16>
 __device__ __forceinline__ void find_nonfinite(const v4i x, unsigned& pos, unsigned& neg) {
@@ -352,10 +333,13 @@ __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(
       const uint32_t va = opaque(vat);
       static_for<NDB / 4>([&](auto B_) {
         constexpr int b4 = 4 * decltype(B_)::value;
-        v4i vv[4];
-        v_read4<D>(va ^ (32 * b4), va ^ (32 * b4 + 32), va ^ (32 * b4 + 64), va ^ (32 * b4 + 96), vv);
+        v8bf vv[4];                                      // 32 keys of 4 channel blocks: two reads each, 16 keys apart
+        vt_read4<0, 16 * ROW>(va ^ (32 * b4), va ^ (32 * b4 + 32), va ^ (32 * b4 + 64), va ^ (32 * b4 + 96), vv[0], vv[1], vv[2], vv[3]);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) oacc[b4 + d] = mma16<PB>(vv[d], pl, mma16<PB>(vv[d], pk, oacc[b4 + d]));
+        for (int d = 0; d < 4; ++d) {
+          const v4i x = __builtin_bit_cast(v4i, vv[d]);
+          oacc[b4 + d] = mma16<PB>(x, pl, mma16<PB>(x, pk, oacc[b4 + d]));
+        }
       });
       id = id1;
       id1 = id2;

@@ -37,8 +37,8 @@ __device__ __forceinline__ int vswz(int row, int ch) {
 }
 
 // The A operands (V^T) of one K-step for two channel blocks: per block two
-// transposing reads 8 keys apart, at LDS byte addresses a + OFF and a + OFF + 8
-// rows.  One asm block with its own wait: for the builtin the compiler first
+// transposing reads, at LDS byte addresses a + OFF and a + OFF8 (8 keys further on
+// for 32 x 32 x 16, 16 for 16 x 16 x 32).  One asm block with its own wait: for the builtin the compiler first
 // waits for every direct-to-LDS load in flight (see sage_common.h).
 template <int OFF, int OFF8>
 __device__ __forceinline__ void vt_read2(uint32_t a0, uint32_t a1, v8bf& r0, v8bf& r1) {
