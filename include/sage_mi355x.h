@@ -359,8 +359,12 @@ int sage_attn_int8_bwd_ws(const void* q, const void* k, const void* v, const flo
 /* softmax and sums are fp32.  Probabilities are rounded to 16 bits for     */
 /* their product with V (over the cache in two 16-bit parts).  D is 64 or   */
 /* 128.  `stream` must belong to the current device.  No output overlaps an */
-/* input or another output.  Results are the same bits from call to call.   */
-/* Nothing is allocated inside.                                             */
+/* input or another output.  The same call gives the same bits; between     */
+/* calls of other B, H, N or S, by which the work is split, a row's last    */
+/* bits may differ.  Sums over keys are divided at their end: in bf16,      */
+/* |v| up to 2^120 / (keys seen) keeps them finite.  L has no gradient.     */
+/* Nothing is allocated inside.  Calls that may overlap, in two streams or  */
+/* two captured graphs, need a workspace each.                              */
 /* ======================================================================== */
 
 /* Element strides of a [B, H, N, D] tensor; its channels are contiguous and
@@ -387,12 +391,17 @@ int sage_attn_window_fwd(const void* q, const void* k, const void* v, void* o, f
 
 /* Workspace bytes for sage_attn_window_bwd (two fp32 values per query row, and fp32
  * parts of the gradients of keys whose queries several workgroups share: the sinks',
- * and all keys' of small batches); 0 for invalid arguments.  Host only. */
+ * and all keys' where the batch is small or the keys' numbers of queries differ much:
+ * 271 MB for 8192 causal tokens of 32 / 8 heads, D = 128, 19 MB under a window of 1024 with
+ * 16 sinks);
+ * 0 for invalid arguments.  Host only. */
 size_t sage_attn_window_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D, int window, int sinks);
 
 /*
  * sage_attn_window_bwd -- backward: the gradients of q, k, v for dout, that of o.
- *  q, k, v, o, lse, lens, window, sinks: as given to the forward, and its outputs
+ *  q, k, v, o, lse, lens, window, sinks: as given to the forward, and its outputs.
+ *            They have to be this call's own: rows of dS are taken to sum to zero, so an
+ *            o and lse that were joined from parts of the keys give wrong dq and dk
  *  dout    : [B, Hq, N, D], any strides; rows behind a sequence's end are not read
  *  dq      : [B, Hq, N, D], dk, dv: [B, Hkv, N, D] (summed over the group's query
  *            heads), contiguous, 16-byte aligned; 0 behind a sequence's end
@@ -436,8 +445,9 @@ typedef struct {
  *  k, v   : [S, Hkv, N, D] 16-bit, any strides, 16-byte aligned
  *  pos    : int32 [S], cached tokens before the call; counts: int32 [S] or NULL (N)
  *  weights: fp32 [S, Hkv, weights_stride] or NULL: set to 0 for the new tokens
- * Two tokens of one call stored in the same slot leave either.  For an INT8 cache
- * k and v must be finite.
+ * Where two tokens of one call go to the same slot, parts of both may be left there (of
+ * an INT8 cache also one's codes with the other's scale).  For an INT8 cache k and v
+ * must be finite.
  */
 int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
                    const sage_strides* v_strides, const int32_t* table, int max_pages, const int32_t* pos,
@@ -445,7 +455,9 @@ int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, con
                    hipStream_t stream);
 
 /* Workspace bytes for sage_attn_paged_decode; 0 where it needs none (short
- * capacities, no weights) and for invalid arguments.  Host only. */
+ * capacities, no weights) and for invalid arguments.  With weights it holds the scores,
+ * 4 * S * Hq * max_pages * page_size bytes whatever the lengths and the window are.
+ * Host only. */
 size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int max_pages, int page_size, int with_weights);
 
 /*
@@ -460,7 +472,7 @@ size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int 
  *           token j, summed over the group's query heads, is added to
  *           weights[s][head][j]; weights_stride >= max_pages * page_size
  *  workspace: at least sage_attn_paged_decode_workspace_size() bytes, 256-byte
- *           aligned (NULL if that is 0); calls that may overlap need one each
+ *           aligned (NULL if that is 0)
  */
 int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
                            float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,
@@ -477,7 +489,8 @@ size_t sage_kv_evict_workspace_size(int S, int Hkv, int max_pages, int page_size
  * stay, and of those between the ones with the largest weights (equal weights:
  * the lowest index; NaN is lowest).  The kept tokens are copied, in their order,
  * to positions 0, 1, ... of the pages in new_table.  Shorter sequences are copied
- * whole (a token whose new place is its old one stays there).
+ * whole (a token whose new place is its old one stays there).  Which tokens are kept
+ * does not depend on their pages: one without a page leaves its new place as it was.
  *  weights    : fp32 [S, Hkv, weights_stride], weights_stride >= max_pages * page_size
  *  new_table  : int32 [S, new_max_pages], new_max_pages * page_size >= budget.  Its
  *               pages may not hold other tokens that this call moves

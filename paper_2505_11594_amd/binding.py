@@ -496,7 +496,7 @@ def attn_window_bwd_workspace_size(B: int, Hq: int, Hkv: int, N: int, D: int, wi
 
 def sage_attn_window_bwd(q, k, v, o, lse, dout, window=None, sinks: int = 0, lens=None, workspace=None, out=None):
     """The gradients (dQ, dK, dV) of sage_attn_window_fwd for dout, the gradient of its O; o and lse
-    are its outputs, window, sinks and lens as given to it.  q, k, v, o, dout of any strides with
+    are its own outputs (not joined from parts of the keys), window, sinks and lens as given to it.  q, k, v, o, dout of any strides with
     contiguous channels; the gradients are contiguous, of q's type, dK and dV summed over a group's
     query heads.  ``out``: three preallocated tensors; with ``workspace`` (uint8, at least
     attn_window_bwd_workspace_size bytes) too nothing is allocated inside."""
@@ -583,8 +583,9 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
                            weights=None, lse: bool = True, out=None, lse_out=None, workspace=None):
     """Attention of each sequence's last token, q [S, Hq, D], over its lens[s] cached tokens (its own
     among them); the cache as in sage_kv_append.  ``weights`` fp32 [S, Hkv, >= max_pages * page_size]:
-    the attention weights, summed over a group's query heads, are added to it.  Returns (O, L), L fp32
-    [S, Hq] (None when ``lse`` is False).  With ``workspace`` (uint8, at least
+    the attention weights, summed over a group's query heads, are added to it (this takes a workspace
+    of 4 * S * Hq * max_pages * page_size bytes).  Returns (O, L), L fp32 [S, Hq] (None when ``lse``
+    is False).  With ``workspace`` (uint8, at least
     attn_paged_decode_workspace_size bytes) and ``out``, ``lse_out`` nothing is allocated inside."""
     import torch
     c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
