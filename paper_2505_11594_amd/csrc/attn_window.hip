@@ -13,7 +13,7 @@
 // Bound by issue: per 32 x 64 piece of D = 128 the 32 MFMAs take 1024 cycles of a SIMD,
 // 32 exponentials 512 and the other VALU work about 400, and the two waves of a SIMD
 // hide little of one kind under the other.  32768 tokens, 32/8 heads, window 4096:
-// 2.15-2.3 ms, 900-960 TFLOP/s (a large bf16 matrix product: 1200).
+// 2.20-2.26 ms a call, 910-940 TFLOP/s (a large bf16 matrix product: 1200).
 //
 // P is rounded to the input's type for the second product (relative error 2^-8
 // in bf16, 2^-11 in fp16 per probability); everything else is fp32.

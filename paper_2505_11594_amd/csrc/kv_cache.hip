@@ -1,6 +1,6 @@
 // The paged cache of keys and values: storing new tokens, and shortening cached
-// sequences to their most attended tokens.  Both move rows and are bound by the
-// bytes they read and write.
+// sequences to their most attended tokens.  Both move rows; the bytes they read and write
+// bound them, but for the 8-bit append, whose arithmetic does (below).
 #include "lm_args.h"
 #include "sage_common.h"
 #include "window.h"
@@ -35,7 +35,9 @@ __device__ __forceinline__ void quantize8(const v4i x, float* scale, v2u* codes)
 }
 
 // D / 8 lanes per row; rows in the order (sequence, head, token), in which both
-// sides are contiguous for one head.
+// sides are contiguous for one head.  4 sequences of up to 4096 tokens, 8 heads: 16-bit
+// 15-16 us, 5.8 TB/s; INT8 19-20 us, 3.5 TB/s, as the VALU is busy 95% of the time (65%
+// for 16 bits: the divisions that find a row's place).
 template <int D, bool BF16, bool I8>
 __global__ __launch_bounds__(256) void kv_append_kernel(const Append a) {
   constexpr int LPR = D / 8;

@@ -37,11 +37,12 @@ __device__ __forceinline__ float add_pair(uint32_t x, float c) {
   else return __builtin_amdgcn_fdot2(__builtin_bit_cast(v2h, x), __builtin_bit_cast(v2h, 0x3C003C00u), c, false);
 }
 
-// Probabilities enter the second product in 16 bits.  In fp16 they are carried
-// 2^15 larger: probabilities down to 2^-29 of the row's maximum stay normal
-// numbers instead of those above 2^-14 only, and the largest is 2^15 < 65504.  The
-// sums carry the same factor and lose it in the final division.  bf16 has the
-// range of fp32 and needs none.
+// Probabilities enter the second product in 16 bits.  In fp16 the one-token attention
+// and the backward carry them 2^15 larger: probabilities down to 2^-29 of the row's
+// maximum stay normal numbers instead of those above 2^-14 only, and the largest is
+// 2^15 < 65504.  (The window forward carries 2^7, as its maximum may lag by 2^8: normal
+// down to 2^-21 of that maximum.)  The sums carry the same factor and lose it in the final
+// division.  bf16 has the range of fp32 and needs none.
 template <bool BF16> constexpr float kPShift = BF16 ? 0.0f : 15.0f;
 
 // A lane's LDS addresses in a tile at offset 0 of LDS: rows start on multiples of
