@@ -154,7 +154,8 @@ __device__ __forceinline__ void find_nonfinite(const v4i x, unsigned& pos, unsig
 // BF16: the type of q and o.  I8: 8-bit cache; its codes are exact in either type,
 // and P times V's scale, whose size nothing bounds, is taken in bf16.  P enters its
 // product with V in two parts, rounded and rest (together 2^-16 of it in bf16, 2^-22 in
-// fp16): the matrix instructions have the time.
+// fp16): the matrix instructions have the time.  (D = 64 is held to the 168 registers that
+// let three waves on a SIMD; left alone it takes 171.)
 template <int D, bool BF16, bool I8>
 __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(const Decode a) {
   constexpr bool PB = BF16 || I8;                        // type of P and V in the second product
