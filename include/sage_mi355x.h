@@ -3,7 +3,8 @@
  * forward of SageAttention3 (arXiv 2505.11594), of the paper's 8-bit
  * attention (SageBwd: the forward of Algorithm 2, the backward of Algorithm 3),
  * and of 16-bit attention of language models with a sliding window, forward and
- * backward, and over a paged cache.
+ * backward, and over a paged cache (16-bit, INT8 or MXFP4), with the norms and the
+ * rotation of its queries and keys and the page tables of its cache.
  *
  * Every function returns an int status (sage_status).  Arguments are checked
  * on the host before any HIP call, so invalid calls fail without touching the
@@ -62,6 +63,9 @@ typedef enum {
                                       with SAGE_BKV256, non-causal, without SAGE_SMOOTH_Q;
                                       otherwise SAGE_ERR_UNSUPPORTED.  Same results.      */
 #define SAGE_FMT_ALL_BITS   0x1FFu
+/* Calls on a paged cache, and of norms with rotation, only: */
+#define SAGE_KV_FP4         0x200u /* the cache holds MXFP4 rows                           */
+#define SAGE_ROPE_PAIRS     0x400u /* channels 2i and 2i+1 rotate together, not i and i+R/2 */
 
 /* ---- quantization roles ------------------------------------------------ */
 #define SAGE_ROLE_Q 0
@@ -355,7 +359,8 @@ int sage_attn_int8_bwd_ws(const void* q, const void* k, const void* v, const flo
 /* infinity or NaN in a value that it sees makes that channel of its o      */
 /* infinite or NaN, and no other.                                           */
 /* Everything is 16-bit in the type that flags give (SAGE_IN_FP16 or        */
-/* SAGE_IN_BF16, the only accepted bits), o and gradients too; scores,      */
+/* SAGE_IN_BF16; the only accepted bits but where a call names others), o   */
+/* and gradients too; scores,                                               */
 /* softmax and sums are fp32.  Probabilities are rounded to 16 bits for     */
 /* their product with V (over the cache in two 16-bit parts).  D is 64 or   */
 /* 128.  `stream` must belong to the current device.  No output overlaps an */
@@ -426,6 +431,12 @@ int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void
  *     s = max|x| / 127 per row,  code = rint(x * fl32(1/s)) (ties to even),
  * with s in the fp32 arrays [pages, Hkv, page_size] (a row whose s is below
  * 2^-126 has s = 0 and zero codes).
+ * With SAGE_KV_FP4 in a call's flags (sage_kv_append, sage_kv_append_slots and
+ * sage_attn_paged_decode) the cache is MXFP4: a row is D / 2 bytes of E2M1 codes, channel
+ * 2i in the low half of byte i, strides count bytes (multiples of 16), and k_scale
+ * and v_scale point to bytes [pages, Hkv, page_size, D / 32] (4-byte aligned): the
+ * scales 2^(byte - 127) of 32 channels each, the smallest (of bytes 0 to 254) with 6 * scale >=
+ * max|x|; codes are those of x / scale, nearest, ties to even, as sage_quant_fp4 makes them.
  * A sequence's pages are a row of `table`, int32 [S, max_pages] on the device:
  * its token j lies in page table[s][j / page_size], slot j % page_size.  Only
  * entries of tokens that the sequence has are read; a token whose entry is not
@@ -446,13 +457,24 @@ typedef struct {
  *  pos    : int32 [S], cached tokens before the call; counts: int32 [S] or NULL (N)
  *  weights: fp32 [S, Hkv, weights_stride] or NULL: set to 0 for the new tokens
  * Where two tokens of one call go to the same slot, parts of both may be left there (of
- * an INT8 cache also one's codes with the other's scale).  For an INT8 cache k and v
- * must be finite.
+ * an INT8 or MXFP4 cache also one's codes with the other's scale).  For an INT8 or MXFP4
+ * cache k and v must be finite.
  */
 int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
                    const sage_strides* v_strides, const int32_t* table, int max_pages, const int32_t* pos,
                    const int32_t* counts, float* weights, int64_t weights_stride, int S, int N, unsigned flags,
                    hipStream_t stream);
+
+/*
+ * sage_kv_append_slots -- the same by slots, page * page_size + place in the page, as
+ * sage_kv_plan gives them: token t of row b goes to slots[b][t]; slots that the cache does
+ * not have, negative ones among them, are skipped.
+ *  k, v   : [B, Hkv, N, D] 16-bit, any strides, 16-byte aligned (the tokens of several
+ *           sequences behind one another are one row: B = 1); B is at most 65535
+ *  slots  : int64 [B, N]
+ */
+int sage_kv_append_slots(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
+                         const sage_strides* v_strides, const int64_t* slots, int B, int N, unsigned flags, hipStream_t stream);
 
 /* Workspace bytes for sage_attn_paged_decode; 0 where it needs none (short
  * capacities, no weights) and for invalid arguments.  With weights it holds the scores,
@@ -473,6 +495,8 @@ size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int 
  *           weights[s][head][j]; weights_stride >= max_pages * page_size
  *  workspace: at least sage_attn_paged_decode_workspace_size() bytes, 256-byte
  *           aligned (NULL if that is 0)
+ * Over an MXFP4 cache weights must be NULL (SAGE_ERR_UNSUPPORTED), and q of a block of 32
+ * channels enters with an error of at most 2^-22 (fp16: 2^-26) of the block's largest value.
  */
 int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
                            float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,
@@ -506,6 +530,79 @@ int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_page
                   int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
                   int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
                   size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * sage_qk_norm_rope_fwd -- queries and keys as an attention takes them: the norm of every
+ * head's row, and its rotation by the token's position.  Per row x of D channels:
+ *     y = x * (mean(x^2) + eps)^(-1/2) * weight,   t_i = p * inv_freq[i], i < rotary / 2,
+ *     (z_a, z_b) = (y_a cos t_i - y_b sin t_i, y_b cos t_i + y_a sin t_i)
+ * with the pair (a, b) = (i, i + rotary / 2), or (2i, 2i + 1) with SAGE_ROPE_PAIRS; channels
+ * from rotary on are y.  Angles are found in 64 bits, all else in 32, rounded once.
+ *  q, k     : [B, Hq, N, D], [B, Hkv, N, D] 16-bit, any strides (views of one packed
+ *             projection too), 16-byte aligned; |x| below 2^60
+ *  q_weight, k_weight: fp32 [D] or NULL (ones); inv_freq: fp32 [rotary / 2]
+ *  rotary   : 0 to D, a multiple of 8; eps: 2^-100 to 1
+ *  pos      : int32: with pos_per_token [B, N], the tokens' positions; without [B], those of
+ *             the rows' first tokens, from which they run on (below 2^31); or NULL (0)
+ *  lens     : int32 [B] or NULL: tokens of each sequence of a padded batch.  What lies
+ *             behind is not read, and zero in the outputs
+ *  zq, zk   : shapes of q and k, any strides; may be q and k themselves (the same address
+ *             and strides), rows may not overlap otherwise
+ * flags: SAGE_IN_BF16, SAGE_ROPE_PAIRS.  No workspace.
+ */
+int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
+                          int rotary, const int32_t* pos, int pos_per_token, const int32_t* lens, void* zq, void* zk, int B,
+                          int Hq, int Hkv, int N, int D, float eps, unsigned flags, const sage_strides* q_strides,
+                          const sage_strides* k_strides, const sage_strides* zq_strides, const sage_strides* zk_strides,
+                          hipStream_t stream);
+
+/* Workspace bytes for sage_qk_norm_rope_bwd (sums for the weights' gradients, at most
+ * 2 MB); 0 for invalid arguments.  Host only. */
+size_t sage_qk_norm_rope_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D);
+
+/*
+ * sage_qk_norm_rope_bwd -- backward: the gradients of q, k and of the weights.
+ *  q, k and all else as given to the forward
+ *  dzq, dzk : gradients of zq, zk, any strides; not read behind a sequence's end
+ *  dq, dk   : shapes of q and k, any strides; zero behind a sequence's end.  They may be
+ *             dzq and dzk, or q and k, themselves
+ *  dq_weight, dk_weight: fp32 [D] or NULL, written (not added to); the same call gives the
+ *             same bits
+ *  workspace: at least sage_qk_norm_rope_bwd_workspace_size() bytes, 256-byte aligned
+ */
+int sage_qk_norm_rope_bwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
+                          int rotary, const int32_t* pos, int pos_per_token, const int32_t* lens, const void* dzq, const void* dzk,
+                          void* dq, void* dk, float* dq_weight, float* dk_weight, int B, int Hq, int Hkv, int N, int D, float eps,
+                          unsigned flags, const sage_strides* q_strides, const sage_strides* k_strides,
+                          const sage_strides* dzq_strides, const sage_strides* dzk_strides, const sage_strides* dq_strides,
+                          const sage_strides* dk_strides, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * sage_kv_plan -- the pages and slots of a batch's next tokens, on the device (a captured
+ * graph follows the requests).  Request s has lens[s] cached tokens and brings counts[s]
+ * new ones; with a negative count it has ended.
+ *   1. Pages of requests that have ended go onto the stack of free pages, in order; their rows
+ *      of the table become -1, their lengths 0.
+ *   2. The others are granted their tokens in order.  With A and C the pages and tokens asked
+ *      for up to a request, its own among them (not counting those that would exceed max_pages),
+ *      it is granted iff it fits its row of the table, (needs no new page or A <= free pages)
+ *      and C <= max_tokens.  New pages are taken from the top of the stack.
+ *  table      : int32 [S, max_pages]; a request's pages are its own (none is shared)
+ *  lens       : int32 [S], becomes the lengths with the granted tokens
+ *  counts     : int32 [S]
+ *  free_pages : int32 [free_capacity], the stack (the top is entry n_free - 1); what would go
+ *               beyond its capacity is dropped
+ *  n_free     : int32 [1]
+ *  granted    : int32 [S], counts[s] or 0;  starts: int32 [S + 1], their sums before each
+ *  pos, slots : int32, int64 [max_tokens]: new token i's position in its sequence and slot,
+ *               page * page_size + place in the page; behind the last 0 and -1.  Tokens of
+ *               request s are starts[s] to starts[s + 1] - 1
+ * table, lens, free_pages and n_free are changed in place.  No two arguments overlap.  S is at
+ * most 65535.  No workspace.
+ */
+int sage_kv_plan(int32_t* table, int max_pages, int32_t* lens, const int32_t* counts, int32_t* free_pages, int free_capacity,
+                 int32_t* n_free, int page_size, int32_t* granted, int32_t* starts, int32_t* pos, int64_t* slots, int max_tokens,
+                 int S, hipStream_t stream);
 
 /* Human-readable status name; never NULL. */
 const char* sage_status_string(int status);

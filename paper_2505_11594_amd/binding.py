@@ -21,6 +21,7 @@ SAGE_NO_SMOOTH_K = 0x10
 SAGE_SMOOTH_Q = 0x20
 SAGE_BKV64 = 0x40
 SAGE_BKV256 = 0x80
+SAGE_KV_FP4, SAGE_ROPE_PAIRS = 0x200, 0x400
 SAGE_WG256 = 0x100       # 256 queries per workgroup (MXFP4, 256-key tiles, non-causal, no smoothing Q)
 
 
@@ -88,6 +89,13 @@ def lib():
         L.sage_attn_window_bwd_workspace_size.restype = sz
         L.sage_attn_window_bwd.argtypes = [vp] * 10 + [i] * 7 + [u] + [st] * 5 + [vp, sz, vp]
         L.sage_kv_append.argtypes = [ca, vp, vp, st, st, vp, i, vp, vp, vp, i64, i, i, u, vp]
+        L.sage_kv_append_slots.argtypes = [ca, vp, vp, st, st, vp, i, i, u, vp]
+        f = ctypes.c_float
+        L.sage_qk_norm_rope_fwd.argtypes = [vp] * 5 + [i, vp, i, vp, vp, vp] + [i] * 5 + [f, u] + [st] * 4 + [vp]
+        L.sage_qk_norm_rope_bwd_workspace_size.argtypes = [i] * 5
+        L.sage_qk_norm_rope_bwd_workspace_size.restype = sz
+        L.sage_qk_norm_rope_bwd.argtypes = [vp] * 5 + [i, vp, i] + [vp] * 7 + [i] * 5 + [f, u] + [st] * 6 + [vp, sz, vp]
+        L.sage_kv_plan.argtypes = [vp, i, vp, vp, vp, i, vp, i, vp, vp, vp, vp, i, i, vp]
         L.sage_attn_paged_decode_workspace_size.argtypes = [i] * 7
         L.sage_attn_paged_decode_workspace_size.restype = sz
         L.sage_attn_paged_decode.argtypes = [ca, vp, i64, i64, vp, vp, vp, i, vp, i, i, i, i, vp, i64, u, vp, sz, vp]
@@ -101,7 +109,8 @@ def lib():
                      "sage_attn_fp4_fwd_noalloc", "sage_attn_fp4_fwd_prequant", "sage_attn_bf16_fwd", "sage_quant_int8_sizes",
                      "sage_quant_int8", "sage_attn_int8_fwd", "sage_attn_int8_fwd_ws",
                      "sage_attn_int8_fwd_prequant", "sage_attn_int8_bwd", "sage_attn_int8_bwd_ws",
-                     "sage_attn_window_fwd", "sage_attn_window_bwd", "sage_kv_append", "sage_attn_paged_decode", "sage_kv_evict"):
+                     "sage_attn_window_fwd", "sage_attn_window_bwd", "sage_kv_append", "sage_attn_paged_decode", "sage_kv_evict",
+                     "sage_kv_append_slots", "sage_qk_norm_rope_fwd", "sage_qk_norm_rope_bwd", "sage_kv_plan"):
             getattr(L, name).restype = i
         _lib = L
     return _lib
@@ -521,26 +530,37 @@ def sage_attn_window_bwd(q, k, v, o, lse, dout, window=None, sinks: int = 0, len
     return dq, dk, dv
 
 
-def _check_cache(k_cache, v_cache, k_scale, v_scale, table):
-    """The C description of a paged cache, and (S, max_pages, page_size, Hkv, D)."""
+def _check_pages(k_cache, v_cache, k_scale, v_scale):
+    """The C description of a paged cache, its flag, and (page_size, Hkv, D)."""
     import torch
     ks, vs = _rows(k_cache, "k_cache"), _rows(v_cache, "v_cache")
     P, Hkv, page, D = k_cache.shape
     _same(v_cache, k_cache, "v_cache", k_cache.shape)
-    dev = k_cache.device
-    if (k_scale is None) != (v_scale is None) or (k_cache.dtype == torch.int8) != (k_scale is not None):
-        raise ValueError("an int8 cache has k_scale and v_scale, a 16-bit one has neither")
-    if k_scale is not None:
+    dev, fp4 = k_cache.device, k_cache.dtype == torch.uint8
+    if (k_scale is None) != (v_scale is None) or (k_cache.dtype in (torch.int8, torch.uint8)) != (k_scale is not None):
+        raise ValueError("an int8 or uint8 (MXFP4) cache has k_scale and v_scale, a 16-bit one has neither")
+    if fp4:
+        D *= 2
+        _check_tensor(k_scale, "k_scale", (P, Hkv, page, D // 32), torch.uint8, dev)
+        _check_tensor(v_scale, "v_scale", (P, Hkv, page, D // 32), torch.uint8, dev)
+    elif k_scale is not None:
         _check_tensor(k_scale, "k_scale", (P, Hkv, page), torch.float32, dev)
         _check_tensor(v_scale, "v_scale", (P, Hkv, page), torch.float32, dev)
     else:
         _in_flag(k_cache)
+    return _cache(k_cache.data_ptr(), v_cache.data_ptr(), _adr(k_scale) or 0, _adr(v_scale) or 0, *ks, *vs, P, page, Hkv, D), \
+        SAGE_KV_FP4 if fp4 else 0, (page, Hkv, D)
+
+
+def _check_cache(k_cache, v_cache, k_scale, v_scale, table):
+    """The same with its tables: the C description, the flag, and (S, max_pages, page_size, Hkv, D)."""
+    import torch
+    c, kind, dims = _check_pages(k_cache, v_cache, k_scale, v_scale)
     if table.dim() != 2 or table.numel() == 0:
         raise ValueError("table must be a non-empty [S, max_pages] tensor")
     S, M = table.shape
-    _check_tensor(table, "table", (S, M), torch.int32, dev)
-    return _cache(k_cache.data_ptr(), v_cache.data_ptr(), _adr(k_scale) or 0, _adr(v_scale) or 0, *ks, *vs, P, page, Hkv, D), \
-        (S, M, page, Hkv, D)
+    _check_tensor(table, "table", (S, M), torch.int32, k_cache.device)
+    return c, kind, (S, M) + dims
 
 
 def _check_weights(w, what: str, S: int, Hkv: int, capacity: int, device):
@@ -553,12 +573,13 @@ def _check_weights(w, what: str, S: int, Hkv: int, capacity: int, device):
 def sage_kv_append(k, v, k_cache, v_cache, table, pos, counts=None, k_scale=None, v_scale=None, weights=None):
     """Store new tokens in a paged cache: token t < counts[s] (None: all) of k, v [S, Hkv, N, D] at
     position pos[s] + t of sequence s.  The cache is [pages, Hkv, page_size, D] of any strides with
-    contiguous channels, of k's type or int8 with fp32 scales [pages, Hkv, page_size]; ``table`` int32
-    [S, max_pages] holds the sequences' pages.  ``weights`` [S, Hkv, >= max_pages * page_size] is set
-    to 0 at the new tokens."""
+    contiguous channels, of k's type or int8 with fp32 scales [pages, Hkv, page_size], or MXFP4: uint8
+    [pages, Hkv, page_size, D / 2] of two codes each with uint8 scales [pages, Hkv, page_size, D / 32].
+    ``table`` int32 [S, max_pages] holds the sequences' pages.  ``weights`` [S, Hkv, >= max_pages *
+    page_size] is set to 0 at the new tokens."""
     import torch
-    c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
-    flags = _in_flag(k)
+    c, kind, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    flags = _in_flag(k) | kind
     ks, vs = _rows(k, "k"), _rows(v, "v")
     N, dev = int(k.shape[2]), k_cache.device
     _same(v, k, "v", (S, Hkv, N, D))
@@ -574,6 +595,23 @@ def sage_kv_append(k, v, k_cache, v_cache, table, pos, counts=None, k_scale=None
           _adr(counts), _adr(weights), weights.shape[2] if weights is not None else 0, S, N, flags)
 
 
+def sage_kv_append_slots(k, v, k_cache, v_cache, slots, k_scale=None, v_scale=None):
+    """Store new tokens in a paged cache (as in sage_kv_append) by slots, int64 [B, N] as sage_kv_plan
+    gives them (page * page_size + place in the page; negative: not stored): token t of row b of k, v
+    [B, Hkv, N, D].  The tokens of several sequences behind one another are one row, B = 1."""
+    import torch
+    c, kind, (page, Hkv, D) = _check_pages(k_cache, v_cache, k_scale, v_scale)
+    flags, dev = _in_flag(k) | kind, k_cache.device
+    ks, vs = _rows(k, "k"), _rows(v, "v")
+    B, N = int(k.shape[0]), int(k.shape[2])
+    _same(k, k, "k", (B, Hkv, N, D))
+    _same(v, k, "v", (B, Hkv, N, D))
+    if k.device != dev or (k_scale is None and k.dtype != k_cache.dtype):
+        raise ValueError("k and v must be on %s and of the cache's type" % dev)
+    _check_tensor(slots, "slots", (B, N), torch.int64, dev)
+    _call("sage_kv_append_slots", dev, c, _adr(k), _adr(v), _strides(*ks), _strides(*vs), _adr(slots), B, N, flags)
+
+
 def attn_paged_decode_workspace_size(S: int, Hq: int, Hkv: int, D: int, max_pages: int, page_size: int,
                                      weights: bool = False) -> int:
     return int(lib().sage_attn_paged_decode_workspace_size(S, Hq, Hkv, D, max_pages, page_size, int(bool(weights))))
@@ -584,12 +622,12 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
     """Attention of each sequence's last token, q [S, Hq, D], over its lens[s] cached tokens (its own
     among them); the cache as in sage_kv_append.  ``weights`` fp32 [S, Hkv, >= max_pages * page_size]:
     the attention weights, summed over a group's query heads, are added to it (this takes a workspace
-    of 4 * S * Hq * max_pages * page_size bytes).  Returns (O, L), L fp32 [S, Hq] (None when ``lse``
+    of 4 * S * Hq * max_pages * page_size bytes; not over an MXFP4 cache).  Returns (O, L), L fp32 [S, Hq] (None when ``lse``
     is False).  With ``workspace`` (uint8, at least
     attn_paged_decode_workspace_size bytes) and ``out``, ``lse_out`` nothing is allocated inside."""
     import torch
-    c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
-    flags, dev = _in_flag(q), k_cache.device
+    c, kind, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    flags, dev = _in_flag(q) | kind, k_cache.device
     qs = _rows(q, "q", 3)
     Hq = int(q.shape[1])
     if tuple(q.shape) != (S, Hq, D) or q.device != dev or (k_scale is None and q.dtype != k_cache.dtype):
@@ -600,6 +638,8 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
     window, sinks = _window_of(window, sinks)
     _check_tensor(lens, "lens", (S,), torch.int32, dev)
     if weights is not None:
+        if kind:
+            raise ValueError("weights are not added up over an MXFP4 cache")
         _check_weights(weights, "weights", S, Hkv, M * page, dev)
     o = torch.empty((S, Hq, D), dtype=q.dtype, device=dev) if out is None else out
     _check_tensor(o, "out", (S, Hq, D), q.dtype, dev)
@@ -631,8 +671,10 @@ def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int
     kept [S, Hkv, budget]: the old positions, -1 behind the last).  With ``out`` (these three) and
     ``workspace`` (uint8, at least kv_evict_workspace_size bytes) nothing is allocated inside."""
     import torch
-    c, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
+    c, kind, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
     dev = k_cache.device
+    if kind:
+        raise ValueError("an MXFP4 cache is not shortened")
     _check_tensor(lens, "lens", (S,), torch.int32, dev)
     _check_weights(weights, "weights", S, Hkv, M * page, dev)
     if new_table.dim() != 2 or new_table.numel() == 0:
@@ -655,6 +697,121 @@ def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int
           M2, budget, keep_first, keep_last, _adr(new_lens), _adr(new_weights), _adr(kept), S, _adr(workspace),
           workspace.numel() if workspace is not None else 0)
     return new_lens, new_weights, kept
+
+
+# ------------------------------------------------- norms with rotation, page tables
+def _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved):
+    """What forward and backward share: the C arguments up to lens, (B, Hq, Hkv, N, D), eps and flags, and the
+    strides of q and k."""
+    import torch
+    flags = _in_flag(q) | (SAGE_ROPE_PAIRS if interleaved else 0)
+    (B, Hq, N, D), Hkv, dev = q.shape, k.shape[1], q.device
+    qs, ks = _rows(q, "q"), _rows(k, "k")
+    if Hq % Hkv:
+        raise ValueError("q's %d heads are no multiple of k's %d" % (Hq, Hkv))
+    _same(k, q, "k", (B, Hkv, N, D))
+    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if w is not None:
+            _check_tensor(w, what, (D,), torch.float32, dev)
+    half = inv_freq.numel()
+    if half > D // 2 or half % 4:
+        raise ValueError("inv_freq must have at most %d entries, a multiple of 4, got %d" % (D // 2, half))
+    _check_tensor(inv_freq, "inv_freq", (half,), torch.float32, dev)
+    each = pos is not None and pos.dim() == 2
+    if pos is not None:
+        _check_tensor(pos, "pos", (B, N) if each else (B,), torch.int32, dev)
+    if lens is not None:
+        _check_tensor(lens, "lens", (B,), torch.int32, dev)
+    if not 2.0 ** -100 <= eps <= 1:
+        raise ValueError("eps must be 2^-100 to 1, got %r" % (eps,))
+    head = (_adr(q), _adr(k), _adr(q_weight), _adr(k_weight), _adr(inv_freq), 2 * half, _adr(pos), int(each), _adr(lens))
+    return head, (B, Hq, Hkv, N, D, float(eps), flags), [_strides(*qs), _strides(*ks)]
+
+
+def sage_qk_norm_rope_fwd(q, k, q_weight, k_weight, inv_freq, pos=None, lens=None, eps: float = 1e-6,
+                          interleaved: bool = False, out=None):
+    """Each head's row of q [B, Hq, N, D] and k [B, Hkv, N, D] (16-bit, any strides with contiguous
+    channels, views of one packed projection too) normed, x * (mean(x^2) + eps)^(-1/2) * weight, and
+    its first 2 * len(inv_freq) channels rotated by position * inv_freq: channel i with i +
+    len(inv_freq), or 2i with 2i + 1 if ``interleaved``.  Weights fp32 [D] or None; inv_freq fp32, a
+    multiple of 4 entries.  ``pos``: int32 [B, N], or [B] for rows whose positions run on from these,
+    or None (from 0 on).  ``lens``: int32 [B], the tokens of a padded batch's sequences; what lies
+    behind is not read, and 0 in the outputs.  Returns both like q and k; ``out``: two tensors of any
+    strides, which may be q and k themselves."""
+    import torch
+    head, tail, st = _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved)
+    zq, zk = out if out is not None else [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
+    for t, x, what in ((zq, q, "out[0]"), (zk, k, "out[1]")):
+        _same(t, q, what, x.shape)
+        st.append(_strides(*_rows(t, what)))
+    _call("sage_qk_norm_rope_fwd", q.device, *head, _adr(zq), _adr(zk), *tail, *st)
+    return zq, zk
+
+
+def qk_norm_rope_bwd_workspace_size(B: int, Hq: int, Hkv: int, N: int, D: int) -> int:
+    return int(lib().sage_qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D))
+
+
+def sage_qk_norm_rope_bwd(q, k, q_weight, k_weight, inv_freq, dzq, dzk, pos=None, lens=None, eps: float = 1e-6,
+                          interleaved: bool = False, workspace=None, out=None):
+    """The gradients (dq, dk, dq_weight, dk_weight) of sage_qk_norm_rope_fwd for dzq and dzk, those of
+    its outputs; all else as given to it.  dq and dk are like q and k (0 behind a sequence's end), those
+    of the weights fp32 [D] (None for a weight that is None).  ``out``: four tensors (or None for the
+    weights'), dq and dk of any strides, which may be dzq and dzk themselves; with ``workspace`` (uint8,
+    at least qk_norm_rope_bwd_workspace_size bytes) too nothing is allocated inside."""
+    import torch
+    head, tail, st = _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved)
+    B, Hq, Hkv, N, D = tail[:5]
+    dev = q.device
+    for t, x, what in ((dzq, q, "dzq"), (dzk, k, "dzk")):
+        _same(t, q, what, x.shape)
+        st.append(_strides(*_rows(t, what)))
+    if out is None:
+        dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k))
+        dwq, dwk = (torch.empty(D, dtype=torch.float32, device=dev) if w is not None else None for w in (q_weight, k_weight))
+    else:
+        dq, dk, dwq, dwk = out
+    for t, x, what in ((dq, q, "dq"), (dk, k, "dk")):
+        _same(t, q, what, x.shape)
+        st.append(_strides(*_rows(t, what)))
+    for w, what in ((dwq, "dq_weight"), (dwk, "dk_weight")):
+        if w is not None:
+            _check_tensor(w, what, (D,), torch.float32, dev)
+    if workspace is None:
+        workspace = torch.empty(qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D), dtype=torch.uint8, device=dev)
+    _check_workspace(workspace, dev)
+    _call("sage_qk_norm_rope_bwd", dev, *head, _adr(dzq), _adr(dzk), _adr(dq), _adr(dk), _adr(dwq), _adr(dwk), *tail, *st,
+          _adr(workspace), workspace.numel())
+    return dq, dk, dwq, dwk
+
+
+def sage_kv_plan(table, lens, counts, free_pages, n_free, page_size: int, max_tokens: int, out=None):
+    """Pages and slots of a batch's next tokens: request s has lens[s] cached tokens and brings
+    counts[s] (negative: it has ended, and its pages go back).  ``table`` int32 [S, max_pages], ``lens``
+    int32 [S], the stack ``free_pages`` int32 and its height ``n_free`` int32 [1] are brought up to date in
+    place; requests are granted in order as far as pages and ``max_tokens`` go.  Returns (granted [S],
+    starts [S + 1], pos [max_tokens], slots int64 [max_tokens]): the tokens granted, their sums before
+    each request, and each new token's position and slot (0 and -1 behind the last), for
+    sage_qk_norm_rope_fwd and sage_kv_append_slots.  With ``out`` (these four) nothing is allocated."""
+    import torch
+    if table.dim() != 2 or table.numel() == 0 or not table.is_cuda:
+        raise ValueError("table must be a non-empty [S, max_pages] device tensor")
+    S, M = table.shape
+    dev = table.device
+    _check_tensor(table, "table", (S, M), torch.int32, dev)
+    _check_tensor(lens, "lens", (S,), torch.int32, dev)
+    _check_tensor(counts, "counts", (S,), torch.int32, dev)
+    _check_tensor(free_pages, "free_pages", (free_pages.numel(),), torch.int32, dev)
+    _check_tensor(n_free, "n_free", (1,), torch.int32, dev)
+    shapes, types = ((S,), (S + 1,), (max_tokens,), (max_tokens,)), (torch.int32,) * 3 + (torch.int64,)
+    if page_size < 1 or max_tokens < 1 or free_pages.numel() == 0:
+        raise ValueError("page_size, max_tokens and the capacity of free_pages must be at least 1")
+    granted, starts, pos, slots = out if out is not None else [torch.empty(n, dtype=d, device=dev) for n, d in zip(shapes, types)]
+    for t, n, d, what in zip((granted, starts, pos, slots), shapes, types, ("granted", "starts", "pos", "slots")):
+        _check_tensor(t, what, n, d, dev)
+    _call("sage_kv_plan", dev, _adr(table), M, _adr(lens), _adr(counts), _adr(free_pages), free_pages.numel(), _adr(n_free),
+          page_size, _adr(granted), _adr(starts), _adr(pos), _adr(slots), max_tokens, S)
+    return granted, starts, pos, slots
 
 
 def version() -> str:

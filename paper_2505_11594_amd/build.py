@@ -23,7 +23,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsage_mi355x.so")
 SOURCES = ["sage_abi.hip", "quant.hip", "attn_fp4.hip", "attn_bf16.hip", "attn_nv16.hip", "quant_int8.hip",
            "attn_int8.hip", "attn_int8_bwd.hip", "sage_abi_lm.hip", "attn_window.hip", "attn_window_bwd.hip",
-           "attn_decode.hip", "kv_cache.hip"]
+           "attn_decode.hip", "kv_cache.hip", "attn_decode_fp4.hip", "norm_rope.hip", "kv_plan.hip"]
 RATES_LIB = os.path.join(HERE, "libsage_rates.so")
 RATES_SOURCES = ["issue_rates.hip"]
 PROBES_LIB = os.path.join(HERE, "libsage_probes.so")

@@ -29,101 +29,11 @@
 // more for such values, and gives their channels what a sum with them is: an infinity, or
 // NaN.  (A look at the sums per sequence for everyone else.  The same look before the waves'
 // join took 14 registers of the tile loop.)
-#include "lm_args.h"
-#include "mma16.h"
-#include "window.h"
+#include "decode_split.h"
 
 namespace sage {
 
 constexpr int DT = 32;                  // keys per tile
-constexpr int DW = 4;                   // waves per workgroup
-constexpr int DG = 16;                  // query heads per workgroup
-
-__device__ __forceinline__ float max_over_groups(float x) {      // over the lanes l % 16 equal
-  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = smax(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return smax(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-
-// Steps of a sequence.
-__device__ __forceinline__ TileList seq_tiles(const Decode& a, int s, int* n) {
-  *n = cached_len(a.lens[s], a.c.max_pages * a.c.page_size);
-  return decode_tiles(*n, a.window, a.sinks, DT);
-}
-
-// The line of all sequences' steps.  Up to 64 sequences each wave adds up their steps
-// itself, one per lane; of more, line_kernel has left the steps before each in
-// a.before.
-constexpr int LINE = 64;
-struct Line {
-  long long total, share;               // steps in all, and per workgroup
-};
-__device__ __forceinline__ int steps_of_lane(const Decode& a) {
-  const int lane = threadIdx.x & 63;
-  int n;
-  return lane < a.c.S ? cdiv(seq_tiles(a, lane, &n).count, DW) : 0;
-}
-__device__ __forceinline__ int lanes_up_to(int x) {      // inclusive sum over the lanes
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-__device__ __forceinline__ Line steps_line(const Decode& a, int sum) {
-  Line l;
-  l.total = a.before ? a.before[a.c.S] : __shfl(sum, 63, 64);
-  l.share = (l.total + a.nw - 1) / a.nw;
-  return l;
-}
-// The sequence that holds step r < total, and the steps before it (c: this lane's
-// steps, sum: up to it).
-__device__ __forceinline__ int find_step(const Decode& a, int c, int sum, long long r, long long* before) {
-  const int lane = threadIdx.x & 63;
-  if (!a.before) {
-    const int first = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum > r));
-    *before = __shfl(sum - c, first, 64);
-    return first;
-  }
-  // the first s with before[s + 1] > r: 64 places are looked at at a time
-  int lo = 0, len = a.c.S;                               // it is in [lo, lo + len)
-  while (len > 1) {
-    const int step = cdiv(len, 64), s = lo + (lane + 1) * step;   // up to s: before[s] > r?
-    const unsigned long long past = __builtin_amdgcn_ballot_w64(s >= lo + len || a.before[s] > r);
-    const int first = __builtin_ctzll(past);
-    len = imin(step, len - first * step);
-    lo += first * step;
-  }
-  *before = a.before[lo];
-  return lo;
-}
-
-// Steps before each of many sequences, and in all.  One workgroup.
-__global__ __launch_bounds__(1024) void line_kernel(const Decode a) {
-  __shared__ int red[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  long long base = 0;
-  for (int s0 = 0; s0 < a.c.S; s0 += 1024) {
-    int n, c = 0;
-    if (s0 + tid < a.c.S) c = cdiv(seq_tiles(a, s0 + tid, &n).count, DW);
-    const int sum = lanes_up_to(c);
-    __syncthreads();
-    if (lane == 63) red[wave] = sum;
-    __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      if (w < wave) before += red[w];
-      all += red[w];
-    }
-    if (s0 + tid < a.c.S) a.before[s0 + tid] = base + before + sum - c;
-    base += all;
-  }
-  if (tid == 0) a.before[a.c.S] = base;
-}
 
 // 16 int8 codes as 16 values of the type (exact).
 template <bool BF16>
@@ -180,7 +90,7 @@ __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(
   int s = blockIdx.x, mine = 0, upto = 0;
   if (a.nw > 0) {
     if (!a.before) {
-      mine = steps_of_lane(a);
+      mine = steps_of_lane<DT>(a);
       upto = lanes_up_to(mine);
     }
     const Line line = steps_line(a, upto);
@@ -194,7 +104,7 @@ __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(
     // one sequence (or the share's part of it)
     s = __builtin_amdgcn_readfirstlane(s);
     int n;
-    const TileList tl = seq_tiles(a, s, &n);
+    const TileList tl = seq_tiles<DT>(a, s, &n);
     const int steps = cdiv(tl.count, DW);
     const int off = a.nw > 0 ? (int)(r0 - before) : 0;
     const int cnt = a.nw > 0 ? (int)min((long long)(steps - off), r1 - r0) : steps;
@@ -447,57 +357,6 @@ __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(
   }
 }
 
-// Sequences whose steps several workgroups shared: O = sum O_w 2^(m_w - m) / l.
-// One workgroup per (sequence, query head); its waves take every fourth part.
-template <int D, bool BF16>
-__global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) {
-  constexpr int CL = D / 64;                             // channels per lane
-  __shared__ float sums[4][D + 1];
-  const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int mine = a.before ? 0 : steps_of_lane(a), upto = a.before ? 0 : lanes_up_to(mine);
-  const Line line = steps_line(a, upto);
-  const long long before = a.before ? a.before[s] : __shfl(upto - mine, s, 64);
-  const int steps = a.before ? (int)(a.before[s + 1] - before) : __shfl(mine, s, 64);
-  const int w0 = steps > 0 ? (int)(before / line.share) : 0, w1 = steps > 0 ? (int)((before + steps - 1) / line.share) : -1;
-  if (w0 == w1) return;                                  // final already
-  const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
-  // a share's slot 1 if the sequence begins in it, slot 0 if it began before
-  auto at = [&](int w) { return ((size_t)w * 2 + (w == w0 ? 1 : 0)) * a.Hq + h; };
-  float m = -INFINITY, l = 0.0f, x[CL] = {};
-  for (int w = w0 + lane; w <= w1; w += 64) m = smax(m, ml[at(w) * 2]);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) m = smax(m, __shfl_xor(m, d, 64));
-  const float mc = m == -INFINITY ? 0.0f : m;
-#pragma unroll 8
-  for (int w = w0 + wave; w <= w1; w += 4) {
-    const float f = __builtin_amdgcn_exp2f(ml[at(w) * 2] - mc);
-    l += ml[at(w) * 2 + 1] * f;
-    const float* p = a.part + at(w) * D + lane * CL;
-#pragma unroll
-    for (int i = 0; i < CL; ++i) x[i] += __builtin_fabsf(p[i]) < INFINITY ? p[i] * f : p[i];   // (an infinity stays one where f is 0)
-  }
-#pragma unroll
-  for (int i = 0; i < CL; ++i) sums[wave][lane * CL + i] = x[i];
-  if (lane == 0) sums[wave][D] = l;
-  __syncthreads();
-  if (wave > 0) return;
-  l = (sums[0][D] + sums[1][D]) + (sums[2][D] + sums[3][D]);
-  const float l2 = l > 0.0f || l != l ? m + (__builtin_log2f(l) - shift) : -INFINITY;
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-#pragma unroll
-  for (int i = 0; i < CL; ++i) {
-    const int c = lane * CL + i;
-    x[i] = ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])) * inv;
-  }
-  uint16_t* o = (uint16_t*)a.o + ((size_t)s * a.Hq + h) * D + lane * CL;
-  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(o) = pack16<BF16>(x[0], x[1]);
-  else *o = (uint16_t)pack16<BF16>(x[0], 0.0f);
-  if (lane == 0) {
-    if (a.lse) a.lse[(size_t)s * a.Hq + h] = l2 * 0.69314718055994530942f;
-    if (a.lse2) a.lse2[(size_t)s * a.Hq + h] = l2;
-  }
-}
-
 // weights[j] += sum over the group's heads of exp(S - L), four cached tokens per thread.
 // Bound by the scores' bytes, if enough of them are on their way: 48 sequences of up to
 // 8000 tokens, 32 heads (34 MB in all) take 10 us, 18 with a wait for each head's.
@@ -564,7 +423,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.nw > 0 ? a.nw : a.c.S), (unsigned)a.c.Hkv, (unsigned)cdiv(G, DG)), block(64 * DW);
   hipError_t e = hipSuccess;
   if (a.before) {
-    hipLaunchKernelGGL(line_kernel, dim3(1), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(line_kernel<DT>, dim3(1), dim3(1024), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.c.k_scale) hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), grid, block, 0, st, a);
@@ -572,7 +431,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
     const float shift = a.c.k_scale ? 0.0f : kPShift<BF16>;
-    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
+    hipLaunchKernelGGL((join_kernel<D, BF16, DT>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.weights) {

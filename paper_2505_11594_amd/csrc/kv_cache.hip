@@ -1,4 +1,4 @@
-// The paged cache of keys and values: storing new tokens, and shortening cached
+// The paged cache of keys and values: storing new tokens by tables or by slots, and shortening cached
 // sequences to their most attended tokens.  Both move rows; the bytes they read and write
 // bound them, but for the 8-bit append, whose arithmetic does (below).
 #include "lm_args.h"
@@ -95,6 +95,134 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
   if (bf16) { SAGE_APPEND(64, true); }
   SAGE_APPEND(64, false);
 #undef SAGE_APPEND
+}
+
+// The same for a cache in MXFP4, and for every kind of cache where the caller gives each
+// token's slot (page * page_size + its place in the page) in place of tables.  MXFP4 rows:
+// per 32 channels the scale 2^e has the smallest e with 6 * 2^e >= max|x| (phi of the FP4
+// attention), codes are E2M1 of x / 2^e, nearest, ties to even; 4 lanes of 8 channels make
+// a block.  Divisions by numbers that the host knows are multiplications.
+struct Divide {
+  uint32_t mul, shift;
+  int by;
+  // n / by for 0 <= n < 2^31: (n + floor(n mul / 2^32)) >> shift, mul = floor(2^32 (2^shift - by) / by) + 1
+  __device__ __forceinline__ int operator()(int n) const {
+    return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift);
+  }
+};
+static Divide divide_by(int by) {
+  Divide d{0, 0, by};
+  while ((1ull << d.shift) < (uint64_t)by) ++d.shift;
+  d.mul = (uint32_t)((((1ull << d.shift) - (uint64_t)by) << 32) / (uint64_t)by + 1);
+  return d;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float max_dpp(float x) {
+  return __builtin_fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t quantize_fp4(const v4i x, int* scale) {
+  float v[8], amax = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = widen<BF16>((uint16_t)((uint32_t)x[i / 2] >> (16 * (i & 1))));
+    amax = __builtin_fmaxf(amax, __builtin_fabsf(v[i]));
+  }
+  amax = max_dpp<0x4E>(max_dpp<0xB1>(amax));             // lanes ^ 1, ^ 2
+  const int e = e8m0_exponent(amax);
+  const float down = __uint_as_float((uint32_t)(127 - e) << 23);         // 2^-e: e is at most 126 for 16-bit inputs
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= down;
+  uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], 1.0f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], 1.0f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], 1.0f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], 1.0f, 3);
+  *scale = e + 127;
+  return c;
+}
+
+struct Store {
+  Append a;
+  const int64_t* slots;
+  Divide heads_tokens, tokens, page;
+};
+template <int D, bool BF16, int KIND, bool SLOTS>
+__global__ __launch_bounds__(256) void kv_store_kernel(const Store st) {
+  const Append& a = st.a;
+  constexpr int LPR = D / 8;
+  const int ch = threadIdx.x % LPR;
+  const int row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;          // (fewer than 2^28 rows)
+  const int s = st.heads_tokens(row), rest = row - s * st.heads_tokens.by, h = st.tokens(rest), t = rest - h * a.N;
+  if (s >= a.c.S) return;
+  long long page, at = 0;
+  int slot;
+  if constexpr (SLOTS) {
+    const long long x = st.slots[(long long)s * a.N + t];
+    if (x < 0) return;                                   // a row's lanes leave together
+    page = x < (1ll << 31) ? (long long)st.page((int)x) : x / st.page.by;
+    slot = (int)(x - page * st.page.by);
+  } else {
+    const int count = a.counts ? a.counts[s] : a.N;
+    at = (long long)a.pos[s] + t;
+    if (t >= count || at < 0 || at >= (long long)a.c.max_pages * a.c.page_size) return;
+    const int j = st.page((int)at);
+    page = a.c.table[(size_t)s * a.c.max_pages + j];
+    slot = (int)at - j * st.page.by;
+  }
+  if (page < 0 || page >= a.c.pages) return;
+  const uint16_t* k = (const uint16_t*)a.k + (s * a.ks.b + h * a.ks.h + t * a.ks.n) + 8 * ch;
+  const uint16_t* v = (const uint16_t*)a.v + (s * a.vs.b + h * a.vs.h + t * a.vs.n) + 8 * ch;
+  const v4i kx = *reinterpret_cast<const v4i*>(k), vx = *reinterpret_cast<const v4i*>(v);
+  const long long kd = page * a.c.ks.b + h * a.c.ks.h + slot * a.c.ks.n;
+  const long long vd = page * a.c.vs.b + h * a.c.vs.h + slot * a.c.vs.n;
+  const size_t sc = ((size_t)page * a.c.Hkv + h) * st.page.by + slot;
+  if constexpr (KIND == kCacheFp4) {
+    int ke, ve;
+    const uint32_t kc = quantize_fp4<BF16>(kx, &ke), vc = quantize_fp4<BF16>(vx, &ve);
+    *reinterpret_cast<uint32_t*>((uint8_t*)a.c.k + kd + 4 * ch) = kc;
+    *reinterpret_cast<uint32_t*>((uint8_t*)a.c.v + vd + 4 * ch) = vc;
+    if ((ch & 3) == 0) {
+      ((uint8_t*)const_cast<float*>(a.c.k_scale))[sc * (D / 32) + ch / 4] = (uint8_t)ke;
+      ((uint8_t*)const_cast<float*>(a.c.v_scale))[sc * (D / 32) + ch / 4] = (uint8_t)ve;
+    }
+  } else if constexpr (KIND == kCacheInt8) {
+    float x;
+    v2u c;
+    quantize8<D, BF16>(kx, &x, &c);
+    *reinterpret_cast<v2u*>((uint8_t*)a.c.k + kd + 8 * ch) = c;
+    if (ch == 0) const_cast<float*>(a.c.k_scale)[sc] = x;
+    quantize8<D, BF16>(vx, &x, &c);
+    *reinterpret_cast<v2u*>((uint8_t*)a.c.v + vd + 8 * ch) = c;
+    if (ch == 0) const_cast<float*>(a.c.v_scale)[sc] = x;
+  } else {
+    *reinterpret_cast<v4i*>((uint16_t*)a.c.k + kd + 8 * ch) = kx;
+    *reinterpret_cast<v4i*>((uint16_t*)a.c.v + vd + 8 * ch) = vx;
+  }
+  if (!SLOTS && a.weights && ch == 0) a.weights[((size_t)s * a.c.Hkv + h) * a.wstride + at] = 0.0f;
+}
+
+template <int D, bool BF16>
+static void launch_store_t(const Store& s, int kind, dim3 grid, hipStream_t st) {
+  const dim3 block(256);
+  if (!s.slots) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheFp4, false>), grid, block, 0, st, s);
+  else if (kind == kCacheFp4) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheFp4, true>), grid, block, 0, st, s);
+  else if (kind == kCacheInt8) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheInt8, true>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCache16, true>), grid, block, 0, st, s);
+}
+hipError_t launch_kv_store(const Append& a, const int64_t* slots, int D, bool bf16, int kind, hipStream_t st) {
+  const Store s{a, slots, divide_by(a.c.Hkv * a.N), divide_by(a.N), divide_by(a.c.page_size)};
+  const long long rows = (long long)a.c.S * a.c.Hkv * a.N;
+  const int per = 256 / (D / 8);
+  const dim3 grid((unsigned)((rows + per - 1) / per));
+  if (D == 128) {
+    if (bf16) launch_store_t<128, true>(s, kind, grid, st);
+    else launch_store_t<128, false>(s, kind, grid, st);
+  } else {
+    if (bf16) launch_store_t<64, true>(s, kind, grid, st);
+    else launch_store_t<64, false>(s, kind, grid, st);
+  }
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------

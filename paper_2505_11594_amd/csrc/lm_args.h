@@ -40,7 +40,8 @@ size_t window_bwd_part_floats(int B, int Hq, int Hkv, int N, int D, int sinks);
 hipError_t launch_window_bwd(const WindowBwd& a, int D, bool bf16, hipStream_t st);
 
 // A paged cache: pages of page_size tokens, strides in elements; int8 codes with
-// one fp32 scale per token and head ([pages, Hkv, page_size], contiguous) or 16-bit.
+// one fp32 scale per token and head ([pages, Hkv, page_size], contiguous), 16-bit, or
+// MXFP4: strides in bytes, scales are bytes [pages, Hkv, page_size, D / 32].
 struct Cache {
   const void *k, *v;
   const float *k_scale, *v_scale;        // null for a 16-bit cache
@@ -60,6 +61,9 @@ struct Append {
   int N;
 };
 hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st);
+// Every kind of cache, by tables and positions or by slots (int64 [S, N] or null).
+enum { kCache16 = 0, kCacheInt8 = 1, kCacheFp4 = 2 };
+hipError_t launch_kv_store(const Append& a, const int64_t* slots, int D, bool bf16, int kind, hipStream_t st);
 
 struct Decode {
   Cache c;
@@ -81,6 +85,8 @@ int decode_workgroups(int S, int Hq, int Hkv, int capacity);
 size_t decode_line_longs(int S, int Hq, int Hkv, int capacity);
 size_t decode_part_floats(int S, int Hq, int Hkv, int D, int capacity);
 hipError_t launch_paged_decode(const Decode& a, int D, bool bf16, hipStream_t st);
+int decode_fp4_workgroups(int S, int Hq, int Hkv, int capacity);
+hipError_t launch_paged_decode_fp4(const Decode& a, int D, bool bf16, hipStream_t st);
 
 struct Evict {
   Cache c;
@@ -95,5 +101,30 @@ struct Evict {
 };
 size_t evict_hist_ints(int S, int Hkv, int capacity);
 hipError_t launch_kv_evict(const Evict& a, int D, hipStream_t st);
+
+// Norms of queries and keys with their rotation; zq, zk are dq, dk in the backward.
+struct NormRope {
+  const void *q, *k, *gq, *gk;           // gq, gk: gradients of the outputs
+  void *zq, *zk;
+  const float *wq, *wk, *freq;           // wq, wk may be null; freq [R / 2]
+  const int32_t *pos, *lens;             // may be null
+  int B, Hq, Hkv, N, R, pos_each;        // pos [B, N] if pos_each, else [B]: the first token's
+  float eps;
+  Strides qs, ks, zqs, zks, gqs, gks;
+  int split;                             // waves that share a token (the launcher's)
+  float *part, *dwq, *dwk;
+};
+int norm_rope_bwd_blocks(long long tokens, int Hq, int Hkv, int D);
+hipError_t launch_norm_rope(const NormRope& a, int D, bool bf16, bool pairs, bool bwd, hipStream_t st);
+
+// Tables and slots of a batch of requests.
+struct Plan {
+  int32_t *table, *lens, *free_pages, *n_free;       // in and out
+  const int32_t* counts;
+  int32_t *granted, *starts, *pos;
+  int64_t* slots;
+  int S, max_pages, page_size, free_capacity, max_tokens;
+};
+hipError_t launch_kv_plan(const Plan& a, hipStream_t st);
 
 }  // namespace sage

@@ -1,4 +1,5 @@
-// C ABI of the window attention, the paged cache and one-token attention over it.
+// C ABI of the window attention, the norms of queries and keys with their rotation, the
+// paged cache, one-token attention over it, and page tables.
 // Argument checks run on the host before any HIP call; kernels are enqueued on the
 // caller's stream; nothing is allocated.
 #include <algorithm>
@@ -71,18 +72,25 @@ inline void clamp_window(int n, int* window, int* sinks) {
 }
 
 // `written`: rows are stored, so they may not overlap.
-int check_cache(const sage_kv_cache* c, const int32_t* table, int max_pages, int S, bool written) {
-  if (!c || !c->k || !c->v || !table || !aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(table, 4)) return SAGE_ERR_INVALID_ARG;
+int check_pages(const sage_kv_cache* c, bool written, bool fp4) {
+  if (!c || !c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16)) return SAGE_ERR_INVALID_ARG;
   if (!c->k_scale != !c->v_scale || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return SAGE_ERR_INVALID_ARG;
-  if (c->pages <= 0 || c->page_size <= 0 || max_pages <= 0 || S <= 0 || S > kMaxSeqs) return SAGE_ERR_INVALID_ARG;
-  if ((long long)max_pages * c->page_size > kMaxCapacity) return SAGE_ERR_INVALID_ARG;
+  if (fp4 && !c->k_scale) return SAGE_ERR_INVALID_ARG;
+  if (c->pages <= 0 || c->page_size <= 0 || c->page_size > kMaxCapacity) return SAGE_ERR_INVALID_ARG;
   if (check_heads(c->Hkv, c->Hkv, c->D) != SAGE_OK) return SAGE_ERR_INVALID_ARG;
   const int per = c->k_scale ? 16 : 8;
   for (const sage_strides* s : {&c->k_strides, &c->v_strides}) {
     const Strides x{s->b, s->h, s->n};
     if (!strides_ok(x, per, kMaxElems)) return SAGE_ERR_INVALID_ARG;
-    if (written && !distinct_rows(x, c->pages, c->Hkv, c->page_size, c->D)) return SAGE_ERR_INVALID_ARG;
+    if (written && !distinct_rows(x, c->pages, c->Hkv, c->page_size, fp4 ? c->D / 2 : c->D)) return SAGE_ERR_INVALID_ARG;
   }
+  return SAGE_OK;
+}
+int check_cache(const sage_kv_cache* c, const int32_t* table, int max_pages, int S, bool written, bool fp4 = false) {
+  const int rc = check_pages(c, written, fp4);
+  if (rc != SAGE_OK) return rc;
+  if (!table || !aligned(table, 4) || max_pages <= 0 || S <= 0 || S > kMaxSeqs) return SAGE_ERR_INVALID_ARG;
+  if ((long long)max_pages * c->page_size > kMaxCapacity) return SAGE_ERR_INVALID_ARG;
   return SAGE_OK;
 }
 sage::Cache cache_of(const sage_kv_cache* c, const int32_t* table, int max_pages, int S) {
@@ -93,6 +101,38 @@ sage::Cache cache_of(const sage_kv_cache* c, const int32_t* table, int max_pages
   r.pages = c->pages; r.page_size = c->page_size; r.Hkv = c->Hkv;
   r.table = table; r.S = S; r.max_pages = max_pages;
   return r;
+}
+
+// The arguments that norm and rotation share with their backward.
+int check_norm_rope(sage::NormRope& a, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                    const float* inv_freq, int rotary, const int32_t* pos, int pos_per_token, const int32_t* lens, int B, int Hq,
+                    int Hkv, int N, int D, float eps, unsigned flags, const sage_strides* q_strides,
+                    const sage_strides* k_strides) {
+  if (flags & ~(unsigned)(SAGE_IN_BF16 | SAGE_ROPE_PAIRS)) return SAGE_ERR_INVALID_ARG;
+  if (check_heads(Hq, Hkv, D) != SAGE_OK || B <= 0 || N <= 0) return SAGE_ERR_INVALID_ARG;
+  if ((long long)B * N > (1LL << 30) || (long long)B * N * Hq * D > kMaxElems) return SAGE_ERR_INVALID_ARG;
+  if (rotary < 0 || rotary > D || rotary % 8 || (rotary > 0 && !inv_freq) || pos_per_token < 0 || pos_per_token > 1)
+    return SAGE_ERR_INVALID_ARG;
+  if (!(eps >= 0x1p-100f) || !(eps <= 1.0f)) return SAGE_ERR_INVALID_ARG;
+  if (!q || !k || !aligned(q, 16) || !aligned(k, 16)) return SAGE_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)q_weight, (const void*)k_weight, (const void*)inv_freq, (const void*)pos, (const void*)lens})
+    if (!aligned(p, 4)) return SAGE_ERR_INVALID_ARG;
+  a.q = q; a.k = k; a.wq = q_weight; a.wk = k_weight; a.freq = inv_freq; a.pos = pos; a.lens = lens;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.N = N; a.R = rotary; a.pos_each = pos_per_token; a.eps = eps;
+  a.qs = strides_or(q_strides, Hq, N, D); a.ks = strides_or(k_strides, Hkv, N, D);
+  for (const Strides& s : {a.qs, a.ks})
+    if (!strides_ok(s, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
+  return SAGE_OK;
+}
+// Its outputs: rows apart, and each either away from its input or the very same tensor.
+int check_norm_rope_out(sage::NormRope& a, void* zq, void* zk, int D, const sage_strides* zq_strides, const sage_strides* zk_strides) {
+  if (!zq || !zk || !aligned(zq, 16) || !aligned(zk, 16)) return SAGE_ERR_INVALID_ARG;
+  a.zq = zq; a.zk = zk;
+  a.zqs = strides_or(zq_strides, a.Hq, a.N, D); a.zks = strides_or(zk_strides, a.Hkv, a.N, D);
+  for (const Strides& s : {a.zqs, a.zks})
+    if (!strides_ok(s, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
+  if (!distinct_rows(a.zqs, a.B, a.Hq, a.N, D) || !distinct_rows(a.zks, a.B, a.Hkv, a.N, D)) return SAGE_ERR_INVALID_ARG;
+  return SAGE_OK;
 }
 
 struct BwdWs {
@@ -206,8 +246,9 @@ int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, con
                    const sage_strides* v_strides, const int32_t* table, int max_pages, const int32_t* pos,
                    const int32_t* counts, float* weights, int64_t weights_stride, int S, int N, unsigned flags,
                    hipStream_t stream) {
-  if (flags & ~(unsigned)SAGE_IN_BF16) return SAGE_ERR_INVALID_ARG;
-  const int rc = check_cache(cache, table, max_pages, S, true);
+  if (flags & ~(unsigned)(SAGE_IN_BF16 | SAGE_KV_FP4)) return SAGE_ERR_INVALID_ARG;
+  const bool fp4 = (flags & SAGE_KV_FP4) != 0;
+  const int rc = check_cache(cache, table, max_pages, S, true, fp4);
   if (rc != SAGE_OK) return rc;
   if (N <= 0 || (long long)cache->Hkv * N > (1LL << 30) || (long long)S * cache->Hkv * N * cache->D > kMaxElems / 64)
     return SAGE_ERR_INVALID_ARG;
@@ -220,7 +261,28 @@ int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, con
   a.ks = strides_or(k_strides, cache->Hkv, N, cache->D);
   a.vs = strides_or(v_strides, cache->Hkv, N, cache->D);
   if (!strides_ok(a.ks, 8, kMaxElems) || !strides_ok(a.vs, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
+  if (fp4) return hip_status(sage::launch_kv_store(a, nullptr, cache->D, (flags & SAGE_IN_BF16) != 0, sage::kCacheFp4, stream));
   return hip_status(sage::launch_kv_append(a, cache->D, (flags & SAGE_IN_BF16) != 0, stream));
+}
+
+int sage_kv_append_slots(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
+                         const sage_strides* v_strides, const int64_t* slots, int B, int N, unsigned flags, hipStream_t stream) {
+  if (flags & ~(unsigned)(SAGE_IN_BF16 | SAGE_KV_FP4)) return SAGE_ERR_INVALID_ARG;
+  const bool fp4 = (flags & SAGE_KV_FP4) != 0;
+  const int rc = check_pages(cache, true, fp4);
+  if (rc != SAGE_OK) return rc;
+  if (B <= 0 || B > kMaxSeqs || N <= 0 || (long long)cache->Hkv * N > (1LL << 30) ||
+      (long long)B * cache->Hkv * N * cache->D > kMaxElems / 64)
+    return SAGE_ERR_INVALID_ARG;
+  if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return SAGE_ERR_INVALID_ARG;
+  sage::Append a;
+  a.c = cache_of(cache, nullptr, 0, B);
+  a.k = k; a.v = v; a.pos = nullptr; a.counts = nullptr; a.weights = nullptr; a.wstride = 0; a.N = N;
+  a.ks = strides_or(k_strides, cache->Hkv, N, cache->D);
+  a.vs = strides_or(v_strides, cache->Hkv, N, cache->D);
+  if (!strides_ok(a.ks, 8, kMaxElems) || !strides_ok(a.vs, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
+  const int kind = fp4 ? sage::kCacheFp4 : cache->k_scale ? sage::kCacheInt8 : sage::kCache16;
+  return hip_status(sage::launch_kv_store(a, slots, cache->D, (flags & SAGE_IN_BF16) != 0, kind, stream));
 }
 
 size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int max_pages, int page_size, int with_weights) {
@@ -234,8 +296,9 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
                            float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,
                            int sinks, float* weights, int64_t weights_stride, unsigned flags, void* workspace,
                            size_t workspace_bytes, hipStream_t stream) {
-  if (flags & ~(unsigned)SAGE_IN_BF16) return SAGE_ERR_INVALID_ARG;
-  int rc = check_cache(cache, table, max_pages, S, false);
+  if (flags & ~(unsigned)(SAGE_IN_BF16 | SAGE_KV_FP4)) return SAGE_ERR_INVALID_ARG;
+  const bool fp4 = (flags & SAGE_KV_FP4) != 0;
+  int rc = check_cache(cache, table, max_pages, S, false, fp4);
   if (rc != SAGE_OK) return rc;
   rc = check_heads(Hq, cache->Hkv, cache->D);
   if (rc != SAGE_OK) return rc;
@@ -245,6 +308,7 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   if (!strides_ok(Strides{q_stride_s, q_stride_h, 0}, 8, 0)) return SAGE_ERR_INVALID_ARG;
   const int capacity = max_pages * cache->page_size;
   if (weights && weights_stride < capacity) return SAGE_ERR_INVALID_ARG;
+  if (weights && fp4) return SAGE_ERR_UNSUPPORTED;
   const DecodeWs w = decode_ws(S, Hq, cache->Hkv, cache->D, capacity, weights != nullptr);
   if (w.total > 0) {
     if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
@@ -258,13 +322,14 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   a.window = window; a.sinks = sinks;
   clamp_window(capacity, &a.window, &a.sinks);
   a.weights = weights; a.wstride = weights_stride;
-  a.nw = sage::decode_workgroups(S, Hq, cache->Hkv, capacity);
+  a.nw = fp4 ? sage::decode_fp4_workgroups(S, Hq, cache->Hkv, capacity) : sage::decode_workgroups(S, Hq, cache->Hkv, capacity);
   a.c2 = softmax_c2(cache->D);
   a.part = reinterpret_cast<float*>(base + w.part);
-  a.before = w.lse2 > w.line ? reinterpret_cast<long long*>(base + w.line) : nullptr;
+  a.before = a.nw > 0 && w.lse2 > w.line ? reinterpret_cast<long long*>(base + w.line) : nullptr;
   a.lse2 = weights ? reinterpret_cast<float*>(base + w.lse2) : nullptr;
   a.scores = weights ? reinterpret_cast<float*>(base + w.scores) : nullptr;
   a.score_stride = w.score_stride;
+  if (fp4) return hip_status(sage::launch_paged_decode_fp4(a, cache->D, (flags & SAGE_IN_BF16) != 0, stream));
   return hip_status(sage::launch_paged_decode(a, cache->D, (flags & SAGE_IN_BF16) != 0, stream));
 }
 
@@ -304,6 +369,65 @@ int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_page
   a.new_wstride = (long long)new_max_pages * cache->page_size;
   a.new_max_pages = new_max_pages; a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last;
   return hip_status(sage::launch_kv_evict(a, cache->D, stream));
+}
+
+int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
+                          int rotary, const int32_t* pos, int pos_per_token, const int32_t* lens, void* zq, void* zk, int B,
+                          int Hq, int Hkv, int N, int D, float eps, unsigned flags, const sage_strides* q_strides,
+                          const sage_strides* k_strides, const sage_strides* zq_strides, const sage_strides* zk_strides,
+                          hipStream_t stream) {
+  sage::NormRope a{};
+  int rc = check_norm_rope(a, q, k, q_weight, k_weight, inv_freq, rotary, pos, pos_per_token, lens, B, Hq, Hkv, N, D, eps, flags,
+                           q_strides, k_strides);
+  if (rc == SAGE_OK) rc = check_norm_rope_out(a, zq, zk, D, zq_strides, zk_strides);
+  if (rc != SAGE_OK) return rc;
+  return hip_status(sage::launch_norm_rope(a, D, (flags & SAGE_IN_BF16) != 0, (flags & SAGE_ROPE_PAIRS) != 0, false, stream));
+}
+
+size_t sage_qk_norm_rope_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D) {
+  if (check_heads(Hq, Hkv, D) != SAGE_OK || B <= 0 || N <= 0 || (long long)B * N > (1LL << 30)) return 0;
+  return up256((size_t)sage::norm_rope_bwd_blocks((long long)B * N, Hq, Hkv, D) * 2 * D * sizeof(float));
+}
+
+int sage_qk_norm_rope_bwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
+                          int rotary, const int32_t* pos, int pos_per_token, const int32_t* lens, const void* dzq, const void* dzk,
+                          void* dq, void* dk, float* dq_weight, float* dk_weight, int B, int Hq, int Hkv, int N, int D, float eps,
+                          unsigned flags, const sage_strides* q_strides, const sage_strides* k_strides,
+                          const sage_strides* dzq_strides, const sage_strides* dzk_strides, const sage_strides* dq_strides,
+                          const sage_strides* dk_strides, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  sage::NormRope a{};
+  int rc = check_norm_rope(a, q, k, q_weight, k_weight, inv_freq, rotary, pos, pos_per_token, lens, B, Hq, Hkv, N, D, eps, flags,
+                           q_strides, k_strides);
+  if (rc == SAGE_OK) rc = check_norm_rope_out(a, dq, dk, D, dq_strides, dk_strides);
+  if (rc != SAGE_OK) return rc;
+  if (!dzq || !dzk || !aligned(dzq, 16) || !aligned(dzk, 16) || !aligned(dq_weight, 4) || !aligned(dk_weight, 4))
+    return SAGE_ERR_INVALID_ARG;
+  a.gq = dzq; a.gk = dzk; a.dwq = dq_weight; a.dwk = dk_weight;
+  a.gqs = strides_or(dzq_strides, Hq, N, D); a.gks = strides_or(dzk_strides, Hkv, N, D);
+  for (const Strides& s : {a.gqs, a.gks})
+    if (!strides_ok(s, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
+  if (workspace_bytes < sage_qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D)) return SAGE_ERR_WORKSPACE;
+  a.part = static_cast<float*>(workspace);
+  return hip_status(sage::launch_norm_rope(a, D, (flags & SAGE_IN_BF16) != 0, (flags & SAGE_ROPE_PAIRS) != 0, true, stream));
+}
+
+int sage_kv_plan(int32_t* table, int max_pages, int32_t* lens, const int32_t* counts, int32_t* free_pages, int free_capacity,
+                 int32_t* n_free, int page_size, int32_t* granted, int32_t* starts, int32_t* pos, int64_t* slots, int max_tokens,
+                 int S, hipStream_t stream) {
+  if (S <= 0 || S > kMaxSeqs || max_pages <= 0 || page_size <= 0 || (long long)max_pages * page_size > kMaxCapacity)
+    return SAGE_ERR_INVALID_ARG;
+  if (free_capacity <= 0 || max_tokens <= 0 || max_tokens > kMaxCapacity) return SAGE_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)table, (const void*)lens, (const void*)counts, (const void*)free_pages, (const void*)n_free,
+                        (const void*)granted, (const void*)starts, (const void*)pos})
+    if (!p || !aligned(p, 4)) return SAGE_ERR_INVALID_ARG;
+  if (!slots || !aligned(slots, 8)) return SAGE_ERR_INVALID_ARG;
+  if (counts == lens || counts == granted) return SAGE_ERR_INVALID_ARG;
+  sage::Plan a;
+  a.table = table; a.lens = lens; a.free_pages = free_pages; a.n_free = n_free; a.counts = counts;
+  a.granted = granted; a.starts = starts; a.pos = pos; a.slots = slots;
+  a.S = S; a.max_pages = max_pages; a.page_size = page_size; a.free_capacity = free_capacity; a.max_tokens = max_tokens;
+  return hip_status(sage::launch_kv_plan(a, stream));
 }
 
 }  // extern "C"
