@@ -495,8 +495,7 @@ size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int 
  *           weights[s][head][j]; weights_stride >= max_pages * page_size
  *  workspace: at least sage_attn_paged_decode_workspace_size() bytes, 256-byte
  *           aligned (NULL if that is 0)
- * Over an MXFP4 cache weights must be NULL (SAGE_ERR_UNSUPPORTED), and q of a block of 32
- * channels enters with an error of at most 2^-22 (fp16: 2^-26) of the block's largest value.
+ * Over an MXFP4 cache weights must be NULL (SAGE_ERR_UNSUPPORTED).
  */
 int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
                            float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,

@@ -3,14 +3,12 @@
 // and the split are those of attn_decode.hip; what differs is how 4 bits reach the matrix
 // instructions.
 //
-//   S^T (keys x heads) = K . q^T  on v_mfma_scale_f32_16x16x128_f8f6f4: a cached row's
-// codes and scale bytes are its A operand as they lie in memory, 32 channels a lane.  q is
-// the B operand, as a sum of E4M3 parts of 4 bits each with a scale per 32 channels: two
-// hold a bf16 value exactly, three an fp16 value.  (A value below 2^-16 of its block's
-// largest one is off by up to 2^-22 (bf16) or 2^-26 (fp16) of that.)
-//   O^T += V^T . P^T  on v_mfma_f32_16x16x32_bf16: V's scales lie along the keys of this
-// product, so its codes are widened to bf16 with them (exact), two values an instruction,
-// into a wave-private LDS tile that is transposed as it is read.  P enters in two bf16 parts.
+// The codes are widened to bf16 with their scales, two values an instruction and exactly, and
+// both products run on v_mfma_f32_16x16x32_bf16: K's codes go from memory straight into the A
+// operand's registers; V's into a wave-private LDS tile that is transposed as it is read.  q of
+// fp16 enters in two bf16 parts (exact), P in two for either type.
+// (The block-scaled product takes K as it lies in memory, times q in E4M3 parts; its sums of
+// parts that differ in size are off by 2^-18 of their terms, so L was by 8e-5.)
 //
 // A group of up to 4 (8) query heads leaves 12 (8) of the product's 16 columns free: its
 // heads stand there 4 (2) times, and each copy takes the softmax of another 16 (32) of
@@ -23,46 +21,21 @@ namespace {
 
 constexpr int FT = 64;                  // keys per tile
 
-// The exponent (of a float, biased) of the largest of a block of 32 values of q, as E4M3 parts
-// take it: it goes to 2^7, part p's scale byte is be - 7 - 4 p.
+// 8 values of q in bf16: rounded, and of fp16 what the rounding left (11 bits in 8 and 8: exact).
 template <bool BF16>
-__device__ __forceinline__ int block_exponent(const uint16_t* q) {
-  float amax = 0.0f;
+__device__ __forceinline__ void split_q(const uint16_t* q, v4i* hi, v4i* lo) {
+  const v4i v = *reinterpret_cast<const v4i*>(q);
+  if constexpr (BF16) {
+    *hi = v;
+  } else {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const v4i v = *reinterpret_cast<const v4i*>(q + 8 * c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      amax = __builtin_fmaxf(amax, __builtin_fabsf(widen<BF16>((uint16_t)((uint32_t)v[i / 2] >> (16 * (i & 1))))));
-  }
-  return imax((int)(__float_as_uint(amax) >> 23), 20);   // (bytes of the last part stay above 0)
-}
-// 16 values of q as E4M3 parts, the sum of part p * 2^(be - 134 - 4 p).  An infinity becomes NaN.
-template <bool BF16, int PARTS>
-__device__ __forceinline__ void split_q(const uint16_t* q, int be, v4i (&part)[PARTS]) {
-  const float down = __uint_as_float((uint32_t)(261 - be) << 23);
-  float x[16];
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const v4i v = *reinterpret_cast<const v4i*>(q + 8 * c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float y = widen<BF16>((uint16_t)((uint32_t)v[i / 2] >> (16 * (i & 1)))) * down;
-      x[8 * c + i] = __builtin_fmaf(y, 0.0f, y);
+    for (int i = 0; i < 4; ++i) {
+      const float x0 = fp16_to_f32((uint16_t)v[i]), x1 = fp16_to_f32((uint16_t)((uint32_t)v[i] >> 16));
+      const uint32_t h = pack16<true>(x0, x1);
+      (*hi)[i] = (int)h;
+      (*lo)[i] = (int)pack16<true>(x0 - bf16_to_f32((uint16_t)h), x1 - bf16_to_f32((uint16_t)(h >> 16)));
     }
   }
-#pragma unroll
-  for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      int y = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w], x[4 * w + 1], 0, false);
-      y = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * w + 2], x[4 * w + 3], y, true);
-      part[p][w] = y;
-      x[4 * w] = 16.0f * (x[4 * w] - __builtin_amdgcn_cvt_f32_fp8(y, 0));
-      x[4 * w + 1] = 16.0f * (x[4 * w + 1] - __builtin_amdgcn_cvt_f32_fp8(y, 1));
-      x[4 * w + 2] = 16.0f * (x[4 * w + 2] - __builtin_amdgcn_cvt_f32_fp8(y, 2));
-      x[4 * w + 3] = 16.0f * (x[4 * w + 3] - __builtin_amdgcn_cvt_f32_fp8(y, 3));
-    }
 }
 
 // 8 codes as bf16 values times a power of two.
@@ -83,7 +56,7 @@ template <int D, bool BF16, int COPIES>
 __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Decode a) {
   constexpr int ROW = D * 2, SB = D / 32;                // bytes of a V row in LDS; scale bytes of a cached row
   constexpr int HC = 16 / COPIES, TS = 4 / COPIES;       // heads per copy; subtiles of 16 keys whose softmax a copy takes
-  constexpr int PARTS = BF16 ? 2 : 3, NQ = D == 128 ? PARTS : (PARTS + 1) / 2;
+  constexpr int NKS = D / 32;                            // steps of 32 channels of S; lane: 8 channels of each, D / 4 in a row
   constexpr int VL = D / 32, NDB = D / 16;
   constexpr int PADQ = D + 4;
   constexpr int REG = FT * ROW;                          // LDS bytes per wave: V tile, then its O
@@ -113,9 +86,6 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
     s = find_step(a, mine, upto, r0, &before);
   }
   const int ps = a.c.page_size;
-  // K: key 16 t + c16, 32 channels from 32 kb on.  D = 64: blocks 2 and 3 of the product are
-  // the same channels again, times q's second part
-  const int kb = D == 128 ? grp : grp & 1;
   for (;;) {
     // one sequence (or the share's part of it)
     s = __builtin_amdgcn_readfirstlane(s);
@@ -127,29 +97,11 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
     const int tend = imin(tl.count, DW * (off + cnt));
     const int32_t* const table = a.c.table + (size_t)s * a.c.max_pages;
 
-    v8i qreg[NQ];
-    int qscale[NQ];
+    v4i qreg[NKS], qrest[BF16 ? 1 : NKS];                // channels in the order in which K's lie in its registers
     {
-      // FP8 operands hold indices 16 grp .. + 15 and 64 + 16 grp .. + 15, with the scale of 32 grp .. + 31
-      const uint16_t* q = (const uint16_t*)a.q + s * a.q_s + (h0 + imin(head, gn - 1)) * a.q_h;
-      const int be = block_exponent<BF16>(q + 32 * kb);
-      v4i low[PARTS], high[PARTS];
-      split_q<BF16, PARTS>(q + 16 * grp, __shfl(be, c16 + 16 * (grp >> 1), 64), low);
-      if constexpr (D == 128) split_q<BF16, PARTS>(q + 64 + 16 * grp, __shfl(be, c16 + 32 + 16 * (grp >> 1), 64), high);
+      const uint16_t* q = (const uint16_t*)a.q + s * a.q_s + (h0 + imin(head, gn - 1)) * a.q_h + D / 4 * grp;
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        v4i x, y;
-        if constexpr (D == 128) {
-          x = low[i];
-          y = high[i];
-          qscale[i] = be - 7 - 4 * i;
-        } else {                                         // indices from 64 on: the same channels' next part
-          x = low[2 * i];
-          y = 2 * i + 1 < PARTS ? low[(2 * i + 1) % PARTS] : v4i{};
-          qscale[i] = imax(be - 7 - 8 * i - (grp < 2 ? 0 : 4), 0);
-        }
-        qreg[i] = v8i{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-      }
+      for (int j = 0; j < NKS; ++j) split_q<BF16>(q + 8 * j, &qreg[j], &qrest[BF16 ? 0 : j]);
     }
     v4f oacc[NDB];
 #pragma unroll
@@ -164,7 +116,8 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
       return page_ok(id, a.c.pages) ? id : -1;
     };
     struct Rows {
-      v4i k[4], v[VL];
+      int k[4][NKS];                                     // K: key 16 t + c16, channels from D / 4 grp on
+      v4i v[VL];                                         // V: key 64 / VL j + lane / SB, channels from 32 (lane % SB) on
       int ks[4], vs[VL];
     };
     auto load = [&](int i, int id, Rows& r) {
@@ -173,11 +126,13 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int p = __shfl(pid, 16 * t + c16, 64), sl = __shfl(slot, 16 * t + c16, 64);
-        r.k[t] = *reinterpret_cast<const v4i*>((const uint8_t*)a.c.k + (p * a.c.ks.b + hk * a.c.ks.h + sl * a.c.ks.n) + 16 * kb);
-        r.ks[t] = k_scale[(((size_t)p * a.c.Hkv + hk) * ps + sl) * SB + kb];
+        const uint8_t* k = (const uint8_t*)a.c.k + (p * a.c.ks.b + hk * a.c.ks.h + sl * a.c.ks.n) + D / 8 * grp;
+        if constexpr (D == 128) *reinterpret_cast<v4i*>(r.k[t]) = *reinterpret_cast<const v4i*>(k);
+        else *reinterpret_cast<v2u*>(r.k[t]) = *reinterpret_cast<const v2u*>(k);
+        r.ks[t] = k_scale[(((size_t)p * a.c.Hkv + hk) * ps + sl) * SB + D * grp / 128];
       }
 #pragma unroll
-      for (int j = 0; j < VL; ++j) {                     // V: key 64 / VL j + lane / SB, chunk lane % SB
+      for (int j = 0; j < VL; ++j) {
         const int row = 64 / SB * j + lane / SB, ch = lane % SB;
         const int p = __shfl(pid, row, 64), sl = __shfl(slot, row, 64);
         r.v[j] = *reinterpret_cast<const v4i*>((const uint8_t*)a.c.v + (p * a.c.vs.b + hk * a.c.vs.h + sl * a.c.vs.n) + 16 * ch);
@@ -198,11 +153,14 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
       v4f acc[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const v8i k = {cur.k[t][0], cur.k[t][1], cur.k[t][2], cur.k[t][3], 0, 0, 0, 0};
+        const float f = __uint_as_float((uint32_t)cur.ks[t] << 23);
         acc[t] = v4f{};
 #pragma unroll
-        for (int p = NQ - 1; p >= 0; --p)
-          acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, qreg[p], acc[t], 4, 0, 0, cur.ks[t], 0, qscale[p]);
+        for (int j = 0; j < NKS; ++j) {
+          const v4i k = widen_fp4(cur.k[t][j], f);
+          if constexpr (!BF16) acc[t] = mma16<true>(k, qrest[j], acc[t]);
+          acc[t] = mma16<true>(k, qreg[j], acc[t]);
+        }
       }
       float sc[TS][4];
 #pragma unroll

@@ -10,11 +10,6 @@
 //     l supplies row / column l%32 and a contiguous run of the reduction index
 //     at (l/32) times the run length; lane l of the accumulator holds column
 //     l%32 and rows 8g + 4(l/32) + r, g, r in 0..3, at register 4g + r.
-//   - that of v_mfma_scale_f32_16x16x128_f8f6f4 with FP4 and FP8 operands together:
-//     lane l supplies row / column l%16; FP4 in 4 registers, the reduction index
-//     from 32(l/16) on; FP8 in 8, from 16(l/16) on in the first 4 and from 64 + 16(l/16)
-//     on in the others; the E8M0 scale of either is that of the indices from 32(l/16)
-//     on; lane l of the accumulator holds column l%16 and rows 4(l/16) + r.
 // Every kernel is one or a few wave64 workgroups over caller buffers whose
 // sizes the host checks.
 #include <hip/hip_runtime.h>
@@ -103,23 +98,6 @@ __global__ __launch_bounds__(64) void mfma_fp4_kernel(const uint8_t* __restrict_
     for (int r = 0; r < 4; ++r) c[(8 * g + 4 * h + r) * 32 + row] = acc[4 * g + r];
 }
 
-// C[16][16] = A[16][128] B[16][128]^T with A in FP4 codes (packed, 64 bytes a row), B in
-// E4M3 bytes, and one E8M0 scale per row and 32 elements of each; C row-major fp32.
-__global__ __launch_bounds__(64) void mfma_fp4_fp8_kernel(const uint8_t* __restrict__ a, const uint8_t* __restrict__ as,
-                                                          const uint8_t* __restrict__ b, const uint8_t* __restrict__ bs,
-                                                          float* __restrict__ c) {
-  const int l = threadIdx.x, row = l & 15, g = l >> 4;
-  const v4i x = *reinterpret_cast<const v4i*>(a + row * 64 + 16 * g);
-  const v4i y0 = *reinterpret_cast<const v4i*>(b + row * 128 + 16 * g), y1 = *reinterpret_cast<const v4i*>(b + row * 128 + 64 + 16 * g);
-  typedef float v4f __attribute__((ext_vector_type(4)));
-  const v8i A = v8i{x[0], x[1], x[2], x[3], 0, 0, 0, 0}, B = v8i{y0[0], y0[1], y0[2], y0[3], y1[0], y1[1], y1[2], y1[3]};
-  const int sa = as[row * 4 + g], sb = bs[row * 4 + g];
-  v4f acc = v4f{};
-  acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc, 4, 0, 0, sa, 0, sb);
-#pragma unroll
-  for (int r = 0; r < 4; ++r) c[(4 * g + r) * 16 + row] = acc[r];
-}
-
 // C[32][32] = A[32][32] B[32][32]^T, int8 operands, int32 C row-major
 __global__ __launch_bounds__(64) void mfma_i8_kernel(const int8_t* __restrict__ a, const int8_t* __restrict__ b,
                                                      int* __restrict__ c) {
@@ -201,14 +179,6 @@ int sage_probe_mfma_fp4(const uint8_t* a, const uint8_t* as, const uint8_t* b, c
                         hipStream_t stream) {
   if (!a || !as || !b || !bs || !c) return 1;
   hipLaunchKernelGGL(mfma_fp4_kernel, dim3(1), dim3(64), 0, stream, a, as, b, bs, c);
-  return st(hipGetLastError());
-}
-
-// a: 16 x 64 bytes of codes; b: 16 x 128 E4M3 bytes (both 16-byte aligned); as, bs: 16 x 4 E8M0 bytes; c: 16 x 16 fp32
-int sage_probe_mfma_fp4_fp8(const uint8_t* a, const uint8_t* as, const uint8_t* b, const uint8_t* bs, float* c,
-                            hipStream_t stream) {
-  if (!a || !as || !b || !bs || !c || ((uintptr_t)a & 15) || ((uintptr_t)b & 15)) return 1;
-  hipLaunchKernelGGL(mfma_fp4_fp8_kernel, dim3(1), dim3(64), 0, stream, a, as, b, bs, c);
   return st(hipGetLastError());
 }
 

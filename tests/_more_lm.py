@@ -108,11 +108,11 @@ def fp4_values(codes, scale):
 
 
 def fp4_decode(q, kr, vr, has, window, sinks):
-    """As _lm.decode_attention, with this kernel's bounds: q enters in up to 3 parts, whose D products each are
-    added with errors of at most 2 f a step, and P in two bf16 parts (2^-16)."""
+    """As _lm.decode_attention, with this kernel's bounds: an fp16 q enters in two parts, whose D products each are added
+    up, and the scale's product; P in two bf16 parts (2^-16)."""
     D = q.shape[-1]
     r = _lm.decode_attention(q, kr, vr, has, window, sinks)
-    r["e"] = r["e"] * (2 * (3 * D + 8) / (D + 4)) + 2.0 ** -22 * r["e"] / 2.0 ** -24 / (D + 4)
+    r["e"] = r["e"] * (2 * D + 8) / (D + 4)
     return r
 
 
