@@ -556,7 +556,7 @@ int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, c
                           hipStream_t stream);
 
 /* Workspace bytes for sage_qk_norm_rope_bwd (sums for the weights' gradients, at most
- * 2 MB); 0 for invalid arguments.  Host only. */
+ * 1 MB); 0 for invalid arguments.  Host only. */
 size_t sage_qk_norm_rope_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D);
 
 /*

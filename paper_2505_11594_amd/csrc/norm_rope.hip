@@ -110,28 +110,32 @@ __device__ __forceinline__ void turn_row(float* x, const float* cs, const float*
   }
 }
 
-// A wave's token and its angles; false where there is none.
+// A wave's token.
 struct Token {
-  int b, n;
+  int b, n, p;
   bool inside;                                           // not behind the sequence's end
-  float cs[4], sn[4];                                    // of this lane's pairs
 };
-template <int D>
-__device__ __forceinline__ void find_token(const NormRope& a, long long tk, Token& t) {
-  const int lane = threadIdx.x & 63, l = lane % (D / 8);
-  t.b = (int)(tk / a.N);
-  t.n = (int)(tk - (long long)t.b * a.N);
+__device__ __forceinline__ Token find_token(const NormRope& a, int tk) {
+  Token t;
+  t.b = tk / a.N;
+  t.n = tk - t.b * a.N;
   t.inside = !a.lens || t.n < a.lens[t.b];
-  int p = t.n;
-  if (a.pos) p = a.pos_each ? a.pos[tk] : (int)((unsigned)a.pos[t.b] + (unsigned)t.n);
+  t.p = t.n;
+  if (a.pos) t.p = a.pos_each ? a.pos[tk] : (int)((unsigned)a.pos[t.b] + (unsigned)t.n);
+  return t;
+}
+// Cosines and sines of this lane's pairs; freq: inv_freq of pair `lane`.
+template <int D>
+__device__ __forceinline__ void token_angles(const NormRope& a, int p, float freq, float* cs, float* sn) {
+  const int l = (threadIdx.x & 63) % (D / 8);
   float c, s;
-  turn(p, lane < a.R / 2 ? a.freq[lane] : 0.0f, &c, &s);
+  turn(p, freq, &c, &s);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {                          // pair 4 l + j; channels that are not rotated: angle 0
     const int from = 4 * l + j;
-    t.cs[j] = __shfl(c, from & 63, 64);
-    t.sn[j] = __shfl(s, from & 63, 64);
-    if (from >= a.R / 2) { t.cs[j] = 1.0f; t.sn[j] = 0.0f; }
+    cs[j] = __shfl(c, from & 63, 64);
+    sn[j] = __shfl(s, from & 63, 64);
+    if (from >= a.R / 2) { cs[j] = 1.0f; sn[j] = 0.0f; }
   }
 }
 
@@ -143,135 +147,158 @@ __device__ __forceinline__ void load_weight(const float* w, int c0, int c1, floa
   }
 }
 
-constexpr int NU = 4;                                    // row loads in flight per lane
-
-// A token's heads of q or k, those of this wave's part.  One wave step is 512 / D rows.
-template <int D, bool BF16, bool PAIRS>
-__device__ __forceinline__ void fwd_heads(const NormRope& a, const Token& t, const void* x, void* z, const Strides& xs,
-                                          const Strides& zs, int H, int first, const float* w, int c0, int c1) {
-  constexpr int LPR = D / 8, RPW = 64 / LPR;
-  const int rg = (threadIdx.x & 63) / LPR;
-  const uint16_t* src = (const uint16_t*)x + t.b * xs.b + t.n * xs.n;
-  uint16_t* dst = (uint16_t*)z + t.b * zs.b + t.n * zs.n;
-  for (int h0 = first * RPW; h0 < H; h0 += NU * a.split * RPW) {
-    Row8 in[NU];
-    if (t.inside) {
-#pragma unroll
-      for (int u = 0; u < NU; ++u)
-        in[u] = load_row<PAIRS>(src + imin(h0 + u * a.split * RPW + rg, H - 1) * xs.h, c0, c1);
-    }
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      const int h = h0 + u * a.split * RPW + rg;
-      float v[8] = {};
-      if (t.inside) {
-        widen_row<BF16>(in[u], v);
-        float ss = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
-        const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<D>(ss), 1.0f / D, a.eps));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= r * w[i];
-        turn_row<PAIRS, false>(v, t.cs, t.sn);
-      }
-      if (h < H) store_row<PAIRS>(dst + h * zs.h, c0, c1, pack_row<BF16>(v));
-    }
-  }
+// A token's rows, in steps of 512 / D rows that a wave takes at once: first q's, then k's.  A wave
+// whose part of them is `part` of split takes the steps part, part + split, ...
+struct Step {
+  bool q, ok;                                            // ok: this lane has a row (else it holds the last one again)
+  int h;
+};
+template <int D>
+__device__ __forceinline__ Step step_of(const NormRope& a, int i, int sq) {
+  constexpr int RPW = 512 / D;
+  const int rg = (threadIdx.x & 63) / (D / 8);
+  Step s;
+  s.q = i < sq;
+  const int H = s.q ? a.Hq : a.Hkv, h = (s.q ? i : i - sq) * RPW + rg;
+  s.ok = h < H;
+  s.h = imin(h, H - 1);
+  return s;
+}
+__device__ __forceinline__ const uint16_t* row_in(const void* x, const Strides& s, const Token& t, int h) {
+  return (const uint16_t*)x + (t.b * s.b + t.n * s.n) + h * s.h;
+}
+__device__ __forceinline__ uint16_t* row_out(void* x, const Strides& s, const Token& t, int h) {
+  return (uint16_t*)x + (t.b * s.b + t.n * s.n) + h * s.h;
 }
 
+constexpr int NU = 4;                                    // steps whose rows are on their way at a time
 template <int D, bool BF16, bool PAIRS>
 __global__ __launch_bounds__(256) void norm_rope_fwd_kernel(const NormRope a) {
-  constexpr int LPR = D / 8, RPW = 64 / LPR;
-  const int l = threadIdx.x % LPR;
+  constexpr int RPW = 512 / D;
+  const int lane = threadIdx.x & 63, l = lane % (D / 8);
   int c0, c1;
   lane_channels<PAIRS>(l, a.R, &c0, &c1);
   float wq[8], wk[8];
   load_weight(a.wq, c0, c1, wq);
   load_weight(a.wk, c0, c1, wk);
-  const long long tokens = (long long)a.B * a.N;
-  const int sq = cdiv(a.Hq, RPW);
-  for (long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < tokens * a.split;
-       i += (long long)gridDim.x * 4) {
-    const long long tk = i / a.split;
-    const int part = (int)(i - tk * a.split);
-    Token t;
-    find_token<D>(a, tk, t);
-    // steps of q, then of k, dealt out to the token's waves in turn
-    fwd_heads<D, BF16, PAIRS>(a, t, a.q, a.zq, a.qs, a.zqs, a.Hq, part, wq, c0, c1);
-    const int over = sq % a.split;
-    fwd_heads<D, BF16, PAIRS>(a, t, a.k, a.zk, a.ks, a.zks, a.Hkv, part >= over ? part - over : part + a.split - over, wk, c0, c1);
-  }
-}
-
-template <int D, bool BF16, bool PAIRS>
-__device__ __forceinline__ void bwd_heads(const NormRope& a, const Token& t, const void* x, const void* g, void* dx,
-                                          const Strides& xs, const Strides& gs, const Strides& ds, int H, int first,
-                                          const float* w, float* dw, int c0, int c1) {
-  constexpr int LPR = D / 8, RPW = 64 / LPR, U = NU / 2;
-  const int rg = (threadIdx.x & 63) / LPR;
-  const uint16_t* src = (const uint16_t*)x + t.b * xs.b + t.n * xs.n;
-  const uint16_t* gsrc = (const uint16_t*)g + t.b * gs.b + t.n * gs.n;
-  uint16_t* dst = (uint16_t*)dx + t.b * ds.b + t.n * ds.n;
-  for (int h0 = first * RPW; h0 < H; h0 += U * a.split * RPW) {
-    Row8 in[U], gin[U];
-    if (t.inside) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = imin(h0 + u * a.split * RPW + rg, H - 1);
-        in[u] = load_row<PAIRS>(src + h * xs.h, c0, c1);
-        gin[u] = load_row<PAIRS>(gsrc + h * gs.h, c0, c1);
+  const float freq = lane < a.R / 2 ? a.freq[lane] : 0.0f;
+  const int waves = a.B * a.N * a.split, sq = cdiv(a.Hq, RPW), steps = sq + cdiv(a.Hkv, RPW);
+  for (long long wv = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); wv < waves;
+       wv += (long long)gridDim.x * 4) {
+    const int tk = (int)wv / a.split, part = (int)wv - tk * a.split;
+    const Token t = find_token(a, tk);
+    if (!t.inside) {
+      for (int i = part; i < steps; i += a.split) {
+        const Step s = step_of<D>(a, i, sq);
+        if (s.ok) store_row<PAIRS>(row_out(s.q ? a.zq : a.zk, s.q ? a.zqs : a.zks, t, s.h), c0, c1, Row8{});
       }
+      continue;
     }
+    Row8 in[NU];
+    auto load = [&](int i0) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * a.split * RPW + rg;
-      float v[8] = {}, d[8] = {};
-      if (t.inside) {
-        if (h >= H) in[u] = gin[u] = Row8{};             // (a lane without a row holds the last one's)
-        widen_row<BF16>(in[u], v);
-        widen_row<BF16>(gin[u], d);
-        turn_row<PAIRS, true>(d, t.cs, t.sn);
-        float ss = 0.0f, ux = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          ss = __builtin_fmaf(v[i], v[i], ss);
-          ux = __builtin_fmaf(d[i] * w[i], v[i], ux);
+      for (int u = 0; u < NU; ++u)
+        if (i0 + u * a.split < steps) {
+          const Step s = step_of<D>(a, i0 + u * a.split, sq);
+          in[u] = load_row<PAIRS>(row_in(s.q ? a.q : a.k, s.q ? a.qs : a.ks, t, s.h), c0, c1);
         }
+    };
+    load(part);                                          // (the angles are found meanwhile)
+    float cs[4], sn[4];
+    token_angles<D>(a, t.p, freq, cs, sn);
+    for (int i0 = part; i0 < steps; i0 += NU * a.split) {
+      Row8 cur[NU];
+#pragma unroll
+      for (int u = 0; u < NU; ++u) cur[u] = in[u];
+      load(i0 + NU * a.split);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        if (i0 + u * a.split >= steps) break;
+        const Step s = step_of<D>(a, i0 + u * a.split, sq);
+        float v[8], ss = 0.0f;
+        widen_row<BF16>(cur[u], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(v[i], v[i], ss);
         const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<D>(ss), 1.0f / D, a.eps));
-        const float m = row_sum<D>(ux) * (1.0f / D) * r * r;         // mean(u x) r^2
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          dw[i] = __builtin_fmaf(d[i], v[i] * r, dw[i]);
-          d[i] = r * __builtin_fmaf(-m, v[i], d[i] * w[i]);
-        }
+        for (int i = 0; i < 8; ++i) v[i] *= r * (s.q ? wq[i] : wk[i]);
+        turn_row<PAIRS, false>(v, cs, sn);
+        if (s.ok) store_row<PAIRS>(row_out(s.q ? a.zq : a.zk, s.q ? a.zqs : a.zks, t, s.h), c0, c1, pack_row<BF16>(v));
       }
-      if (h < H) store_row<PAIRS>(dst + h * ds.h, c0, c1, pack_row<BF16>(d));
     }
   }
 }
 
 // Gradients of x, and per workgroup the sums for those of the weights: part [workgroups][q, k][D].
+constexpr int BU = 2;
 template <int D, bool BF16, bool PAIRS>
 __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(const NormRope a) {
   constexpr int LPR = D / 8, RPW = 64 / LPR;
   __shared__ float sums[4][2][D];
-  const int lane = threadIdx.x & 63, l = threadIdx.x % LPR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, l = lane % LPR, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int c0, c1;
   lane_channels<PAIRS>(l, a.R, &c0, &c1);
   float wq[8], wk[8], dwq[8] = {}, dwk[8] = {};
   load_weight(a.wq, c0, c1, wq);
   load_weight(a.wk, c0, c1, wk);
-  const long long tokens = (long long)a.B * a.N;
-  const int sq = cdiv(a.Hq, RPW);
-  for (long long i = (long long)blockIdx.x * 4 + wave; i < tokens * a.split; i += (long long)gridDim.x * 4) {
-    const long long tk = i / a.split;
-    const int part = (int)(i - tk * a.split);
-    Token t;
-    find_token<D>(a, tk, t);
-    bwd_heads<D, BF16, PAIRS>(a, t, a.q, a.gq, a.zq, a.qs, a.gqs, a.zqs, a.Hq, part, wq, dwq, c0, c1);
-    const int over = sq % a.split;
-    bwd_heads<D, BF16, PAIRS>(a, t, a.k, a.gk, a.zk, a.ks, a.gks, a.zks, a.Hkv,
-                              part >= over ? part - over : part + a.split - over, wk, dwk, c0, c1);
+  const float freq = lane < a.R / 2 ? a.freq[lane] : 0.0f;
+  const int waves = a.B * a.N * a.split, sq = cdiv(a.Hq, RPW), steps = sq + cdiv(a.Hkv, RPW);
+  for (long long wv = (long long)blockIdx.x * 4 + wave; wv < waves; wv += (long long)gridDim.x * 4) {
+    const int tk = (int)wv / a.split, part = (int)wv - tk * a.split;
+    const Token t = find_token(a, tk);
+    if (!t.inside) {
+      for (int i = part; i < steps; i += a.split) {
+        const Step s = step_of<D>(a, i, sq);
+        if (s.ok) store_row<PAIRS>(row_out(s.q ? a.zq : a.zk, s.q ? a.zqs : a.zks, t, s.h), c0, c1, Row8{});
+      }
+      continue;
+    }
+    Row8 in[BU], gin[BU];
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int u = 0; u < BU; ++u)
+        if (i0 + u * a.split < steps) {
+          const Step s = step_of<D>(a, i0 + u * a.split, sq);
+          in[u] = load_row<PAIRS>(row_in(s.q ? a.q : a.k, s.q ? a.qs : a.ks, t, s.h), c0, c1);
+          gin[u] = load_row<PAIRS>(row_in(s.q ? a.gq : a.gk, s.q ? a.gqs : a.gks, t, s.h), c0, c1);
+        }
+    };
+    load(part);
+    float cs[4], sn[4];
+    token_angles<D>(a, t.p, freq, cs, sn);
+    for (int i0 = part; i0 < steps; i0 += BU * a.split) {
+      Row8 cur[BU], gcur[BU];
+#pragma unroll
+      for (int u = 0; u < BU; ++u) { cur[u] = in[u]; gcur[u] = gin[u]; }
+      load(i0 + BU * a.split);
+#pragma unroll
+      for (int u = 0; u < BU; ++u) {
+        if (i0 + u * a.split >= steps) break;
+        const Step s = step_of<D>(a, i0 + u * a.split, sq);
+        if (!s.ok) cur[u] = gcur[u] = Row8{};            // adds nothing to the weights' gradients
+        float v[8], d[8], ss = 0.0f, ux = 0.0f;
+        widen_row<BF16>(cur[u], v);
+        widen_row<BF16>(gcur[u], d);
+        turn_row<PAIRS, true>(d, cs, sn);
+        const auto rows = [&](const float* w, float* dw) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            ss = __builtin_fmaf(v[i], v[i], ss);
+            ux = __builtin_fmaf(d[i] * w[i], v[i], ux);
+          }
+          const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<D>(ss), 1.0f / D, a.eps));
+          const float m = row_sum<D>(ux) * (1.0f / D) * r * r;       // mean(u x) r^2
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            dw[i] = __builtin_fmaf(d[i], v[i] * r, dw[i]);
+            d[i] = r * __builtin_fmaf(-m, v[i], d[i] * w[i]);
+          }
+        };
+        if (s.q) rows(wq, dwq);
+        else rows(wk, dwk);
+        if (s.ok) store_row<PAIRS>(row_out(s.q ? a.zq : a.zk, s.q ? a.zqs : a.zks, t, s.h), c0, c1, pack_row<BF16>(d));
+      }
+    }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -300,8 +327,13 @@ __global__ __launch_bounds__(1024) void weight_sum_kernel(const float* part, int
   __shared__ float sums[64][17];
   const int c = threadIdx.x & 15, y = threadIdx.x >> 4, at = blockIdx.x * 16 + c;
   float x = 0.0f;
-#pragma unroll 4
-  for (int i = y; i < blocks; i += 64) x += part[(size_t)i * 2 * D + at];
+  for (int i0 = y; i0 < blocks; i0 += 16 * 64) {         // 16 loads on their way
+    float v[16];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) v[u] = part[(size_t)imin(i0 + 64 * u, blocks - 1) * 2 * D + at];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) x += i0 + 64 * u < blocks ? v[u] : 0.0f;
+  }
   sums[y][c] = x;
   __syncthreads();
   for (int o = 32; o >= 1; o >>= 1) {
@@ -320,10 +352,11 @@ static int split_of(long long tokens, int Hq, int Hkv, int D) {
   while (split * 2 <= steps && tokens * split < 8192) split *= 2;
   return split;
 }
-// The backward's workgroups: each leaves a sum of its own, so no more than fill the GPU twice.
+// The backward's workgroups: each leaves a sum of its own, so no more than fill the GPU once (4
+// waves per SIMD).
 int norm_rope_bwd_blocks(long long tokens, int Hq, int Hkv, int D) {
   const long long want = (tokens * split_of(tokens, Hq, Hkv, D) + 3) / 4;
-  return (int)(want < 2048 ? want : 2048);
+  return (int)(want < 1024 ? want : 1024);
 }
 
 template <int D, bool BF16>

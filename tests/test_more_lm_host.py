@@ -62,8 +62,8 @@ def test_norm_rope_backward_refusals(L, bad):
 
 def test_norm_rope_backward_workspace(L):
     need = bd.qk_norm_rope_bwd_workspace_size(2, 4, 2, 16, 128)
-    assert 0 < need <= 2 << 20 and need % 256 == 0
-    assert bd.qk_norm_rope_bwd_workspace_size(1, 64, 8, 1 << 20, 128) <= 2 << 20
+    assert 0 < need <= 1 << 20 and need % 256 == 0
+    assert bd.qk_norm_rope_bwd_workspace_size(1, 64, 8, 1 << 20, 128) <= 1 << 20
     assert rope_bwd(L, size=need - 1) == WORKSPACE
     for bad in ((0, 4, 2, 16, 128), (2, 4, 3, 16, 128), (2, 4, 2, 0, 128), (2, 4, 2, 16, 80), (1 << 15, 4, 2, 1 << 16, 64)):
         assert bd.qk_norm_rope_bwd_workspace_size(*bad) == 0
