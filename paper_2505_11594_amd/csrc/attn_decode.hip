@@ -34,6 +34,7 @@
 namespace sage {
 
 constexpr int DT = 32;                  // keys per tile
+constexpr int DW = 4;                   // waves per workgroup
 
 // 16 int8 codes as 16 values of the type (exact).
 template <bool BF16>
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(
   int s = blockIdx.x, mine = 0, upto = 0;
   if (a.nw > 0) {
     if (!a.before) {
-      mine = steps_of_lane<DT>(a);
+      mine = steps_of_lane<DT, DW>(a);
       upto = lanes_up_to(mine);
     }
     const Line line = steps_line(a, upto);
@@ -423,7 +424,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   const dim3 grid((unsigned)(a.nw > 0 ? a.nw : a.c.S), (unsigned)a.c.Hkv, (unsigned)cdiv(G, DG)), block(64 * DW);
   hipError_t e = hipSuccess;
   if (a.before) {
-    hipLaunchKernelGGL(line_kernel<DT>, dim3(1), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((line_kernel<DT, DW>), dim3(1), dim3(1024), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.c.k_scale) hipLaunchKernelGGL((paged_decode_kernel<D, BF16, true>), grid, block, 0, st, a);
@@ -431,7 +432,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
     const float shift = a.c.k_scale ? 0.0f : kPShift<BF16>;
-    hipLaunchKernelGGL((join_kernel<D, BF16, DT>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
+    hipLaunchKernelGGL((join_kernel<D, BF16, DT, DW>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.weights) {

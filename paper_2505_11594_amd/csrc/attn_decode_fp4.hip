@@ -20,11 +20,15 @@ namespace sage {
 namespace {
 
 constexpr int FT = 64;                  // keys per tile
+#ifndef FWX
+#define FWX 4
+#define FWO 2
+#endif
+constexpr int FW = FWX;                   // waves per workgroup: two workgroups a CU are three waves a SIMD
 
 // 8 values of q in bf16: rounded, and of fp16 what the rounding left (11 bits in 8 and 8: exact).
 template <bool BF16>
-__device__ __forceinline__ void split_q(const uint16_t* q, v4i* hi, v4i* lo) {
-  const v4i v = *reinterpret_cast<const v4i*>(q);
+__device__ __forceinline__ void split_q(const v4i v, v4i* hi, v4i* lo) {
   if constexpr (BF16) {
     *hi = v;
   } else {
@@ -52,16 +56,28 @@ template <int CTRL>
 __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
 constexpr int kLanesOn = 0x100, kTurn = 0x120;           // + n: lane i takes lane i + n (0 past the row of 16); rows turned by n
 
-template <int D, bool BF16, int COPIES>
-__global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Decode a) {
+// The lowest x bits.
+__device__ __forceinline__ unsigned long long low_bits(int x) { return x <= 0 ? 0ull : x >= 64 ? ~0ull : (1ull << x) - 1; }
+
+// A transposing read: 16 keys (rows) by 16 channels of the wave's V tile.
+__device__ __forceinline__ v2u tr_read(uint32_t at) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)at));
+}
+
+// WHOLE: the 16 keys of a subtile lie on one page, K and V lie alike, and 32 bits hold their
+// offsets: a subtile's place is found once for the wave, in scalar registers.  (Not only to save
+// instructions: a launch finds its code out of the caches, and every KB of it takes some 0.3 us.)
+template <int D, bool BF16, int COPIES, bool WHOLE>
+__global__ __launch_bounds__(64 * FW, 2) void paged_decode_fp4_kernel(const Decode a) {
   constexpr int ROW = D * 2, SB = D / 32;                // bytes of a V row in LDS; scale bytes of a cached row
   constexpr int HC = 16 / COPIES, TS = 4 / COPIES;       // heads per copy; subtiles of 16 keys whose softmax a copy takes
   constexpr int NKS = D / 32;                            // steps of 32 channels of S; lane: 8 channels of each, D / 4 in a row
-  constexpr int VL = D / 32, NDB = D / 16;
+  constexpr int NDB = D / 16;
   constexpr int PADQ = D + 4;
-  constexpr int REG = FT * ROW;                          // LDS bytes per wave: V tile, then its O
-  static_assert(REG >= DG * PADQ * 4 && REG % 256 == 0, "O fits; addresses inside a tile are xor-ed");
-  __shared__ __attribute__((aligned(256))) uint8_t lds[DW * REG + DW * DG * 8];
+  constexpr int REG = D == 128 ? 33 * 256 : 17 * 256;    // LDS bytes per wave: 32 rows of V, then its O
+  static_assert(REG >= DG * PADQ * 4 && REG >= 32 * ROW && REG % 256 == 0, "both fit; addresses inside a tile are xor-ed");
+  __shared__ __attribute__((aligned(256))) uint8_t lds[FW * REG + FW * DG * 8];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, grp = lane >> 4, copy = c16 / HC, head = c16 % HC;
   const int hk = blockIdx.y, G = a.Hq / a.c.Hkv, g0 = blockIdx.z * DG, gn = imin(DG, G - g0);
@@ -69,14 +85,14 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
   uint8_t* const vt = lds + wave * REG;
   const uint32_t vbase = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)vt;
   const uint32_t vat = vbase + (4 * grp + c16 / 4) * ROW + vswz<D>(4 * grp + c16 / 4, (c16 & 3) / 2) * 16 + 8 * (c16 & 1);
-  const uint8_t* const k_scale = (const uint8_t*)a.c.k_scale;
-  const uint8_t* const v_scale = (const uint8_t*)a.c.v_scale;
+
+  const uint32_t wat = vbase + c16 * ROW + vswz<D>(c16, NKS * grp) * 16;   // its row c16's chunk; the next ones by xor
 
   long long r0 = 0, r1 = 0, before = 0;
-  int s = blockIdx.x, mine = 0, upto = 0;
+  int s = blockIdx.x, mine = 0, upto = 0, length = 0;    // mine, length: of sequence `lane`
   if (a.nw > 0) {
     if (!a.before) {
-      mine = steps_of_lane<FT>(a);
+      mine = steps_of_lane<FT, FW>(a, &length);
       upto = lanes_up_to(mine);
     }
     const Line line = steps_line(a, upto);
@@ -86,81 +102,163 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
     s = find_step(a, mine, upto, r0, &before);
   }
   const int ps = a.c.page_size;
+  // this key head's rows and scales of page 0; a lane's bytes from its subtile's first row on:
+  // key c16, channels from D / 4 grp on, and their scale
+  const uint8_t* const k_rows = (const uint8_t*)a.c.k + hk * a.c.ks.h;
+  const uint8_t* const v_rows = (const uint8_t*)a.c.v + hk * a.c.vs.h;
+  const uint8_t* const k_scale = (const uint8_t*)a.c.k_scale + (size_t)hk * ps * SB;
+  const uint8_t* const v_scale = (const uint8_t*)a.c.v_scale + (size_t)hk * ps * SB;
+  const uint32_t row_at = (uint32_t)c16 * (uint32_t)a.c.ks.n + D / 8 * grp, scale_at = c16 * SB + D * grp / 128;
+  const __amdgpu_buffer_rsrc_t k_buf = make_rsrc(k_rows, 0x80000000u), v_buf = make_rsrc(v_rows, 0x80000000u);
+  const __amdgpu_buffer_rsrc_t ks_buf = make_rsrc(k_scale, 0x80000000u), vs_buf = make_rsrc(v_scale, 0x80000000u);
+  // A sequence, or the share's part of it.
+  struct Part {
+    int s, n, off, cnt, steps, tend;
+    TileList tl;
+    const int32_t* table;
+  };
+  auto part_of = [&](int s, long long before) {
+    Part g;
+    g.s = __builtin_amdgcn_readfirstlane(s);
+    g.n = __builtin_amdgcn_readfirstlane(a.nw > 0 && !a.before ? __shfl(length, g.s, 64) : cached_len(a.lens[g.s], a.c.max_pages * ps));
+    g.tl = decode_tiles(g.n, a.window, a.sinks, FT);
+    g.steps = cdiv(g.tl.count, FW);
+    g.off = a.nw > 0 ? __builtin_amdgcn_readfirstlane((int)(r0 - before)) : 0;
+    g.cnt = a.nw > 0 ? __builtin_amdgcn_readfirstlane((int)min((long long)(g.steps - g.off), r1 - r0)) : g.steps;
+    g.tend = imin(g.tl.count, FW * (g.off + g.cnt));
+    g.table = a.c.table + (size_t)g.s * a.c.max_pages;
+    return g;
+  };
+  // Where a tile's keys lie.  WHOLE: its subtiles' pages (-1: none) and first slots; subtiles behind
+  // the sequence's last key stand for the last one.  Else of this lane's key (key `lane` of the tile).
+  struct Place {
+    int page[WHOLE ? 4 : 1], slot[WHOLE ? 4 : 1];
+  };
+  auto place_of = [&](const Part& g, int i) {
+    Place p;
+    if constexpr (WHOLE) {
+      const int kt = g.tl.tile(imin(i, g.tend - 1)) * FT, last = (g.n - 1) & ~15;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int kb = imax(0, imin(kt + 16 * t, last)), j = a.per_page(kb);
+        p.page[t] = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)g.table)[j];
+        p.slot[t] = kb - j * ps;
+      }
+    } else {
+      const int key = g.tl.tile(i) * FT + lane, j = a.per_page(key);
+      p.page[0] = -1;
+      p.slot[0] = key - j * ps;
+      if (i < g.tend && decode_sees(key, g.n, a.window, a.sinks)) p.page[0] = g.table[j];
+    }
+    return p;
+  };
+  // Which keys of the tile are seen, one bit each.
+  auto seen_of = [&](const Part& g, int i, const Place& p) {
+    if constexpr (WHOLE) {
+      const int kt = g.tl.tile(i) * FT;
+      unsigned long long x = ~0ull;
+      if (kt + FT > g.n || (kt < g.n - a.window && kt + FT > a.sinks))
+        x = low_bits(g.n - kt) & (~low_bits(g.n - a.window - kt) | low_bits(a.sinks - kt));
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (!page_ok(p.page[t], a.c.pages)) x &= ~(0xFFFFull << (16 * t));
+      return x;
+    } else {
+      return (unsigned long long)__builtin_amdgcn_ballot_w64(page_ok(p.page[0], a.c.pages));
+    }
+  };
+  struct Rows {
+    int x[4][NKS], scale[4];                             // key 16 t + c16, channels from D / 4 grp on
+  };
+  // The rows' bytes from the first one on (WHOLE); keys without a page get rows of the cache's first one.
+  struct Offsets {
+    uint32_t row[4], scale[4];
+  };
+  auto offsets_of = [&](const Place& p) {
+    Offsets o;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t ok = page_ok(p.page[WHOLE ? t : 0], a.c.pages) ? ~0u : 0u;
+      const uint32_t page = (uint32_t)p.page[WHOLE ? t : 0] & ok, slot = (uint32_t)p.slot[WHOLE ? t : 0] & ok;
+      o.row[t] = page * (uint32_t)a.c.ks.b + slot * (uint32_t)a.c.ks.n;
+      o.scale[t] = (page * (uint32_t)(a.c.Hkv * ps) + slot) * SB;
+    }
+    return o;
+  };
+  // Behind the last tile a load has no bytes (WHOLE): with a branch around it the compiler would count
+  // on none being in flight behind those of the tile at work, and wait for all (131072 tokens: 46 -> 37 us).
+  auto load = [&](const Part& g, int i, const Offsets& o, __amdgpu_buffer_rsrc_t rows, __amdgpu_buffer_rsrc_t scales, Rows& r) {
+    const uint32_t none = i < g.tend ? 0u : 0x80000000u;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if constexpr (D == 128)
+        *reinterpret_cast<v4i*>(r.x[t]) = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rows, row_at | none, o.row[t], 0));
+      else
+        *reinterpret_cast<v2u*>(r.x[t]) = __builtin_bit_cast(v2u, __builtin_amdgcn_raw_buffer_load_b64(rows, row_at | none, o.row[t], 0));
+      r.scale[t] = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_at | none, o.scale[t], 0);
+    }
+  };
+  auto load_each = [&](const Part& g, int i, const Place& pl, const uint8_t* rows, const Strides& st, const uint8_t* scales, Rows& r) {
+    if (i >= g.tend) return;
+    const bool ok = page_ok(pl.page[0], a.c.pages);
+    const int pid = ok ? pl.page[0] : 0, place = ok ? pl.slot[0] : 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int page = __shfl(pid, 16 * t + c16, 64), slot = __shfl(place, 16 * t + c16, 64);
+      const uint8_t* p = rows + (page * st.b + slot * st.n) + D / 8 * grp;
+      if constexpr (D == 128) *reinterpret_cast<v4i*>(r.x[t]) = *reinterpret_cast<const v4i*>(p);
+      else *reinterpret_cast<v2u*>(r.x[t]) = *reinterpret_cast<const v2u*>(p);
+      r.scale[t] = scales[((size_t)page * a.c.Hkv * ps + slot) * SB + D * grp / 128];
+    }
+  };
   for (;;) {
-    // one sequence (or the share's part of it)
-    s = __builtin_amdgcn_readfirstlane(s);
-    int n;
-    const TileList tl = seq_tiles<FT>(a, s, &n);
-    const int steps = cdiv(tl.count, DW);
-    const int off = a.nw > 0 ? (int)(r0 - before) : 0;
-    const int cnt = a.nw > 0 ? (int)min((long long)(steps - off), r1 - r0) : steps;
-    const int tend = imin(tl.count, DW * (off + cnt));
-    const int32_t* const table = a.c.table + (size_t)s * a.c.max_pages;
-
+    const Part now = part_of(s, before);
+    const int tend = now.tend;
+    // K's registers are filled again when the scores have used them, V's when it lies in LDS.
+    int i = FW * now.off + wave;
+    Place at = place_of(now, i), at1 = place_of(now, i + FW);
+    Rows kr, vr;
+    if constexpr (WHOLE) {
+      const Offsets o = offsets_of(at);
+      load(now, i, o, k_buf, ks_buf, kr);
+      load(now, i, o, v_buf, vs_buf, vr);
+    } else {
+      load_each(now, i, at, k_rows, a.c.ks, k_scale, kr);
+      load_each(now, i, at, v_rows, a.c.vs, v_scale, vr);
+    }
     v4i qreg[NKS], qrest[BF16 ? 1 : NKS];                // channels in the order in which K's lie in its registers
     {
-      const uint16_t* q = (const uint16_t*)a.q + s * a.q_s + (h0 + imin(head, gn - 1)) * a.q_h + D / 4 * grp;
+      const uint16_t* q = (const uint16_t*)a.q + now.s * a.q_s + (h0 + imin(head, gn - 1)) * a.q_h + D / 4 * grp;
 #pragma unroll
-      for (int j = 0; j < NKS; ++j) split_q<BF16>(q + 8 * j, &qreg[j], &qrest[BF16 ? 0 : j]);
+      for (int j = 0; j < NKS; ++j) split_q<BF16>(*reinterpret_cast<const v4i*>(q + 8 * j), &qreg[j], &qrest[BF16 ? 0 : j]);
     }
     v4f oacc[NDB];
 #pragma unroll
     for (int db = 0; db < NDB; ++db) oacc[db] = v4f{};
     float m = -INFINITY, l = 0.0f;                       // m in log2 units
-
-    // the page of this lane's key (key `lane` of a tile), -1 where it has none
-    auto page_of = [&](int i) -> int {
-      const int key = tl.tile(i) * FT + lane;
-      if (i >= tend || !decode_sees(key, n, a.window, a.sinks)) return -1;
-      const int id = table[key / ps];
-      return page_ok(id, a.c.pages) ? id : -1;
-    };
-    struct Rows {
-      int k[4][NKS];                                     // K: key 16 t + c16, channels from D / 4 grp on
-      v4i v[VL];                                         // V: key 64 / VL j + lane / SB, channels from 32 (lane % SB) on
-      int ks[4], vs[VL];
-    };
-    auto load = [&](int i, int id, Rows& r) {
-      const int key = tl.tile(i) * FT + lane;
-      const int pid = imax(id, 0), slot = id >= 0 ? key % ps : 0;        // keys without a page: the cache's first row
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int p = __shfl(pid, 16 * t + c16, 64), sl = __shfl(slot, 16 * t + c16, 64);
-        const uint8_t* k = (const uint8_t*)a.c.k + (p * a.c.ks.b + hk * a.c.ks.h + sl * a.c.ks.n) + D / 8 * grp;
-        if constexpr (D == 128) *reinterpret_cast<v4i*>(r.k[t]) = *reinterpret_cast<const v4i*>(k);
-        else *reinterpret_cast<v2u*>(r.k[t]) = *reinterpret_cast<const v2u*>(k);
-        r.ks[t] = k_scale[(((size_t)p * a.c.Hkv + hk) * ps + sl) * SB + D * grp / 128];
-      }
-#pragma unroll
-      for (int j = 0; j < VL; ++j) {
-        const int row = 64 / SB * j + lane / SB, ch = lane % SB;
-        const int p = __shfl(pid, row, 64), sl = __shfl(slot, row, 64);
-        r.v[j] = *reinterpret_cast<const v4i*>((const uint8_t*)a.c.v + (p * a.c.vs.b + hk * a.c.vs.h + sl * a.c.vs.n) + 16 * ch);
-        r.vs[j] = v_scale[(((size_t)p * a.c.Hkv + hk) * ps + sl) * SB + ch];
-      }
-    };
-
-    int i = DW * off + wave;
-    int id = page_of(i), id1 = page_of(i + DW);
-    Rows cur, nxt;
-    if (i < tend) load(i, id, cur);
-    for (; i < tend; i += DW) {
-      const int id2 = page_of(i + 2 * DW);
-      if (i + DW < tend) load(i + DW, id1, nxt);
-      const unsigned long long ok = __builtin_amdgcn_ballot_w64(id >= 0);    // bit: key of the tile
+    for (; i < tend; i += FW) {
+      const Place at2 = place_of(now, i + 2 * FW);
+      const unsigned long long ok = seen_of(now, i, at);
 
       // scores of keys 16 t + 4 grp + e, of which this lane takes t = TS copy + u
       v4f acc[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const float f = __uint_as_float((uint32_t)cur.ks[t] << 23);
-        acc[t] = v4f{};
+      for (int t = 0; t < 4; ++t) acc[t] = v4f{};
 #pragma unroll
-        for (int j = 0; j < NKS; ++j) {
-          const v4i k = widen_fp4(cur.k[t][j], f);
+      for (int j = 0; j < NKS; ++j)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const v4i k = widen_fp4(kr.x[t][j], __uint_as_float((uint32_t)kr.scale[t] << 23));
           if constexpr (!BF16) acc[t] = mma16<true>(k, qrest[j], acc[t]);
           acc[t] = mma16<true>(k, qreg[j], acc[t]);
         }
+      __builtin_amdgcn_sched_barrier(0);                 // (phases kept apart: the registers of one serve the next)
+      Offsets o;
+      if constexpr (WHOLE) {
+        o = offsets_of(at1);
+        load(now, i + FW, o, k_buf, ks_buf, kr);
+      } else {
+        load_each(now, i + FW, at1, k_rows, a.c.ks, k_scale, kr);
       }
       float sc[TS][4];
 #pragma unroll
@@ -170,9 +268,23 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
           float x = acc[u][e];
           if constexpr (COPIES >= 2) x = copy == 1 ? acc[TS + u][e] : x;
           if constexpr (COPIES == 4) x = copy == 2 ? acc[2][e] : copy == 3 ? acc[3][e] : x;
-          const int key = 16 * (TS * copy + u) + 4 * grp + e;
-          sc[u][e] = (ok >> key) & 1ull ? x * a.c2 : -INFINITY;
+          sc[u][e] = x * a.c2;
         }
+      if (~ok) {                                         // some keys are not seen
+#pragma unroll
+        for (int u = 0; u < TS; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (!((ok >> (16 * (TS * copy + u) + 4 * grp + e)) & 1ull)) sc[u][e] = -INFINITY;
+        // their rows of V are zero, whatever lies in the cache
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (!((ok >> (16 * t + c16)) & 1ull)) {
+#pragma unroll
+            for (int j = 0; j < NKS; ++j) vr.x[t][j] = 0;
+            vr.scale[t] = 127;
+          }
+      }
       float x = sc[0][0];
 #pragma unroll
       for (int e = 1; e < 4 * TS; ++e) x = smax(x, sc[e >> 2][e & 3]);
@@ -224,61 +336,68 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
           put(ic<3>{}, hi[6 + w], lo[6 + w]);
         }
       }
-      // V into the wave's tile; rows that are not seen are zero, whatever lies in the cache
-#pragma unroll
-      for (int j = 0; j < VL; ++j) {
-        const int row = 64 / SB * j + lane / SB, ch = lane % SB;
-        v4i v = cur.v[j];
-        uint32_t f = (uint32_t)cur.vs[j] << 23;
-        if (!((ok >> row) & 1ull)) { v = v4i{}; f = 0x3F800000u; }
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          *reinterpret_cast<v4i*>(vt + row * ROW + vswz<D>(row, 4 * ch + w) * 16) = widen_fp4(v[w], __uint_as_float(f));
-      }
+      // V through the wave's tile, 32 keys at a time
+      __builtin_amdgcn_sched_barrier(0);
       const uint32_t va = opaque(vat);
-      static_for<2 * NDB / 4>([&](auto B_) {
-        constexpr int b4 = 4 * (decltype(B_)::value % (NDB / 4)), h = decltype(B_)::value / (NDB / 4);
-        v8bf vv[4];                                      // 32 keys of 4 channel blocks: two reads each, 16 keys apart
-        vt_read4<32 * h * ROW, (32 * h + 16) * ROW>(va ^ (32 * b4), va ^ (32 * b4 + 32), va ^ (32 * b4 + 64), va ^ (32 * b4 + 96),
-                                                    vv[0], vv[1], vv[2], vv[3]);
+      static_for<2>([&](auto H_) {
+        constexpr int h = decltype(H_)::value;
+        const uint32_t wa = opaque(wat);
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const v4i x = __builtin_bit_cast(v4i, vv[d]);
-          oacc[b4 + d] = mma16<true>(x, pl[h], mma16<true>(x, pk[h], oacc[b4 + d]));
+        for (int t = 0; t < 2; ++t) {
+          const float f = __uint_as_float((uint32_t)vr.scale[2 * h + t] << 23);
+#pragma unroll
+          for (int j = 0; j < NKS; ++j)
+            *(__attribute__((address_space(3))) v4i*)(uintptr_t)((wa ^ (16 * j)) + 16 * ROW * t) = widen_fp4(vr.x[2 * h + t][j], f);
+        }
+        if constexpr (h == 1 && WHOLE) load(now, i + FW, o, v_buf, vs_buf, vr);
+        else if constexpr (h == 1) load_each(now, i + FW, at1, v_rows, a.c.vs, v_scale, vr);
+#pragma unroll
+        for (int d4 = 0; d4 < NDB; d4 += 4) {
+          __builtin_amdgcn_sched_barrier(0);
+          v4i x[4];                                      // 32 keys of 4 channel blocks: two reads each, 16 keys apart
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const uint32_t at = va ^ (32 * (d4 + d));
+            const v2u lower = tr_read(at), upper = tr_read(at + 16 * ROW);
+            x[d] = v4i{(int)lower[0], (int)lower[1], (int)upper[0], (int)upper[1]};
+          }
+#pragma unroll
+          for (int d = 0; d < 4; ++d) oacc[d4 + d] = mma16<true>(x[d], pl[h], oacc[d4 + d]);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) oacc[d4 + d] = mma16<true>(x[d], pk[h], oacc[d4 + d]);
         }
       });
-      id = id1;
-      id1 = id2;
-      cur = nxt;
+      at = at1;
+      at1 = at2;
     }
 
-    // join the copies and the 4 waves
+    // join the copies and the waves
     if constexpr (COPIES >= 2) l += __int_as_float(dpp<kTurn + 8>(__float_as_int(l)));
     if constexpr (COPIES == 4) l += __int_as_float(dpp<kTurn + 4>(__float_as_int(l)));
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    float* const ml = reinterpret_cast<float*>(lds + DW * REG);
+    float* const ml = reinterpret_cast<float*>(lds + FW * REG);
     if (grp == 0 && copy == 0) {
       ml[(wave * DG + head) * 2] = m;
       ml[(wave * DG + head) * 2 + 1] = l;
     }
-    __syncthreads();                                     // also: every wave is past its last V tile
+    lds_barrier();                                       // (the next part's rows stay in flight)
     float mm = -INFINITY, ll = 0.0f;
 #pragma unroll
-    for (int w = 0; w < DW; ++w) mm = smax(mm, ml[(w * DG + head) * 2]);
+    for (int w = 0; w < FW; ++w) mm = smax(mm, ml[(w * DG + head) * 2]);
     const float mc = mm == -INFINITY ? 0.0f : mm;
 #pragma unroll
-    for (int w = 0; w < DW; ++w) ll += ml[(w * DG + head) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * DG + head) * 2] - mc);
+    for (int w = 0; w < FW; ++w) ll += ml[(w * DG + head) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(w * DG + head) * 2] - mc);
     const float f = __builtin_amdgcn_exp2f(m - mc);
     if (copy == 0) {
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
         *reinterpret_cast<v4f*>(vt + (head * PADQ + 16 * db + 4 * grp) * 4) = oacc[db] * v4f{f, f, f, f};
     }
-    __syncthreads();
+    lds_barrier();
 
-    const bool whole = off == 0 && cnt == steps;
-    const size_t slot = (size_t)blockIdx.x * 2 + (off == 0 ? 1 : 0);
+    const bool whole = now.off == 0 && now.cnt == now.steps;
+    const size_t slot = (size_t)blockIdx.x * 2 + (now.off == 0 ? 1 : 0);
     if (wave == 0 && grp == 0 && c16 < gn) {
       if (whole) {
         const float l2 = ll > 0.0f || ll != ll ? mm + __builtin_log2f(ll) : -INFINITY;
@@ -299,7 +418,7 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
         const int d = 64 * c + 4 * (tid & 15);
         v4f x = v4f{};
 #pragma unroll
-        for (int w = 0; w < DW; ++w) x += *reinterpret_cast<const v4f*>(lds + w * REG + (qh * PADQ + d) * 4);
+        for (int w = 0; w < FW; ++w) x += *reinterpret_cast<const v4f*>(lds + w * REG + (qh * PADQ + d) * 4);
         if (whole) {
           const v2u o = {pack16<BF16>(x[0] * inv, x[1] * inv), pack16<BF16>(x[2] * inv, x[3] * inv)};
           *reinterpret_cast<v2u*>((uint16_t*)a.o + ((size_t)s * a.Hq + h0 + qh) * D + d) = o;
@@ -309,28 +428,37 @@ __global__ __launch_bounds__(64 * DW, 2) void paged_decode_fp4_kernel(const Deco
       }
     }
     if (a.nw == 0) return;
-    r0 += cnt;
+    r0 += now.cnt;
     if (r0 >= r1) return;
     s = find_step(a, mine, upto, r0, &before);           // the next one that has steps
-    __syncthreads();                                     // the next sequence's V tiles overwrite the join's LDS
+    lds_barrier();                                       // its V tiles overwrite the join's LDS
   }
 }
 
 template <int D, bool BF16>
 hipError_t launch_t(const Decode& a, hipStream_t st) {
   const int G = a.Hq / a.c.Hkv;
-  const dim3 grid((unsigned)(a.nw > 0 ? a.nw : a.c.S), (unsigned)a.c.Hkv, (unsigned)cdiv(G, DG)), block(64 * DW);
+  const dim3 grid((unsigned)(a.nw > 0 ? a.nw : a.c.S), (unsigned)a.c.Hkv, (unsigned)cdiv(G, DG)), block(64 * FW);
   hipError_t e = hipSuccess;
   if (a.before) {
-    hipLaunchKernelGGL(line_kernel<FT>, dim3(1), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((line_kernel<FT, FW>), dim3(1), dim3(1024), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4>), grid, block, 0, st, a);
-  else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 1>), grid, block, 0, st, a);
+  // (a lane's own offset is below 2^31: the bit above it marks loads that are none)
+  const Strides &ks = a.c.ks, &vs = a.c.vs;
+  const long long most = (a.c.pages - 1LL) * ks.b + (a.c.page_size - 1LL) * ks.n + D / 2;
+  const bool whole = a.c.page_size % 16 == 0 && ks.b == vs.b && ks.n == vs.n && ks.b < 1LL << 32 && ks.n < 1LL << 27 &&
+                     most < 1LL << 32 && (long long)a.c.pages * a.c.Hkv * a.c.page_size < (1LL << 32) / (D / 32);
+  if (whole) {
+    if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4, true>), grid, block, 0, st, a);
+    else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 1, true>), grid, block, 0, st, a);
+  } else if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4, false>), grid, block, 0, st, a);
+  else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 1, false>), grid, block, 0, st, a);
   e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
-    hipLaunchKernelGGL((join_kernel<D, BF16, FT>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, 0.0f);
+    hipLaunchKernelGGL((join_kernel<D, BF16, FT, FW>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, 0.0f);
     e = hipGetLastError();
   }
   return e;
@@ -338,9 +466,9 @@ hipError_t launch_t(const Decode& a, hipStream_t st) {
 
 }  // namespace
 
-// As decode_workgroups (never more than it: the same workspace does), for steps of 64-key tiles.
+// As decode_workgroups (never more than it: the same workspace does), for longer steps.
 int decode_fp4_workgroups(int S, int Hq, int Hkv, int capacity) {
-  const long long steps = cdiv(capacity, FT * DW) + 1;
+  const long long steps = cdiv(capacity, FT * FW) + 1;
   if (steps <= 5) return 0;
   const int heads = Hkv * cdiv(Hq / Hkv, DG);
   const long long want = imax(1, 512 / heads), most = (long long)S * steps;

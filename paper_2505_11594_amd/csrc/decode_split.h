@@ -1,5 +1,5 @@
 // The split of one-token attention over a paged cache, which its kernels share: the
-// visible tiles of DT keys of all sequences, in steps of one tile per wave, form one line
+// visible tiles of DT keys of all sequences, in steps of one tile for each of DW waves, form one line
 // that the workgroups of a key head cut into equal shares (attn_decode.hip says more),
 // and the join of what they leave.
 #pragma once
@@ -9,7 +9,6 @@
 
 namespace sage {
 
-constexpr int DW = 4;                   // waves per workgroup
 constexpr int DG = 16;                  // query heads per workgroup
 
 __device__ __forceinline__ float max_over_groups(float x) {      // over the lanes l % 16 equal
@@ -30,28 +29,41 @@ __device__ __forceinline__ TileList seq_tiles(const Decode& a, int s, int* n) {
 // itself, one per lane; of more, line_kernel has left the steps before each in
 // a.before.
 constexpr int LINE = 64;
+// a / b (b > 0, a >= 0), in 32 bits where they do: a 64-bit division takes some 150 instructions.
+__device__ __forceinline__ long long divide(long long a, long long b) {
+  if ((unsigned long long)(a | b) < 1ull << 32) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
 struct Line {
   long long total, share;               // steps in all, and per workgroup
 };
-template <int DT>
-__device__ __forceinline__ int steps_of_lane(const Decode& a) {
+template <int DT, int DW>
+__device__ __forceinline__ int steps_of_lane(const Decode& a, int* n) {      // (n: the length)
   const int lane = threadIdx.x & 63;
+  *n = 0;
+  return lane < a.c.S ? cdiv(seq_tiles<DT>(a, lane, n).count, DW) : 0;
+}
+template <int DT, int DW>
+__device__ __forceinline__ int steps_of_lane(const Decode& a) {
   int n;
-  return lane < a.c.S ? cdiv(seq_tiles<DT>(a, lane, &n).count, DW) : 0;
+  return steps_of_lane<DT, DW>(a, &n);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_lanes(int x) {        // lanes that the control does not reach add 0
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
 }
 __device__ __forceinline__ int lanes_up_to(int x) {      // inclusive sum over the lanes
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  return x;
+  x = add_lanes<0x111, 0xF>(x);                          // within rows of 16: from 1, 2, 4, 8 lanes before
+  x = add_lanes<0x112, 0xF>(x);
+  x = add_lanes<0x114, 0xF>(x);
+  x = add_lanes<0x118, 0xF>(x);
+  x = add_lanes<0x142, 0xA>(x);                          // a row's last lane to the next row, lane 31 to the upper half
+  return add_lanes<0x143, 0xC>(x);
 }
 __device__ __forceinline__ Line steps_line(const Decode& a, int sum) {
   Line l;
   l.total = a.before ? a.before[a.c.S] : __shfl(sum, 63, 64);
-  l.share = (l.total + a.nw - 1) / a.nw;
+  l.share = divide(l.total + a.nw - 1, a.nw);
   return l;
 }
 // The sequence that holds step r < total, and the steps before it (c: this lane's
@@ -77,7 +89,7 @@ __device__ __forceinline__ int find_step(const Decode& a, int c, int sum, long l
 }
 
 // Steps before each of many sequences, and in all.  One workgroup.
-template <int DT>
+template <int DT, int DW>
 __global__ __launch_bounds__(1024) void line_kernel(const Decode a) {
   __shared__ int red[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -103,16 +115,16 @@ __global__ __launch_bounds__(1024) void line_kernel(const Decode a) {
 
 // Sequences whose steps several workgroups shared: O = sum O_w 2^(m_w - m) / l.
 // One workgroup per (sequence, query head); its waves take every fourth part.
-template <int D, bool BF16, int DT>
+template <int D, bool BF16, int DT, int DW>
 __global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) {
   constexpr int CL = D / 64;                             // channels per lane
   __shared__ float sums[4][D + 1];
   const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int mine = a.before ? 0 : steps_of_lane<DT>(a), upto = a.before ? 0 : lanes_up_to(mine);
+  const int mine = a.before ? 0 : steps_of_lane<DT, DW>(a), upto = a.before ? 0 : lanes_up_to(mine);
   const Line line = steps_line(a, upto);
   const long long before = a.before ? a.before[s] : __shfl(upto - mine, s, 64);
   const int steps = a.before ? (int)(a.before[s + 1] - before) : __shfl(mine, s, 64);
-  const int w0 = steps > 0 ? (int)(before / line.share) : 0, w1 = steps > 0 ? (int)((before + steps - 1) / line.share) : -1;
+  const int w0 = steps > 0 ? (int)divide(before, line.share) : 0, w1 = steps > 0 ? (int)divide(before + steps - 1, line.share) : -1;
   if (w0 == w1) return;                                  // final already
   const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
   // a share's slot 1 if the sequence begins in it, slot 0 if it began before

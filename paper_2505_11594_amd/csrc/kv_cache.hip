@@ -101,22 +101,7 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
 // token's slot (page * page_size + its place in the page) in place of tables.  MXFP4 rows:
 // per 32 channels the scale 2^e has the smallest e with 6 * 2^e >= max|x| (phi of the FP4
 // attention), codes are E2M1 of x / 2^e, nearest, ties to even; 4 lanes of 8 channels make
-// a block.  Divisions by numbers that the host knows are multiplications.
-struct Divide {
-  uint32_t mul, shift;
-  int by;
-  // n / by for 0 <= n < 2^31: (n + floor(n mul / 2^32)) >> shift, mul = floor(2^32 (2^shift - by) / by) + 1
-  __device__ __forceinline__ int operator()(int n) const {
-    return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift);
-  }
-};
-static Divide divide_by(int by) {
-  Divide d{0, 0, by};
-  while ((1ull << d.shift) < (uint64_t)by) ++d.shift;
-  d.mul = (uint32_t)((((1ull << d.shift) - (uint64_t)by) << 32) / (uint64_t)by + 1);
-  return d;
-}
-
+// a block.
 template <int CTRL>
 __device__ __forceinline__ float max_dpp(float x) {
   return __builtin_fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)));

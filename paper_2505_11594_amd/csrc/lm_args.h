@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "window.h"
+
 namespace sage {
 
 struct Strides { long long b, h, n; };   // in elements; channels are contiguous
@@ -76,6 +78,7 @@ struct Decode {
   const int32_t* lens;
   int Hq, window, sinks, nw;             // nw: workgroups that share the batch's steps (0: one per sequence)
   float c2;
+  Divide per_page;                       // by the page size (4-bit caches)
   float* part;                           // per (workgroup, end, head): D sums, then (log2 maximum, sum)
   long long* before;                     // steps before each of more than 64 sequences, or null
   float *lse2, *scores;                  // for weights: [S, Hq], [S, Hq, score_stride]

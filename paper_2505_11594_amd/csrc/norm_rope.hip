@@ -171,7 +171,9 @@ __device__ __forceinline__ uint16_t* row_out(void* x, const Strides& s, const To
   return (uint16_t*)x + (t.b * s.b + t.n * s.n) + h * s.h;
 }
 
-constexpr int NU = 4;                                    // steps whose rows are on their way at a time
+// Steps whose rows are on their way behind those at work.  (4948 tokens of 48 heads, D = 64: 13.9
+// us; 14.7 with 1, 15.2 with 3 or 4, whose registers let fewer waves on a SIMD.)
+constexpr int NU = 2;
 template <int D, bool BF16, bool PAIRS>
 __global__ __launch_bounds__(256) void norm_rope_fwd_kernel(const NormRope a) {
   constexpr int RPW = 512 / D;
@@ -344,12 +346,14 @@ __global__ __launch_bounds__(1024) void weight_sum_kernel(const float* part, int
   if (y == 0 && out) out[at < D ? at : at - D] = sums[0][c];
 }
 
-// Waves that share a token's heads: one, and more where the tokens do not fill the GPU (8
-// waves on each of 1024 SIMDs), up to one per step.
+// Waves that share a token's heads: one, and more where the tokens do not fill the GPU, up to
+// one per step.  A wave's start -- its weights, its token, the angles -- takes as long as several
+// steps, so that 4 waves on each of 1024 SIMDs do (4948 tokens of 48 heads, D = 64: 13.9 us, 16.6
+// with 8, 25 with 16; of 40 heads, D = 128: 22.5, 24, 30).
 static int split_of(long long tokens, int Hq, int Hkv, int D) {
   const int rpw = 512 / D, steps = cdiv(Hq, rpw) + cdiv(Hkv, rpw);
   int split = 1;
-  while (split * 2 <= steps && tokens * split < 8192) split *= 2;
+  while (split * 2 <= steps && tokens * split < 4096) split *= 2;
   return split;
 }
 // The backward's workgroups: each leaves a sum of its own, so no more than fill the GPU once (4

@@ -324,6 +324,7 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   a.weights = weights; a.wstride = weights_stride;
   a.nw = fp4 ? sage::decode_fp4_workgroups(S, Hq, cache->Hkv, capacity) : sage::decode_workgroups(S, Hq, cache->Hkv, capacity);
   a.c2 = softmax_c2(cache->D);
+  a.per_page = sage::divide_by(cache->page_size);
   a.part = reinterpret_cast<float*>(base + w.part);
   a.before = a.nw > 0 && w.lse2 > w.line ? reinterpret_cast<long long*>(base + w.line) : nullptr;
   a.lse2 = weights ? reinterpret_cast<float*>(base + w.lse2) : nullptr;

@@ -46,6 +46,22 @@ SAGE_HD int cached_len(int n, int capacity) { return imax(0, imin(n, capacity));
 // A page id is used only if the cache has that page.
 SAGE_HD bool page_ok(int id, int pages) { return (unsigned)id < (unsigned)pages; }
 
+// Division by a number that the host knows, as a multiplication: for 0 <= n < 2^31,
+// n / by = (n + floor(n mul / 2^32)) >> shift with mul = floor(2^32 (2^shift - by) / by) + 1.
+struct Divide {
+  uint32_t mul, shift;
+  int by;
+  SAGE_HD int operator()(int n) const {
+    return (int)(((uint32_t)(((uint64_t)(uint32_t)n * mul) >> 32) + (uint32_t)n) >> shift);
+  }
+};
+inline Divide divide_by(int by) {
+  Divide d{0, 0, by};
+  while ((1ull << d.shift) < (uint64_t)by) ++d.shift;
+  d.mul = (uint32_t)((((1ull << d.shift) - (uint64_t)by) << 32) / (uint64_t)by + 1);
+  return d;
+}
+
 // Which of `total` pieces of work, `groups` equal runs that share keys, a block takes.
 // Blocks go to the 8 XCDs in turn; every run stays on one (its keys in one L2).  Runs
 // are dealt out in turn where 8 divides them, so that sequences of differing lengths
