@@ -7,6 +7,7 @@ library has not been built, ``lib()`` raises: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import struct
 
@@ -134,13 +135,18 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
 
+_in_flags = {}
+
+
 def _in_flag(t) -> int:
-    import torch
-    if t.dtype == torch.bfloat16:
-        return SAGE_IN_BF16
-    if t.dtype == torch.float16:
-        return SAGE_IN_FP16
-    raise TypeError("inputs must be bf16 or fp16, got %s" % t.dtype)
+    flag = _in_flags.get(t.dtype)
+    if flag is None:
+        import torch
+        _in_flags.update({torch.bfloat16: SAGE_IN_BF16, torch.float16: SAGE_IN_FP16})
+        if t.dtype not in _in_flags:
+            raise TypeError("inputs must be bf16 or fp16, got %s" % t.dtype)
+        flag = _in_flags[t.dtype]
+    return flag
 
 
 def _shape(t):
@@ -164,7 +170,7 @@ def _check_qkv(q, k, v):
 def _check_tensor(t, what: str, shape, dtype, device):
     """A caller-supplied buffer must match what the kernels will write or read
     (the C ABI receives bare pointers and cannot check it)."""
-    if not t.is_contiguous() or t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s, got %s %s on %s"
                          % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
@@ -416,16 +422,24 @@ def sage_attn_int8_bwd(q, k, v, o, lse, dout, causal: bool = False, flags: int =
 _NO_WINDOW = 2 ** 31 - 1
 
 
+_calls = {}
+
+
 def _call(fn: str, device, *args):
     """The C call on ``device`` and its current stream."""
-    import torch
+    f = _calls.get(fn)
+    if f is None:
+        f = _calls[fn] = getattr(lib(), fn)
+        import torch
+        _calls[""] = torch
+    torch = _calls[""]
     index = device.index
     stream = torch._C._cuda_getCurrentRawStream(index)
     if torch._C._cuda_getDevice() == index:
-        rc = getattr(lib(), fn)(*args, stream)
+        rc = f(*args, stream)
     else:
         with torch.cuda.device(device):
-            rc = getattr(lib(), fn)(*args, stream)
+            rc = f(*args, stream)
     if rc != SAGE_OK:
         raise SageError(fn, rc)
 
@@ -451,7 +465,7 @@ def _rows(t, what: str, ndim: int = 4):
 
 
 def _same(t, like, what: str, shape):
-    if t.dtype != like.dtype or t.device != like.device or t.shape != shape:
+    if t.dtype is not like.dtype or t.shape != shape or t.device != like.device:
         raise ValueError("%s must be a %s tensor of shape %s on %s, got %s %s on %s"
                          % (what, like.dtype, tuple(shape), like.device, t.dtype, tuple(t.shape), t.device))
 
@@ -612,6 +626,7 @@ def sage_kv_append_slots(k, v, k_cache, v_cache, slots, k_scale=None, v_scale=No
     _call("sage_kv_append_slots", dev, c, _adr(k), _adr(v), _strides(*ks), _strides(*vs), _adr(slots), B, N, flags)
 
 
+@functools.lru_cache(maxsize=256)
 def attn_paged_decode_workspace_size(S: int, Hq: int, Hkv: int, D: int, max_pages: int, page_size: int,
                                      weights: bool = False) -> int:
     return int(lib().sage_attn_paged_decode_workspace_size(S, Hq, Hkv, D, max_pages, page_size, int(bool(weights))))
@@ -641,11 +656,16 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
         if kind:
             raise ValueError("weights are not added up over an MXFP4 cache")
         _check_weights(weights, "weights", S, Hkv, M * page, dev)
-    o = torch.empty((S, Hq, D), dtype=q.dtype, device=dev) if out is None else out
-    _check_tensor(o, "out", (S, Hq, D), q.dtype, dev)
+    if out is None:
+        o = q.new_empty((S, Hq, D))
+    else:
+        o = out
+        _check_tensor(o, "out", (S, Hq, D), q.dtype, dev)
     L = None
-    if lse:
-        L = torch.empty((S, Hq), dtype=torch.float32, device=dev) if lse_out is None else lse_out
+    if lse and lse_out is None:
+        L = q.new_empty((S, Hq), dtype=torch.float32)
+    elif lse:
+        L = lse_out
         _check_tensor(L, "lse_out", (S, Hq), torch.float32, dev)
     if workspace is None:
         n = attn_paged_decode_workspace_size(S, Hq, Hkv, D, M, page, weights is not None)
@@ -728,6 +748,17 @@ def _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interle
     return head, (B, Hq, Hkv, N, D, float(eps), flags), [_strides(*qs), _strides(*ks)]
 
 
+def _like(out, tensors, names, strides):
+    """Outputs like tensors: new ones, contiguous (no strides for the C call), or the caller's, checked."""
+    if out is None:
+        strides += [None] * len(tensors)
+        return [t.new_empty(t.shape) for t in tensors]
+    for t, x, what in zip(out, tensors, names):
+        _same(t, x, what, x.shape)
+        strides.append(_strides(*_rows(t, what)))
+    return out
+
+
 def sage_qk_norm_rope_fwd(q, k, q_weight, k_weight, inv_freq, pos=None, lens=None, eps: float = 1e-6,
                           interleaved: bool = False, out=None):
     """Each head's row of q [B, Hq, N, D] and k [B, Hkv, N, D] (16-bit, any strides with contiguous
@@ -740,14 +771,12 @@ def sage_qk_norm_rope_fwd(q, k, q_weight, k_weight, inv_freq, pos=None, lens=Non
     strides, which may be q and k themselves."""
     import torch
     head, tail, st = _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved)
-    zq, zk = out if out is not None else [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k)]
-    for t, x, what in ((zq, q, "out[0]"), (zk, k, "out[1]")):
-        _same(t, q, what, x.shape)
-        st.append(_strides(*_rows(t, what)))
-    _call("sage_qk_norm_rope_fwd", q.device, *head, _adr(zq), _adr(zk), *tail, *st)
+    zq, zk = _like(out, (q, k), ("out[0]", "out[1]"), st)
+    _call("sage_qk_norm_rope_fwd", q.device, *head, zq.data_ptr(), zk.data_ptr(), *tail, *st)
     return zq, zk
 
 
+@functools.lru_cache(maxsize=256)
 def qk_norm_rope_bwd_workspace_size(B: int, Hq: int, Hkv: int, N: int, D: int) -> int:
     return int(lib().sage_qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D))
 
@@ -763,25 +792,22 @@ def sage_qk_norm_rope_bwd(q, k, q_weight, k_weight, inv_freq, dzq, dzk, pos=None
     head, tail, st = _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved)
     B, Hq, Hkv, N, D = tail[:5]
     dev = q.device
-    for t, x, what in ((dzq, q, "dzq"), (dzk, k, "dzk")):
-        _same(t, q, what, x.shape)
-        st.append(_strides(*_rows(t, what)))
+    _like((dzq, dzk), (q, k), ("dzq", "dzk"), st)
     if out is None:
-        dq, dk = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k))
-        dwq, dwk = (torch.empty(D, dtype=torch.float32, device=dev) if w is not None else None for w in (q_weight, k_weight))
+        dwq, dwk = (q.new_empty(D, dtype=torch.float32) if w is not None else None for w in (q_weight, k_weight))
+        dq, dk = _like(None, (q, k), None, st)
     else:
         dq, dk, dwq, dwk = out
-    for t, x, what in ((dq, q, "dq"), (dk, k, "dk")):
-        _same(t, q, what, x.shape)
-        st.append(_strides(*_rows(t, what)))
-    for w, what in ((dwq, "dq_weight"), (dwk, "dk_weight")):
-        if w is not None:
-            _check_tensor(w, what, (D,), torch.float32, dev)
+        _like((dq, dk), (q, k), ("dq", "dk"), st)
+        for w, what in ((dwq, "dq_weight"), (dwk, "dk_weight")):
+            if w is not None:
+                _check_tensor(w, what, (D,), torch.float32, dev)
     if workspace is None:
-        workspace = torch.empty(qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D), dtype=torch.uint8, device=dev)
-    _check_workspace(workspace, dev)
-    _call("sage_qk_norm_rope_bwd", dev, *head, _adr(dzq), _adr(dzk), _adr(dq), _adr(dk), _adr(dwq), _adr(dwk), *tail, *st,
-          _adr(workspace), workspace.numel())
+        workspace = q.new_empty(qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D), dtype=torch.uint8)
+    else:
+        _check_workspace(workspace, dev)
+    _call("sage_qk_norm_rope_bwd", dev, *head, dzq.data_ptr(), dzk.data_ptr(), dq.data_ptr(), dk.data_ptr(), _adr(dwq), _adr(dwk),
+          *tail, *st, workspace.data_ptr(), workspace.numel())
     return dq, dk, dwq, dwk
 
 
@@ -806,9 +832,12 @@ def sage_kv_plan(table, lens, counts, free_pages, n_free, page_size: int, max_to
     shapes, types = ((S,), (S + 1,), (max_tokens,), (max_tokens,)), (torch.int32,) * 3 + (torch.int64,)
     if page_size < 1 or max_tokens < 1 or free_pages.numel() == 0:
         raise ValueError("page_size, max_tokens and the capacity of free_pages must be at least 1")
-    granted, starts, pos, slots = out if out is not None else [torch.empty(n, dtype=d, device=dev) for n, d in zip(shapes, types)]
-    for t, n, d, what in zip((granted, starts, pos, slots), shapes, types, ("granted", "starts", "pos", "slots")):
-        _check_tensor(t, what, n, d, dev)
+    if out is None:
+        granted, starts, pos, slots = [table.new_empty(n, dtype=d) for n, d in zip(shapes, types)]
+    else:
+        granted, starts, pos, slots = out
+        for t, n, d, what in zip(out, shapes, types, ("granted", "starts", "pos", "slots")):
+            _check_tensor(t, what, n, d, dev)
     _call("sage_kv_plan", dev, _adr(table), M, _adr(lens), _adr(counts), _adr(free_pages), free_pages.numel(), _adr(n_free),
           page_size, _adr(granted), _adr(starts), _adr(pos), _adr(slots), max_tokens, S)
     return granted, starts, pos, slots
