@@ -102,29 +102,47 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
 // per 32 channels the scale 2^e has the smallest e with 6 * 2^e >= max|x| (phi of the FP4
 // attention), codes are E2M1 of x / 2^e, nearest, ties to even; 4 lanes of 8 channels make
 // a block.
+typedef uint16_t v2us __attribute__((ext_vector_type(2)));
 template <int CTRL>
-__device__ __forceinline__ float max_dpp(float x) {
-  return __builtin_fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true)));
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
+  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true));
 }
+// 8 values of a block whose 32 are in 4 lanes.  Sizes of 16-bit values are in the order of their
+// bits; the conversion takes pairs of them and the scale's exponent (not that of a scale below
+// 2^-126, which 8 values are multiplied by).
 template <bool BF16>
 __device__ __forceinline__ uint32_t quantize_fp4(const v4i x, int* scale) {
-  float v[8], amax = 0.0f;
+  v2us big = __builtin_bit_cast(v2us, x[0] & 0x7FFF7FFF);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = widen<BF16>((uint16_t)((uint32_t)x[i / 2] >> (16 * (i & 1))));
-    amax = __builtin_fmaxf(amax, __builtin_fabsf(v[i]));
-  }
-  amax = max_dpp<0x4E>(max_dpp<0xB1>(amax));             // lanes ^ 1, ^ 2
-  const int e = e8m0_exponent(amax);
-  const float down = __uint_as_float((uint32_t)(127 - e) << 23);         // 2^-e: e is at most 126 for 16-bit inputs
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] *= down;
-  uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], 1.0f, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], 1.0f, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], 1.0f, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], 1.0f, 3);
+  for (int i = 1; i < 4; ++i) big = __builtin_elementwise_max(big, __builtin_bit_cast(v2us, x[i] & 0x7FFF7FFF));
+  const uint32_t top = max_dpp<0x4E>(max_dpp<0xB1>(max((uint32_t)big[0], (uint32_t)big[1])));     // lanes ^ 1, ^ 2
+  const int e = e8m0_exponent(widen<BF16>((uint16_t)top));
   *scale = e + 127;
-  return c;
+  uint32_t c = 0;
+  if (BF16 && e == -127) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = widen<BF16>((uint16_t)((uint32_t)x[i / 2] >> (16 * (i & 1)))) * 0x1p127f;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], 1.0f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], 1.0f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], 1.0f, 3);
+  }
+  const float f = __uint_as_float((uint32_t)imax(e + 127, 1) << 23);      // (fp16: -127 is a block of zeros)
+  const int x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];  // (a bit cast of a vector's element would take the first one's)
+  if constexpr (BF16) {
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(v2b, x0), f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(v2b, x1), f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(v2b, x2), f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(v2b, x3), f, 3);
+  } else {
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(v2h, x0), f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(v2h, x1), f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(v2h, x2), f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(v2h, x3), f, 3);
+  }
 }
 
 struct Store {
@@ -132,33 +150,48 @@ struct Store {
   const int64_t* slots;
   Divide heads_tokens, tokens, page;
 };
-template <int D, bool BF16, int KIND, bool SLOTS>
+// TILED: a workgroup's rows are tokens of one sequence and head.
+template <int D, bool BF16, int KIND, bool SLOTS, bool TILED>
 __global__ __launch_bounds__(256) void kv_store_kernel(const Store st) {
   const Append& a = st.a;
   constexpr int LPR = D / 8;
   const int ch = threadIdx.x % LPR;
-  const int row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;          // (fewer than 2^28 rows)
-  const int s = st.heads_tokens(row), rest = row - s * st.heads_tokens.by, h = st.tokens(rest), t = rest - h * a.N;
-  if (s >= a.c.S) return;
-  long long page, at = 0;
-  int slot;
+  int s, h, t;
+  if constexpr (TILED) {
+    s = blockIdx.z;
+    h = blockIdx.y;
+    t = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    if (t >= a.N) return;
+  } else {
+    const int row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;        // (fewer than 2^28 rows)
+    s = st.heads_tokens(row);
+    const int rest = row - s * st.heads_tokens.by;
+    h = st.tokens(rest);
+    t = rest - h * a.N;
+    if (s >= a.c.S) return;
+  }
+  long long page = 0, at = 0, where = 0;
   if constexpr (SLOTS) {
-    const long long x = st.slots[(long long)s * a.N + t];
-    if (x < 0) return;                                   // a row's lanes leave together
-    page = x < (1ll << 31) ? (long long)st.page((int)x) : x / st.page.by;
-    slot = (int)(x - page * st.page.by);
+    where = st.slots[(long long)s * a.N + t];
   } else {
     const int count = a.counts ? a.counts[s] : a.N;
     at = (long long)a.pos[s] + t;
     if (t >= count || at < 0 || at >= (long long)a.c.max_pages * a.c.page_size) return;
-    const int j = st.page((int)at);
-    page = a.c.table[(size_t)s * a.c.max_pages + j];
-    slot = (int)at - j * st.page.by;
+    page = a.c.table[(size_t)s * a.c.max_pages + st.page((int)at)];
   }
-  if (page < 0 || page >= a.c.pages) return;
+  // (the rows are on their way while their place is looked up)
   const uint16_t* k = (const uint16_t*)a.k + (s * a.ks.b + h * a.ks.h + t * a.ks.n) + 8 * ch;
   const uint16_t* v = (const uint16_t*)a.v + (s * a.vs.b + h * a.vs.h + t * a.vs.n) + 8 * ch;
   const v4i kx = *reinterpret_cast<const v4i*>(k), vx = *reinterpret_cast<const v4i*>(v);
+  int slot;
+  if constexpr (SLOTS) {
+    if (where < 0) return;                               // a row's lanes leave together
+    page = where < (1ll << 31) ? (long long)st.page((int)where) : where / st.page.by;
+    slot = (int)(where - page * st.page.by);
+  } else {
+    slot = (int)at - st.page((int)at) * st.page.by;
+  }
+  if (page < 0 || page >= a.c.pages) return;
   const long long kd = page * a.c.ks.b + h * a.c.ks.h + slot * a.c.ks.n;
   const long long vd = page * a.c.vs.b + h * a.c.vs.h + slot * a.c.vs.n;
   const size_t sc = ((size_t)page * a.c.Hkv + h) * st.page.by + slot;
@@ -187,25 +220,33 @@ __global__ __launch_bounds__(256) void kv_store_kernel(const Store st) {
   if (!SLOTS && a.weights && ch == 0) a.weights[((size_t)s * a.c.Hkv + h) * a.wstride + at] = 0.0f;
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool TILED>
 static void launch_store_t(const Store& s, int kind, dim3 grid, hipStream_t st) {
   const dim3 block(256);
-  if (!s.slots) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheFp4, false>), grid, block, 0, st, s);
-  else if (kind == kCacheFp4) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheFp4, true>), grid, block, 0, st, s);
-  else if (kind == kCacheInt8) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheInt8, true>), grid, block, 0, st, s);
-  else hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCache16, true>), grid, block, 0, st, s);
+  if (!s.slots) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheFp4, false, TILED>), grid, block, 0, st, s);
+  else if (kind == kCacheFp4) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheFp4, true, TILED>), grid, block, 0, st, s);
+  else if (kind == kCacheInt8) hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCacheInt8, true, TILED>), grid, block, 0, st, s);
+  else hipLaunchKernelGGL((kv_store_kernel<D, BF16, kCache16, true, TILED>), grid, block, 0, st, s);
+}
+// Rows in tiles, unless a sequence and head has too few of them for one.
+template <int D, bool BF16>
+static void launch_store(const Store& s, int kind, hipStream_t st) {
+  const int per = 256 / (D / 8);
+  if (s.a.N >= per) {
+    launch_store_t<D, BF16, true>(s, kind, dim3((unsigned)cdiv(s.a.N, per), (unsigned)s.a.c.Hkv, (unsigned)s.a.c.S), st);
+  } else {
+    const long long rows = (long long)s.a.c.S * s.a.c.Hkv * s.a.N;
+    launch_store_t<D, BF16, false>(s, kind, dim3((unsigned)((rows + per - 1) / per)), st);
+  }
 }
 hipError_t launch_kv_store(const Append& a, const int64_t* slots, int D, bool bf16, int kind, hipStream_t st) {
   const Store s{a, slots, divide_by(a.c.Hkv * a.N), divide_by(a.N), divide_by(a.c.page_size)};
-  const long long rows = (long long)a.c.S * a.c.Hkv * a.N;
-  const int per = 256 / (D / 8);
-  const dim3 grid((unsigned)((rows + per - 1) / per));
   if (D == 128) {
-    if (bf16) launch_store_t<128, true>(s, kind, grid, st);
-    else launch_store_t<128, false>(s, kind, grid, st);
+    if (bf16) launch_store<128, true>(s, kind, st);
+    else launch_store<128, false>(s, kind, st);
   } else {
-    if (bf16) launch_store_t<64, true>(s, kind, grid, st);
-    else launch_store_t<64, false>(s, kind, grid, st);
+    if (bf16) launch_store<64, true>(s, kind, st);
+    else launch_store<64, false>(s, kind, st);
   }
   return hipGetLastError();
 }
