@@ -65,8 +65,8 @@ __device__ __forceinline__ v2u tr_read(uint32_t at) {
   return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)at));
 }
 
-// WHOLE: the 16 keys of a subtile lie on one page, K and V lie alike, and 32 bits hold their
-// offsets: a subtile's place is found once for the wave, in scalar registers.  (Not only to save
+// WHOLE: the 16 keys of a subtile lie on one page, K and V lie alike, and each has at most
+// 2^31 bytes: a subtile's place is found once for the wave, in scalar registers.  (Not only to save
 // instructions: a launch finds its code out of the caches, and every KB of it takes some 0.3 us.)
 template <int D, bool BF16, int COPIES, bool WHOLE>
 __global__ __launch_bounds__(64 * FW, 2) void paged_decode_fp4_kernel(const Decode a) {
@@ -444,11 +444,11 @@ hipError_t launch_t(const Decode& a, hipStream_t st) {
     hipLaunchKernelGGL((line_kernel<FT, FW>), dim3(1), dim3(1024), 0, st, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  // (a lane's own offset is below 2^31: the bit above it marks loads that are none)
+  // (the buffers' bounds, 2^31 bytes, hold for a load's whole offset; a lane's own of 2^31 marks one that is none)
   const Strides &ks = a.c.ks, &vs = a.c.vs;
-  const long long most = (a.c.pages - 1LL) * ks.b + (a.c.page_size - 1LL) * ks.n + D / 2;
-  const bool whole = a.c.page_size % 16 == 0 && ks.b == vs.b && ks.n == vs.n && ks.b < 1LL << 32 && ks.n < 1LL << 27 &&
-                     most < 1LL << 32 && (long long)a.c.pages * a.c.Hkv * a.c.page_size < (1LL << 32) / (D / 32);
+  const double most = (a.c.pages - 1.0) * ks.b + (a.c.page_size - 1.0) * ks.n + D / 2, rows = (double)a.c.pages * a.c.Hkv * a.c.page_size;
+  const bool whole = a.c.page_size % 16 == 0 && ks.b == vs.b && ks.n == vs.n && ks.n < 1LL << 27 && most <= 0x1p31 &&
+                     rows * (D / 32) <= 0x1p31;
   if (whole) {
     if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4, true>), grid, block, 0, st, a);
     else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2, true>), grid, block, 0, st, a);

@@ -250,6 +250,45 @@ def test_paged_decode_fp4(case):
     assert torch.equal(o, o2) and none is None
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_paged_decode_fp4_layouts(D):
+    """K and V of differing strides, and pages of 16-token multiples or not, give the same; a captured call follows
+    the lengths and tables."""
+    import torch
+    g = gen(31)
+    lens = [1500, 33, 700]
+    c, table, _ = fp4_cache(g, 3, 2, 48, D, lens)
+    q = (0.5 * randn(g, 3, 10, D)).to(torch.bfloat16)
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    kw = dict(window=900, sinks=3, k_scale=c["k_scale"], v_scale=c["v_scale"])
+    o, lse = bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], table, ln, **kw)
+    check_decode(q, c, table, lens, 900, 3, o, lse, "pages of 48, D %d" % D)
+    other = c["v_cache"].transpose(1, 2).contiguous().transpose(1, 2)
+    again = bd.sage_attn_paged_decode(q, c["k_cache"], other, table, ln, **kw)
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+    # pages of 24: each of the 48 cut into two
+    cut = {x: t.unflatten(2, (2, 24)).transpose(1, 2).flatten(0, 1).contiguous() for x, t in c.items()}
+    halves = torch.stack([2 * table, 2 * table + 1], -1).flatten(1).contiguous()
+    again = bd.sage_attn_paged_decode(q, cut["k_cache"], cut["v_cache"], halves, ln, window=900, sinks=3, k_scale=cut["k_scale"],
+                                      v_scale=cut["v_scale"])
+    assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], table, ln, **kw)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], table, ln, **kw)
+    for new in ([1500, 33, 700], [0, 1536, 48], [64, 65, 1000], [1, 0, 0]):
+        ln.copy_(torch.tensor(new, dtype=torch.int32))
+        table.copy_(table.flip(0))
+        graph.replay()
+        want = bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], table, ln, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(held[0], want[0]) and torch.equal(held[1], want[1])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_paged_decode_fp4_wide_scales_and_large_q(D, dtype):
@@ -389,8 +428,9 @@ def test_append_by_slots_equals_append_by_tables(dtype, D, page, N, flat, kind):
         assert c[x] is None or torch.equal(c[x], other[x]), x
 
 
-def test_fp4_caches_beyond_32_bit_offsets():
-    """Pages behind 2^32 bytes of the cache and 2^31 slots: stored and read as in a small one."""
+@pytest.mark.parametrize("gib", [1, 3, 4])
+def test_fp4_caches_beyond_32_bit_offsets(gib):
+    """Pages behind 2^30, 2^31 and 2^32 bytes of the cache: stored and read as in a small one."""
     import torch
     g = gen(51)
     S, Hkv, page, D, lens = 2, 16, 256, 128, [1700, 513]
@@ -398,7 +438,7 @@ def test_fp4_caches_beyond_32_bit_offsets():
     q = (0.5 * randn(g, S, 32, D)).to(torch.bfloat16)
     ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
     kn, vn = (randn(g, S, Hkv, 1, D).to(torch.bfloat16) for _ in range(2))
-    P, n = len(c["k_cache"]), 2 ** 32 // (Hkv * page * D // 2)
+    P, n = len(c["k_cache"]), gib * 2 ** 30 // (Hkv * page * D // 2)
     big = {}
     for x, t in c.items():                               # the same pages, n places further on
         big[x] = torch.zeros((n + P,) + tuple(t.shape[1:]), dtype=torch.uint8, device="cuda")
@@ -413,7 +453,12 @@ def test_fp4_caches_beyond_32_bit_offsets():
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(*outs))
     assert all(torch.equal(big[x][n:], c[x]) for x in c)
-    # slots past 2^31: pages of few bytes
+
+
+def test_append_by_slots_past_32_bits():
+    """Slots past 2^31: pages of few bytes."""
+    import torch
+    g = gen(52)
     k1, v1 = (torch.zeros((2 ** 21 + 2, 1, 1024, 32), dtype=torch.uint8, device="cuda") for _ in range(2))
     s1, s2 = (torch.zeros((2 ** 21 + 2, 1, 1024, 2), dtype=torch.uint8, device="cuda") for _ in range(2))
     x = randn(g, 1, 1, 2, 64).to(torch.bfloat16)
@@ -616,6 +661,39 @@ def test_training_step_captured_with_window_attention():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
     assert not torch.equal(alive[0], want[0])
+
+
+def test_norm_rope_beyond_2_31_elements():
+    """Tensors and strides past 2^31 elements: as the same rows in a small one."""
+    import torch
+    g = gen(61)
+    N, D = 3, 128
+    w, inv = 1 + 0.1 * randn(g, D), torch.rand(64, generator=g, device="cuda")
+    big = torch.zeros((2 ** 31 // D + 64, D), dtype=torch.bfloat16, device="cuda")
+    far = 2 ** 31 // D                                   # rows of head 1
+    q = big.as_strided((1, 2, N, D), (0, far * D, D, 1))
+    q.copy_(randn(g, 1, 2, N, D))
+    k = randn(g, 1, 1, N, D).to(torch.bfloat16)
+    dq, dk = randn(g, 1, 2, N, D).to(torch.bfloat16), randn(g, 1, 1, N, D).to(torch.bfloat16)
+    want = bd.sage_qk_norm_rope_fwd(q.contiguous(), k, w, w, inv)
+    got = bd.sage_qk_norm_rope_fwd(q, k, w, w, inv)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    want = bd.sage_qk_norm_rope_bwd(q.contiguous(), k, w, w, inv, dq, dk)
+    got = bd.sage_qk_norm_rope_bwd(q, k, w, w, inv, dq, dk)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    bd.sage_qk_norm_rope_bwd(q, k, w, w, inv, dq, dk, out=(q, k.clone(), None, None))
+    assert torch.equal(q, want[0])
+    # many tokens: more rows than 2^31 elements hold
+    B, N = 9, 1 << 21
+    x = torch.empty((B, 1, N, D), dtype=torch.bfloat16, device="cuda")
+    for b in range(B):
+        x[b] = randn(g, 1, N, D)
+    lens = torch.tensor([N, 0, N, 5, N, N, 1, N, N - 1], dtype=torch.int32, device="cuda")
+    z, zk = bd.sage_qk_norm_rope_fwd(x, x[:, :, :], w, w, inv, lens=lens)
+    for b in (0, 1, 3, 8):
+        part = bd.sage_qk_norm_rope_fwd(x[b:b + 1, :, -64:], x[b:b + 1, :, -64:], w, w, inv, pos=torch.tensor([N - 64], dtype=torch.int32, device="cuda"))
+        n = max(0, min(64, int(lens[b]) - (N - 64)))
+        assert torch.equal(z[b, 0, -64:][:n], part[0][0, 0, :n]) and bool((zk[b, 0, -64:][n:] == 0).all())
 
 
 def test_norm_rope_backward_of_two_streams_at_once():
