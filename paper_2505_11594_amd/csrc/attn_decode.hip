@@ -358,6 +358,57 @@ __global__ __launch_bounds__(64 * DW, D == 64 ? 3 : 2) void paged_decode_kernel(
   }
 }
 
+// Sequences whose steps several workgroups shared: O = sum O_w 2^(m_w - m) / l.
+// One workgroup per (sequence, query head); its waves take every fourth part.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void join_kernel(const Decode a, float shift) {
+  constexpr int CL = D / 64;                             // channels per lane
+  __shared__ float sums[4][D + 1];
+  const int s = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int mine = a.before ? 0 : steps_of_lane<DT, DW>(a), upto = a.before ? 0 : lanes_up_to(mine);
+  const Line line = steps_line(a, upto);
+  const long long before = a.before ? a.before[s] : __shfl(upto - mine, s, 64);
+  const int steps = a.before ? (int)(a.before[s + 1] - before) : __shfl(mine, s, 64);
+  const int w0 = steps > 0 ? (int)divide(before, line.share) : 0, w1 = steps > 0 ? (int)divide(before + steps - 1, line.share) : -1;
+  if (w0 == w1) return;                                  // final already
+  const float* ml = a.part + (size_t)a.nw * 2 * a.Hq * D;
+  // a share's slot 1 if the sequence begins in it, slot 0 if it began before
+  auto at = [&](int w) { return ((size_t)w * 2 + (w == w0 ? 1 : 0)) * a.Hq + h; };
+  float m = -INFINITY, l = 0.0f, x[CL] = {};
+  for (int w = w0 + lane; w <= w1; w += 64) m = smax(m, ml[at(w) * 2]);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) m = smax(m, __shfl_xor(m, d, 64));
+  const float mc = m == -INFINITY ? 0.0f : m;
+#pragma unroll 8
+  for (int w = w0 + wave; w <= w1; w += 4) {
+    const float f = __builtin_amdgcn_exp2f(ml[at(w) * 2] - mc);
+    l += ml[at(w) * 2 + 1] * f;
+    const float* p = a.part + at(w) * D + lane * CL;
+#pragma unroll
+    for (int i = 0; i < CL; ++i) x[i] += __builtin_fabsf(p[i]) < INFINITY ? p[i] * f : p[i];   // (an infinity stays one where f is 0)
+  }
+#pragma unroll
+  for (int i = 0; i < CL; ++i) sums[wave][lane * CL + i] = x[i];
+  if (lane == 0) sums[wave][D] = l;
+  __syncthreads();
+  if (wave > 0) return;
+  l = (sums[0][D] + sums[1][D]) + (sums[2][D] + sums[3][D]);
+  const float l2 = l > 0.0f || l != l ? m + (__builtin_log2f(l) - shift) : -INFINITY;
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+#pragma unroll
+  for (int i = 0; i < CL; ++i) {
+    const int c = lane * CL + i;
+    x[i] = ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])) * inv;
+  }
+  uint16_t* o = (uint16_t*)a.o + ((size_t)s * a.Hq + h) * D + lane * CL;
+  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(o) = pack16<BF16>(x[0], x[1]);
+  else *o = (uint16_t)pack16<BF16>(x[0], 0.0f);
+  if (lane == 0) {
+    if (a.lse) a.lse[(size_t)s * a.Hq + h] = l2 * 0.69314718055994530942f;
+    if (a.lse2) a.lse2[(size_t)s * a.Hq + h] = l2;
+  }
+}
+
 // weights[j] += sum over the group's heads of exp(S - L), four cached tokens per thread.
 // Bound by the scores' bytes, if enough of them are on their way: 48 sequences of up to
 // 8000 tokens, 32 heads (34 MB in all) take 10 us, 18 with a wait for each head's.
@@ -432,7 +483,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
   e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
     const float shift = a.c.k_scale ? 0.0f : kPShift<BF16>;
-    hipLaunchKernelGGL((join_kernel<D, BF16, DT, DW>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
+    hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.weights) {
