@@ -101,7 +101,8 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
 // token's slot (page * page_size + its place in the page) in place of tables.  MXFP4 rows:
 // per 32 channels the scale 2^e has the smallest e with 6 * 2^e >= max|x| (phi of the FP4
 // attention), codes are E2M1 of x / 2^e, nearest, ties to even; 4 lanes of 8 channels make
-// a block.
+// a block.  (4 sequences of up to 4096 tokens, 8 heads: 13.3 us, 4.3 TB/s, VALU busy 43%; 14.2 with
+// values widened before their conversion, divisions per row and loads behind the look-up.)
 typedef uint16_t v2us __attribute__((ext_vector_type(2)));
 template <int CTRL>
 __device__ __forceinline__ uint32_t max_dpp(uint32_t x) {

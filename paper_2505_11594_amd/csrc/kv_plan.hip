@@ -1,7 +1,8 @@
 // Page tables and slots of a batch of requests, from their lengths: pages of requests that
 // have ended go back on the stack of free pages, requests that bring tokens take theirs from
 // it, and every new token gets its position and its slot in the cache.  Whole numbers
-// only; what it takes is the way through memory and the launches.
+// only; what it takes is the way through memory and the launches: 7 us for the next step of 256
+// requests of 8000 cached tokens, 26 of them ended; 6 + 4 us for 64 prompts of up to 2000 tokens.
 //
 // Requests are granted in their order: with A and C the sums of the pages and tokens asked
 // for up to a request, its own among them (by requests that cannot fit their row of the table:
@@ -70,7 +71,8 @@ __device__ __forceinline__ void store_token(const Plan& a, long long i, int at, 
 // What it takes is latency: loads that wait for one another, barriers.  So a thread loads its
 // request once for both passes (where one thread has one), and the page that its next token may
 // go to before it is known whether it does; and where no request brings more than DIRECT pages or
-// tokens -- every batch that generates -- it writes them itself, without the search.
+// tokens -- every batch that generates -- it writes them itself, without the search.  (256 requests:
+// 27 us with 64-bit scans through shuffles, every request loaded twice, and searches.)
 constexpr int DIRECT = 2;
 template <bool INLINE>
 __global__ __launch_bounds__(PT) void plan_kernel(const Plan a) {

@@ -7,7 +7,9 @@
 //
 // D / 8 lanes hold a row, 8 channels each: four whole pairs, so nothing is exchanged but the
 // sums.  A wave takes a token (or a part of its heads): its lanes find the token's angles
-// once, one each, for all of its rows.  The bytes bound it.
+// once, one each, for all of its rows.  The bytes bound it: 32768 tokens of 32 / 8 heads, D = 128,
+// take 133 us, 5.05 TB/s (a large copy: 5.27); 8192 tokens 34 us, their backward 51 and 4.8 for the
+// weights' sums (VALU busy half of the time in all three).
 //
 // Angles: p f in 64 bits (a position has up to 31 bits, f 24: 53 keep the product's
 // fraction of a turn to 2^-22 of one at the farthest), reduced there to an eighth of a turn

@@ -540,6 +540,55 @@ def test_plan_odd_states():
                 assert (got is not None) and (a.cpu().numpy() == b).all(), (counts, n_free, T)
 
 
+def test_binding_refuses_mismatched_tensors():
+    """Every check of the binding that a bare pointer cannot carry; nothing is launched, nothing changes."""
+    import torch
+    g = gen(1)
+    q, k = randn(g, 2, 8, 5, 64).to(torch.bfloat16), randn(g, 2, 2, 5, 64).to(torch.bfloat16)
+    w, inv, z = torch.ones(64, device="cuda"), torch.ones(32, device="cuda"), torch.zeros
+    i32 = dict(dtype=torch.int32, device="cuda")
+    fwd = lambda q=q, k=k, qw=w, kw=w, inv=inv, **a: bd.sage_qk_norm_rope_fwd(q, k, qw, kw, inv, **a)
+    for bad in (dict(k=k[:, :, :4]), dict(k=k.half()), dict(k=randn(g, 2, 3, 5, 64).to(torch.bfloat16)), dict(qw=w[:32]), dict(kw=w.half()),
+                dict(qw=w.cpu()), dict(inv=torch.ones(33, device="cuda")), dict(inv=torch.ones(30, device="cuda")), dict(inv=torch.ones(36, device="cuda")),
+                dict(pos=z(2, 4, **i32)), dict(pos=z(3, **i32)), dict(pos=z(2, dtype=torch.int64, device="cuda")), dict(lens=z(3, **i32)), dict(eps=0.0),
+                dict(eps=2.0), dict(q=q.transpose(-1, -2).contiguous().transpose(-1, -2)), dict(out=(q, k.half())), dict(out=(q[:, :4], k))):
+        with pytest.raises(ValueError):
+            fwd(**bad)
+    bwd = lambda dq=q, dk=k, **a: bd.sage_qk_norm_rope_bwd(q, k, w, w, inv, dq, dk, **a)
+    for bad in (dict(dq=q[:1]), dict(dk=k.float()), dict(out=(q, k, w[:3], w)), dict(out=(q, q, w, w)), dict(workspace=z(10, device="cuda"))):
+        with pytest.raises(ValueError):
+            bwd(**bad)
+    with pytest.raises(bd.SageError):
+        bwd(workspace=z(256, dtype=torch.uint8, device="cuda"))
+    c, table, _ = fp4_cache(g, 2, 2, 16, 64, [40, 40])
+    ln, slots = torch.full((2,), 40, **i32), z((2, 5), dtype=torch.int64, device="cuda")
+    before = {x: t.clone() for x, t in c.items()}
+    sc = dict(k_scale=c["k_scale"], v_scale=c["v_scale"])
+    put = lambda k=k, v=k, kc=c["k_cache"], vc=c["v_cache"], s=slots, **a: bd.sage_kv_append_slots(k, v, kc, vc, s, **(a or sc))
+    short = dict(k_scale=c["k_scale"][..., :1].contiguous(), v_scale=c["v_scale"])
+    for bad in (dict(k=k[:, :1]), dict(v=k[:1]), dict(s=slots[:1]), dict(s=slots.int()), dict(kc=c["k_cache"][..., :16]), dict(vc=c["v_cache"].to(torch.int8)),
+                dict(k_scale=None, v_scale=c["v_scale"]), short, dict(k_scale=c["k_scale"].float(), v_scale=c["v_scale"].float())):
+        with pytest.raises(ValueError):
+            put(**bad)
+    one = q[:, :, 0]
+    for call in (lambda: bd.sage_attn_paged_decode(one, c["k_cache"], c["v_cache"], table, ln, weights=z((2, 2, 64), device="cuda"), **sc),
+                 lambda: bd.sage_attn_paged_decode(one[..., :32], c["k_cache"], c["v_cache"], table, ln, **sc),
+                 lambda: bd.sage_attn_paged_decode(one, c["k_cache"], c["v_cache"], table, ln),
+                 lambda: bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, ln, z((2, 2, 64), device="cuda"), table.clone(), 16, **sc)):
+        with pytest.raises(ValueError):
+            call()
+    counts, free, n = torch.ones(2, **i32), z(8, **i32), z(1, **i32)
+    for bad in ((table.long(), ln, counts, free, n, 16, 8), (table, ln[:1], counts, free, n, 16, 8), (table, ln, counts.float(), free, n, 16, 8),
+                (table, ln, counts, free.long(), n, 16, 8), (table, ln, counts, free, z(2, **i32), 16, 8), (table, ln, counts, free, n, 0, 8),
+                (table, ln, counts, free, n, 16, 0), (table, ln, counts, free[:0], n, 16, 8)):
+        with pytest.raises(ValueError):
+            bd.sage_kv_plan(*bad)
+    with pytest.raises(ValueError):
+        bd.sage_kv_plan(table, ln, counts, free, n, 16, 8, out=(counts, counts, counts, counts))
+    torch.cuda.synchronize()
+    assert all(torch.equal(c[x], before[x]) for x in c)
+
+
 # ---------------------------------------------------------------- together
 def step_of(st, kind):
     """One step of a batch that generates: pages and slots, norms and rotation, storing, attention."""

@@ -24,10 +24,10 @@ def P():
 
 
 def test_cvt_bf16_fp4_takes_the_exponent_of_its_scale(P):
-    """All codes by all scale bytes 1 to 253 as exponents of a float, exact in bf16."""
+    """All codes by all scale bytes 0 to 253 as exponents of a float (0: 2^-127, no zero), exact in bf16."""
     import torch
-    codes = np.tile(np.arange(256, dtype=np.uint8), 253)
-    e = np.repeat(np.arange(1, 254, dtype=np.int64), 256)
+    codes = np.tile(np.arange(256, dtype=np.uint8), 254)
+    e = np.repeat(np.arange(254, dtype=np.int64), 256)
     c, s = torch.from_numpy(codes).cuda(), torch.from_numpy((e << 23).astype(np.int32)).cuda().view(torch.float32)
     y = torch.zeros(len(codes), dtype=torch.int32, device="cuda")
     assert P.sage_probe_cvt_bf16_fp4(c.data_ptr(), s.data_ptr(), y.data_ptr(), len(codes), None) == 0
