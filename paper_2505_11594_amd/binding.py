@@ -170,7 +170,7 @@ def _check_qkv(q, k, v):
 def _check_tensor(t, what: str, shape, dtype, device):
     """A caller-supplied buffer must match what the kernels will write or read
     (the C ABI receives bare pointers and cannot check it)."""
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device.index or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s, got %s %s on %s"
                          % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
 
@@ -455,17 +455,24 @@ def _rows(t, what: str, ndim: int = 4):
     if len(n) != ndim or not t.is_cuda or 0 in n:
         raise ValueError("%s must be a non-empty %d-d device tensor, got shape %s on %s"
                          % (what, ndim, tuple(n), t.device))
-    x = s[0] if n[0] > 1 else 0
-    y = s[1] if n[1] > 1 else 0
-    z = s[2] if ndim == 4 and n[2] > 1 else 0
-    if s[-1] != 1 or t.data_ptr() & 15 or (x | y | z) & (16 // t.element_size() - 1):
+    if ndim == 4:
+        x, y, z, c = s
+        if n[2] == 1:
+            z = 0
+    else:
+        (x, y, c), z = s, 0
+    if n[0] == 1:
+        x = 0
+    if n[1] == 1:
+        y = 0
+    if c != 1 or t.data_ptr() & 15 or (x | y | z) & (16 // t.itemsize - 1):
         raise ValueError("%s must have contiguous channels and rows on 16-byte addresses, got strides %s"
                          % (what, tuple(s)))
     return (x, y, z) if ndim == 4 else (x, y)
 
 
 def _same(t, like, what: str, shape):
-    if t.dtype is not like.dtype or t.shape != shape or t.device != like.device:
+    if t.dtype is not like.dtype or t.shape != shape or t.get_device() != like.get_device():
         raise ValueError("%s must be a %s tensor of shape %s on %s, got %s %s on %s"
                          % (what, like.dtype, tuple(shape), like.device, t.dtype, tuple(t.shape), t.device))
 
@@ -720,32 +727,43 @@ def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int
 
 
 # ------------------------------------------------- norms with rotation, page tables
+_F32 = _I32 = None
+
+
 def _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved):
     """What forward and backward share: the C arguments up to lens, (B, Hq, Hkv, N, D), eps and flags, and the
     strides of q and k."""
-    import torch
-    flags = _in_flag(q) | (SAGE_ROPE_PAIRS if interleaved else 0)
-    (B, Hq, N, D), Hkv, dev = q.shape, k.shape[1], q.device
-    qs, ks = _rows(q, "q"), _rows(k, "k")
+    global _F32, _I32
+    if _F32 is None:
+        import torch
+        _F32, _I32 = torch.float32, torch.int32
+    flags = _in_flag(q)
+    if interleaved:
+        flags |= SAGE_ROPE_PAIRS
+    st = [_strides(*_rows(q, "q")), _strides(*_rows(k, "k"))]
+    B, Hq, N, D = q.shape
+    Hkv, dev = k.shape[1], q.device
     if Hq % Hkv:
         raise ValueError("q's %d heads are no multiple of k's %d" % (Hq, Hkv))
     _same(k, q, "k", (B, Hkv, N, D))
-    for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None:
-            _check_tensor(w, what, (D,), torch.float32, dev)
+    if q_weight is not None:
+        _check_tensor(q_weight, "q_weight", (D,), _F32, dev)
+    if k_weight is not None:
+        _check_tensor(k_weight, "k_weight", (D,), _F32, dev)
     half = inv_freq.numel()
     if half > D // 2 or half % 4:
         raise ValueError("inv_freq must have at most %d entries, a multiple of 4, got %d" % (D // 2, half))
-    _check_tensor(inv_freq, "inv_freq", (half,), torch.float32, dev)
-    each = pos is not None and pos.dim() == 2
+    _check_tensor(inv_freq, "inv_freq", (half,), _F32, dev)
+    each = 0
     if pos is not None:
-        _check_tensor(pos, "pos", (B, N) if each else (B,), torch.int32, dev)
+        each = int(pos.dim() == 2)
+        _check_tensor(pos, "pos", (B, N) if each else (B,), _I32, dev)
     if lens is not None:
-        _check_tensor(lens, "lens", (B,), torch.int32, dev)
+        _check_tensor(lens, "lens", (B,), _I32, dev)
     if not 2.0 ** -100 <= eps <= 1:
         raise ValueError("eps must be 2^-100 to 1, got %r" % (eps,))
-    head = (_adr(q), _adr(k), _adr(q_weight), _adr(k_weight), _adr(inv_freq), 2 * half, _adr(pos), int(each), _adr(lens))
-    return head, (B, Hq, Hkv, N, D, float(eps), flags), [_strides(*qs), _strides(*ks)]
+    head = (q.data_ptr(), k.data_ptr(), _adr(q_weight), _adr(k_weight), inv_freq.data_ptr(), 2 * half, _adr(pos), each, _adr(lens))
+    return head, (B, Hq, Hkv, N, D, eps, flags), st
 
 
 def _like(out, tensors, names, strides):
@@ -769,7 +787,6 @@ def sage_qk_norm_rope_fwd(q, k, q_weight, k_weight, inv_freq, pos=None, lens=Non
     or None (from 0 on).  ``lens``: int32 [B], the tokens of a padded batch's sequences; what lies
     behind is not read, and 0 in the outputs.  Returns both like q and k; ``out``: two tensors of any
     strides, which may be q and k themselves."""
-    import torch
     head, tail, st = _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved)
     zq, zk = _like(out, (q, k), ("out[0]", "out[1]"), st)
     _call("sage_qk_norm_rope_fwd", q.device, *head, zq.data_ptr(), zk.data_ptr(), *tail, *st)
