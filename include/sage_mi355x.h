@@ -439,7 +439,7 @@ int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void
  * max|x|; codes are those of x / scale, nearest, ties to even, as sage_quant_fp4 makes them.
  * A sequence's pages are a row of `table`, int32 [S, max_pages] on the device:
  * its token j lies in page table[s][j / page_size], slot j % page_size.  Only
- * entries of tokens that the sequence has are read; a token whose entry is not
+ * entries of tokens that the sequence has are used; a token whose entry is not
  * in [0, pages) is not stored, seen or moved.  Sequence lengths above max_pages *
  * page_size (at most 2^30) count as that, negative ones as 0.  S is at most 65535.
  */
