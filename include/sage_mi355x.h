@@ -432,8 +432,8 @@ int sage_attn_window_bwd(const void* q, const void* k, const void* v, const void
  * with s in the fp32 arrays [pages, Hkv, page_size] (a row whose s is below
  * 2^-126 has s = 0 and zero codes).
  * With SAGE_KV_FP4 in a call's flags (sage_kv_append, sage_kv_append_slots and
- * sage_attn_paged_decode) the cache is MXFP4: a row is D / 2 bytes of E2M1 codes, channel
- * 2i in the low half of byte i, strides count bytes (multiples of 16), and k_scale
+ * sage_attn_paged_decode), and in sage_kv_evict_fp4, the cache is MXFP4: a row is
+ * D / 2 bytes of E2M1 codes, channel 2i in the low half of byte i, strides count bytes (multiples of 16), and k_scale
  * and v_scale point to bytes [pages, Hkv, page_size, D / 32] (4-byte aligned): the
  * scales 2^(byte - 127) of 32 channels each, the smallest (of bytes 0 to 254) with 6 * scale >=
  * max|x|; codes are those of x / scale, nearest, ties to even, as sage_quant_fp4 makes them.
@@ -495,7 +495,6 @@ size_t sage_attn_paged_decode_workspace_size(int S, int Hq, int Hkv, int D, int 
  *           weights[s][head][j]; weights_stride >= max_pages * page_size
  *  workspace: at least sage_attn_paged_decode_workspace_size() bytes, 256-byte
  *           aligned (NULL if that is 0)
- * Over an MXFP4 cache weights must be NULL (SAGE_ERR_UNSUPPORTED).
  */
 int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_stride_s, int64_t q_stride_h, void* o,
                            float* lse, const int32_t* table, int max_pages, const int32_t* lens, int S, int Hq, int window,
@@ -529,6 +528,12 @@ int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_page
                   int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
                   int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
                   size_t workspace_bytes, hipStream_t stream);
+
+/* The same for an MXFP4 cache: a kept token's codes and scales are copied as they are. */
+int sage_kv_evict_fp4(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
+                      int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
+                      int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream);
 
 /*
  * sage_qk_norm_rope_fwd -- queries and keys as an attention takes them: the norm of every

@@ -103,6 +103,7 @@ def lib():
         L.sage_kv_evict_workspace_size.argtypes = [i] * 4
         L.sage_kv_evict_workspace_size.restype = sz
         L.sage_kv_evict.argtypes = [ca, vp, i, vp, vp, i64, vp, i, i, i, i, vp, vp, vp, i, vp, sz, vp]
+        L.sage_kv_evict_fp4.argtypes = L.sage_kv_evict.argtypes
         L.sage_status_string.argtypes = [i]
         L.sage_status_string.restype = ctypes.c_char_p
         L.sage_version.restype = ctypes.c_char_p
@@ -111,7 +112,7 @@ def lib():
                      "sage_quant_int8", "sage_attn_int8_fwd", "sage_attn_int8_fwd_ws",
                      "sage_attn_int8_fwd_prequant", "sage_attn_int8_bwd", "sage_attn_int8_bwd_ws",
                      "sage_attn_window_fwd", "sage_attn_window_bwd", "sage_kv_append", "sage_attn_paged_decode", "sage_kv_evict",
-                     "sage_kv_append_slots", "sage_qk_norm_rope_fwd", "sage_qk_norm_rope_bwd", "sage_kv_plan"):
+                     "sage_kv_evict_fp4", "sage_kv_append_slots", "sage_qk_norm_rope_fwd", "sage_qk_norm_rope_bwd", "sage_kv_plan"):
             getattr(L, name).restype = i
         _lib = L
     return _lib
@@ -644,9 +645,9 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
     """Attention of each sequence's last token, q [S, Hq, D], over its lens[s] cached tokens (its own
     among them); the cache as in sage_kv_append.  ``weights`` fp32 [S, Hkv, >= max_pages * page_size]:
     the attention weights, summed over a group's query heads, are added to it (this takes a workspace
-    of 4 * S * Hq * max_pages * page_size bytes; not over an MXFP4 cache).  Returns (O, L), L fp32 [S, Hq] (None when ``lse``
-    is False).  With ``workspace`` (uint8, at least
-    attn_paged_decode_workspace_size bytes) and ``out``, ``lse_out`` nothing is allocated inside."""
+    of 4 * S * Hq * max_pages * page_size bytes).  Returns (O, L), L fp32 [S, Hq] (None when ``lse``
+    is False).  With ``workspace`` (uint8, at least attn_paged_decode_workspace_size bytes) and ``out``,
+    ``lse_out`` nothing is allocated inside."""
     import torch
     c, kind, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
     flags, dev = _in_flag(q) | kind, k_cache.device
@@ -660,8 +661,6 @@ def sage_attn_paged_decode(q, k_cache, v_cache, table, lens, window=None, sinks:
     window, sinks = _window_of(window, sinks)
     _check_tensor(lens, "lens", (S,), torch.int32, dev)
     if weights is not None:
-        if kind:
-            raise ValueError("weights are not added up over an MXFP4 cache")
         _check_weights(weights, "weights", S, Hkv, M * page, dev)
     if out is None:
         o = q.new_empty((S, Hq, D))
@@ -700,8 +699,6 @@ def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int
     import torch
     c, kind, (S, M, page, Hkv, D) = _check_cache(k_cache, v_cache, k_scale, v_scale, table)
     dev = k_cache.device
-    if kind:
-        raise ValueError("an MXFP4 cache is not shortened")
     _check_tensor(lens, "lens", (S,), torch.int32, dev)
     _check_weights(weights, "weights", S, Hkv, M * page, dev)
     if new_table.dim() != 2 or new_table.numel() == 0:
@@ -720,8 +717,8 @@ def sage_kv_evict(k_cache, v_cache, table, lens, weights, new_table, budget: int
         workspace = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     else:
         _check_workspace(workspace, dev)
-    _call("sage_kv_evict", dev, c, _adr(table), M, _adr(lens), _adr(weights), weights.shape[2], _adr(new_table),
-          M2, budget, keep_first, keep_last, _adr(new_lens), _adr(new_weights), _adr(kept), S, _adr(workspace),
+    _call("sage_kv_evict_fp4" if kind else "sage_kv_evict", dev, c, _adr(table), M, _adr(lens), _adr(weights),
+          weights.shape[2], _adr(new_table), M2, budget, keep_first, keep_last, _adr(new_lens), _adr(new_weights), _adr(kept), S, _adr(workspace),
           workspace.numel() if workspace is not None else 0)
     return new_lens, new_weights, kept
 

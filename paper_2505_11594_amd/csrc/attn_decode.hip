@@ -419,7 +419,7 @@ __global__ __launch_bounds__(256) void add_weights_kernel(const Decode a) {
   const float* sc = a.scores + ((size_t)s * a.Hq + (size_t)hk * G) * a.score_stride;
   const float* l2 = a.lse2 + (size_t)s * a.Hq + hk * G;
   for (int j = (blockIdx.x * 256 + threadIdx.x) * 4; j < n; j += gridDim.x * 1024) {
-    // (the scores of a tile of 32 are written together, those of unseen keys as -inf; other tiles hold nothing)
+    // (the scores of a tile are written together, those of unseen keys as -inf; other tiles hold nothing)
     bool see[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) see[e] = decode_sees(j + e, n, a.window, a.sinks);
@@ -449,6 +449,14 @@ __global__ __launch_bounds__(256) void add_weights_kernel(const Decode a) {
     for (int e = 0; e < 4; ++e)
       if (see[e]) w[j + e] = old[e] + x[e];
   }
+}
+
+hipError_t launch_add_weights(const Decode& a, hipStream_t st) {
+  const int capacity = a.c.max_pages * a.c.page_size;
+  const int want = imax(1, (int)(2048 / ((long long)a.c.S * a.c.Hkv)));
+  hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)imin(cdiv(capacity, 1024), want), (unsigned)a.c.Hkv, (unsigned)a.c.S),
+                     dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 // Workgroups per group of 16 query heads of a key head.  Two fit a CU, so 512 in
@@ -486,13 +494,7 @@ static hipError_t launch_decode_t(const Decode& a, hipStream_t st) {
     hipLaunchKernelGGL((join_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(256), 0, st, a, shift);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && a.weights) {
-    const int capacity = a.c.max_pages * a.c.page_size;
-    const int want = imax(1, (int)(2048 / ((long long)a.c.S * a.c.Hkv)));
-    hipLaunchKernelGGL(add_weights_kernel, dim3((unsigned)imin(cdiv(capacity, 1024), want), (unsigned)a.c.Hkv, (unsigned)a.c.S),
-                       dim3(256), 0, st, a);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && a.weights) e = launch_add_weights(a, st);
   return e;
 }
 

@@ -68,7 +68,9 @@ __device__ __forceinline__ v2u tr_read(uint32_t at) {
 // 2^31 bytes: a subtile's place is found once for the wave, in scalar registers.  (Not only to save
 // instructions: a launch does not find its code in the caches.  5 KB more of it, for two tiles'
 // rows in flight, made every call 1 to 2.5 us longer.)
-template <int D, bool BF16, int COPIES, bool WHOLE>
+// SCORES: they are kept for the weights, which another launch adds up (32 sequences of 857 to 6000 tokens, 32 / 8
+// heads, in a graph of calls: 43 us, 34 without: 13 MB written and read, and a launch).
+template <int D, bool BF16, int COPIES, bool WHOLE, bool SCORES>
 __global__ __launch_bounds__(64 * FW, 2) void paged_decode_fp4_kernel(const Decode a) {
   constexpr int ROW = D * 2, SB = D / 32;                // bytes of a V row in LDS; scale bytes of a cached row
   constexpr int HC = 16 / COPIES, TS = 4 / COPIES;       // heads per copy; subtiles of 16 keys whose softmax a copy takes
@@ -285,6 +287,16 @@ __global__ __launch_bounds__(64 * FW, 2) void paged_decode_fp4_kernel(const Deco
             vr.scale[t] = 127;
           }
       }
+      if constexpr (SCORES) {
+        if (head < gn) {
+          float* row = a.scores + ((size_t)now.s * a.Hq + h0 + head) * a.score_stride;
+#pragma unroll
+          for (int u = 0; u < TS; ++u) {
+            const long long key = (long long)now.tl.tile(i) * FT + 16 * (TS * copy + u) + 4 * grp;
+            if (key < a.score_stride) *reinterpret_cast<v4f*>(row + key) = v4f{sc[u][0], sc[u][1], sc[u][2], sc[u][3]};
+          }
+        }
+      }
       float x = sc[0][0];
 #pragma unroll
       for (int e = 1; e < 4 * TS; ++e) x = smax(x, sc[e >> 2][e & 3]);
@@ -402,6 +414,7 @@ __global__ __launch_bounds__(64 * FW, 2) void paged_decode_fp4_kernel(const Deco
       if (whole) {
         const float l2 = ll > 0.0f || ll != ll ? mm + __builtin_log2f(ll) : -INFINITY;
         if (a.lse) a.lse[(size_t)s * a.Hq + h0 + c16] = l2 * 0.69314718055994530942f;
+        if (SCORES) a.lse2[(size_t)s * a.Hq + h0 + c16] = l2;
       } else {
         float* p = a.part + (size_t)a.nw * 2 * a.Hq * D + (slot * a.Hq + h0 + c16) * 2;
         p[0] = mm;
@@ -505,7 +518,11 @@ __global__ __launch_bounds__(64 * JW) void join_fp4_kernel(const Decode a) {
   uint16_t* out = (uint16_t*)a.o + ((size_t)s * a.Hq + h) * D + lane * CL;
   if constexpr (D == 128) *reinterpret_cast<uint32_t*>(out) = pack16<BF16>(o[0] * inv, o[1] * inv);
   else *out = (uint16_t)pack16<BF16>(o[0] * inv, 0.0f);
-  if (lane == 0 && a.lse) a.lse[(size_t)s * a.Hq + h] = some ? (all + __builtin_log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+  if (lane == 0) {
+    const float l2 = some ? all + __builtin_log2f(sum) : -INFINITY;
+    if (a.lse) a.lse[(size_t)s * a.Hq + h] = l2 * 0.69314718055994530942f;
+    if (a.lse2) a.lse2[(size_t)s * a.Hq + h] = l2;
+  }
 }
 
 template <int D, bool BF16>
@@ -522,18 +539,21 @@ hipError_t launch_t(const Decode& a, hipStream_t st) {
   const double most = (a.c.pages - 1.0) * ks.b + (a.c.page_size - 1.0) * ks.n + D / 2, rows = (double)a.c.pages * a.c.Hkv * a.c.page_size;
   const bool whole = a.c.page_size % 16 == 0 && ks.b == vs.b && ks.n == vs.n && ks.n < 1LL << 27 && most <= 0x1p31 &&
                      rows * (D / 32) <= 0x1p31;
-  if (whole) {
-    if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4, true>), grid, block, 0, st, a);
-    else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 1, true>), grid, block, 0, st, a);
-  } else if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4, false>), grid, block, 0, st, a);
-  else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2, false>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 1, false>), grid, block, 0, st, a);
+#define SAGE_DECODE_FP4(WHOLE, SCORES)                                                                                      \
+  if (G <= 4) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 4, WHOLE, SCORES>), grid, block, 0, st, a);              \
+  else if (G <= 8) hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 2, WHOLE, SCORES>), grid, block, 0, st, a);         \
+  else hipLaunchKernelGGL((paged_decode_fp4_kernel<D, BF16, 1, WHOLE, SCORES>), grid, block, 0, st, a)
+  if (whole && a.weights) { SAGE_DECODE_FP4(true, true); }
+  else if (whole) { SAGE_DECODE_FP4(true, false); }
+  else if (a.weights) { SAGE_DECODE_FP4(false, true); }
+  else { SAGE_DECODE_FP4(false, false); }
+#undef SAGE_DECODE_FP4
   e = hipGetLastError();
   if (e == hipSuccess && a.nw > 0) {
     hipLaunchKernelGGL((join_fp4_kernel<D, BF16>), dim3((unsigned)a.c.S, (unsigned)a.Hq), dim3(64 * JW), 0, st, a);
     e = hipGetLastError();
   }
+  if (e == hipSuccess && a.weights) e = launch_add_weights(a, st);
   return e;
 }
 

@@ -495,7 +495,7 @@ __global__ __launch_bounds__(EV) void evict_chunk_kernel(const Evict a, int pass
 }
 
 // 16 bytes per thread.  A row whose new place is its old one is left alone.
-template <int RB>                                        // bytes of a row
+template <int RB, typename Scale>                        // bytes of a row; what holds its scales
 __global__ __launch_bounds__(256) void evict_move_kernel(const Evict a, int elem) {
   constexpr int LPR = RB / 16;
   const int s = blockIdx.z, h = blockIdx.y, ch = threadIdx.x % LPR;
@@ -514,8 +514,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const Evict a, int elem
     *reinterpret_cast<v4i*>(const_cast<uint8_t*>(v) + elem * (dp * a.c.vs.b + h * a.c.vs.h + ds * a.c.vs.n) + 16 * ch) = vx;
     if (a.c.k_scale && ch == 0) {
       const size_t si = ((size_t)sp * a.c.Hkv + h) * ps + ss, di = ((size_t)dp * a.c.Hkv + h) * ps + ds;
-      const_cast<float*>(a.c.k_scale)[di] = a.c.k_scale[si];
-      const_cast<float*>(a.c.v_scale)[di] = a.c.v_scale[si];
+      Scale *ks = (Scale*)const_cast<float*>(a.c.k_scale), *vs = (Scale*)const_cast<float*>(a.c.v_scale);
+      ks[di] = ks[si];
+      vs[di] = vs[si];
     }
   }
 }
@@ -529,7 +530,7 @@ size_t evict_hist_ints(int S, int Hkv, int capacity) {
   return c > 1 ? (size_t)S * Hkv * c * (3 * BINS + 4) : 0;
 }
 
-hipError_t launch_kv_evict(const Evict& x, int D, hipStream_t st) {
+hipError_t launch_kv_evict(const Evict& x, int D, bool fp4, hipStream_t st) {
   Evict a = x;
   const int capacity = a.c.max_pages * a.c.page_size;
   a.chunks = evict_chunks(a.c.S, a.c.Hkv, capacity);
@@ -545,12 +546,14 @@ hipError_t launch_kv_evict(const Evict& x, int D, hipStream_t st) {
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  const int elem = a.c.k_scale ? 1 : 2, rb = D * elem, per = 256 / (rb / 16);
+  const int elem = a.c.k_scale ? 1 : 2, rb = fp4 ? D / 2 : D * elem, per = 256 / (rb / 16);
   const dim3 grid((unsigned)imin(cdiv(a.budget, per), imax(1, (int)(8192 / ((long long)a.c.S * a.c.Hkv)))),
                   (unsigned)a.c.Hkv, (unsigned)a.c.S);
-  if (rb == 256) hipLaunchKernelGGL((evict_move_kernel<256>), grid, dim3(256), 0, st, a, elem);
-  else if (rb == 128) hipLaunchKernelGGL((evict_move_kernel<128>), grid, dim3(256), 0, st, a, elem);
-  else hipLaunchKernelGGL((evict_move_kernel<64>), grid, dim3(256), 0, st, a, elem);
+  // (a row's scales move as one word: one in fp32, or 4 or 2 bytes of an MXFP4 row)
+  if (rb == 256) hipLaunchKernelGGL((evict_move_kernel<256, uint32_t>), grid, dim3(256), 0, st, a, elem);
+  else if (rb == 128) hipLaunchKernelGGL((evict_move_kernel<128, uint32_t>), grid, dim3(256), 0, st, a, elem);
+  else if (rb == 64) hipLaunchKernelGGL((evict_move_kernel<64, uint32_t>), grid, dim3(256), 0, st, a, elem);
+  else hipLaunchKernelGGL((evict_move_kernel<32, uint16_t>), grid, dim3(256), 0, st, a, elem);
   return hipGetLastError();
 }
 

@@ -88,6 +88,7 @@ int decode_workgroups(int S, int Hq, int Hkv, int capacity);
 size_t decode_line_longs(int S, int Hq, int Hkv, int capacity);
 size_t decode_part_floats(int S, int Hq, int Hkv, int D, int capacity);
 hipError_t launch_paged_decode(const Decode& a, int D, bool bf16, hipStream_t st);
+hipError_t launch_add_weights(const Decode& a, hipStream_t st);
 int decode_fp4_workgroups(int S, int Hq, int Hkv, int capacity);
 hipError_t launch_paged_decode_fp4(const Decode& a, int D, bool bf16, hipStream_t st);
 
@@ -103,7 +104,7 @@ struct Evict {
   int chunks, chunk;
 };
 size_t evict_hist_ints(int S, int Hkv, int capacity);
-hipError_t launch_kv_evict(const Evict& a, int D, hipStream_t st);
+hipError_t launch_kv_evict(const Evict& a, int D, bool fp4, hipStream_t st);
 
 // Norms of queries and keys with their rotation; zq, zk are dq, dk in the backward.
 struct NormRope {

@@ -171,6 +171,37 @@ DecodeWs decode_ws(int S, int Hq, int Hkv, int D, int capacity, bool weights) {
   return w;
 }
 
+int evict(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
+          int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first, int keep_last,
+          int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace, size_t workspace_bytes, bool fp4,
+          hipStream_t stream) {
+  const int rc = check_cache(cache, table, max_pages, S, true, fp4);
+  if (rc != SAGE_OK) return rc;
+  if (!lens || !weights || !new_table || !new_lens || !new_weights || !kept) return SAGE_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)lens, (const void*)weights, (const void*)new_table, (const void*)new_lens,
+                        (const void*)new_weights, (const void*)kept})
+    if (!aligned(p, 4)) return SAGE_ERR_INVALID_ARG;
+  if (budget < 1 || keep_first < 0 || keep_last < 0 || (long long)keep_first + keep_last > budget) return SAGE_ERR_INVALID_ARG;
+  if (new_max_pages <= 0 || (long long)new_max_pages * cache->page_size > kMaxCapacity ||
+      (long long)new_max_pages * cache->page_size < budget || weights_stride < (long long)max_pages * cache->page_size)
+    return SAGE_ERR_INVALID_ARG;
+  // outputs that other workgroups still read would change under them
+  if (new_lens == lens || new_weights == weights) return SAGE_ERR_INVALID_ARG;
+  const size_t need = sage_kv_evict_workspace_size(S, cache->Hkv, max_pages, cache->page_size);
+  if (need > 0) {
+    if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return SAGE_ERR_WORKSPACE;
+  }
+  sage::Evict a;
+  a.hist = static_cast<int*>(workspace);
+  a.c = cache_of(cache, table, max_pages, S);
+  a.lens = lens; a.new_table = new_table; a.weights = weights; a.new_weights = new_weights;
+  a.new_lens = new_lens; a.kept = kept; a.wstride = weights_stride;
+  a.new_wstride = (long long)new_max_pages * cache->page_size;
+  a.new_max_pages = new_max_pages; a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last;
+  return hip_status(sage::launch_kv_evict(a, cache->D, fp4, stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -308,7 +339,6 @@ int sage_attn_paged_decode(const sage_kv_cache* cache, const void* q, int64_t q_
   if (!strides_ok(Strides{q_stride_s, q_stride_h, 0}, 8, 0)) return SAGE_ERR_INVALID_ARG;
   const int capacity = max_pages * cache->page_size;
   if (weights && weights_stride < capacity) return SAGE_ERR_INVALID_ARG;
-  if (weights && fp4) return SAGE_ERR_UNSUPPORTED;
   const DecodeWs w = decode_ws(S, Hq, cache->Hkv, cache->D, capacity, weights != nullptr);
   if (w.total > 0) {
     if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
@@ -345,31 +375,16 @@ int sage_kv_evict(const sage_kv_cache* cache, const int32_t* table, int max_page
                   int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
                   int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
                   size_t workspace_bytes, hipStream_t stream) {
-  const int rc = check_cache(cache, table, max_pages, S, true);
-  if (rc != SAGE_OK) return rc;
-  if (!lens || !weights || !new_table || !new_lens || !new_weights || !kept) return SAGE_ERR_INVALID_ARG;
-  for (const void* p : {(const void*)lens, (const void*)weights, (const void*)new_table, (const void*)new_lens,
-                        (const void*)new_weights, (const void*)kept})
-    if (!aligned(p, 4)) return SAGE_ERR_INVALID_ARG;
-  if (budget < 1 || keep_first < 0 || keep_last < 0 || (long long)keep_first + keep_last > budget) return SAGE_ERR_INVALID_ARG;
-  if (new_max_pages <= 0 || (long long)new_max_pages * cache->page_size > kMaxCapacity ||
-      (long long)new_max_pages * cache->page_size < budget || weights_stride < (long long)max_pages * cache->page_size)
-    return SAGE_ERR_INVALID_ARG;
-  // outputs that other workgroups still read would change under them
-  if (new_lens == lens || new_weights == weights) return SAGE_ERR_INVALID_ARG;
-  const size_t need = sage_kv_evict_workspace_size(S, cache->Hkv, max_pages, cache->page_size);
-  if (need > 0) {
-    if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
-    if (workspace_bytes < need) return SAGE_ERR_WORKSPACE;
-  }
-  sage::Evict a;
-  a.hist = static_cast<int*>(workspace);
-  a.c = cache_of(cache, table, max_pages, S);
-  a.lens = lens; a.new_table = new_table; a.weights = weights; a.new_weights = new_weights;
-  a.new_lens = new_lens; a.kept = kept; a.wstride = weights_stride;
-  a.new_wstride = (long long)new_max_pages * cache->page_size;
-  a.new_max_pages = new_max_pages; a.budget = budget; a.keep_first = keep_first; a.keep_last = keep_last;
-  return hip_status(sage::launch_kv_evict(a, cache->D, stream));
+  return evict(cache, table, max_pages, lens, weights, weights_stride, new_table, new_max_pages, budget, keep_first, keep_last,
+               new_lens, new_weights, kept, S, workspace, workspace_bytes, false, stream);
+}
+
+int sage_kv_evict_fp4(const sage_kv_cache* cache, const int32_t* table, int max_pages, const int32_t* lens, const float* weights,
+                      int64_t weights_stride, const int32_t* new_table, int new_max_pages, int budget, int keep_first,
+                      int keep_last, int32_t* new_lens, float* new_weights, int32_t* kept, int S, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream) {
+  return evict(cache, table, max_pages, lens, weights, weights_stride, new_table, new_max_pages, budget, keep_first, keep_last,
+               new_lens, new_weights, kept, S, workspace, workspace_bytes, true, stream);
 }
 
 int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,

@@ -181,14 +181,16 @@ def fp4_cache(g, S, Hkv, page, D, lens, layout="hnd", spare=3, wide=False):
     return c, perm[:S * M].view(S, M).contiguous(), perm[S * M:]
 
 
-def check_decode(q, c, table, lens, window, sinks, o, lse, label):
+def check_decode(q, c, table, lens, window, sinks, o, lse, label, w0=None, w1=None):
+    """(w1: the weights w0 after the call.  Each weight is exp(S - L): S and L are off by e each, the power and the
+    logarithm and the sum that L is of by (n + 64) 2^-23 together; G weights and the old sum are added up.)"""
     import torch
     S, Hq, D = q.shape
     Hkv, page = c["k_cache"].shape[1:3]
     G, u = Hq // Hkv, _lm.unit(q.dtype)
     k, v = (mo.fp4_values(c[x + "_cache"], c[x + "_scale"]) for x in "kv")
     tab = table.cpu()
-    worst = [0.0, 0.0]
+    worst = [0.0, 0.0, 0.0]
     for s in range(S):
         n = max(0, min(int(lens[s]), table.shape[1] * page))
         for h in range(Hkv):
@@ -201,7 +203,13 @@ def check_decode(q, c, table, lens, window, sinks, o, lse, label):
             assert bool((lse[s, hs][dead] == -math.inf).all()), label
             d = torch.where(dead, 0.0, lse[s, hs].double() - r["lse"]).abs()
             worst[1] = max(worst[1], float((d / _lm.lse_bound(r, n)).max()))
-    say("%s: O at %.3f of its bound, L at %.3f" % (label, *worst))
+            if w1 is not None and n:
+                want = w0[s, h, :n].double() + r["p"].sum(0)
+                tol = ((2 * r["e"] + (n + 64) * 2.0 ** -23) * r["p"]).sum(0) + (G + 2) * 2.0 ** -24 * want.abs() + 1e-30
+                worst[2] = max(worst[2], float(((w1[s, h, :n].double() - want).abs() / tol).max()))
+        if w1 is not None:
+            assert torch.equal(w1[s, :, n:], w0[s, :, n:]), label
+    say("%s: O at %.3f of its bound, L at %.3f, weights at %.3f" % (label, *worst))
     assert max(worst) <= 1, label
 
 
@@ -248,6 +256,142 @@ def test_paged_decode_fp4(case):
     pad[:, :Hq, :D] = q
     o2, none = bd.sage_attn_paged_decode(pad[:, :Hq, :D], *args, lse=False, **kw)
     assert torch.equal(o, o2) and none is None
+
+
+@pytest.mark.parametrize("case", DECODES)
+def test_paged_decode_fp4_weights(case):
+    """The weights are added up as they are over other caches; the rest of the answer stays."""
+    import torch
+    Hq, Hkv, page, D, lens, dtype, layout, window, sinks = case
+    g = gen(200 + sum(lens) + D)
+    S = len(lens)
+    c, table, _ = fp4_cache(g, S, Hkv, page, D, lens, layout)
+    q = (0.5 * randn(g, S, Hq, D)).to(getattr(torch, DT[dtype]))
+    if S > 1:
+        table[-1, 0] = -1                                # a hole
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    say("weights fp4 %s" % (case,))
+    args = (c["k_cache"], c["v_cache"], table, ln)
+    kw = dict(window=window, sinks=sinks, k_scale=c["k_scale"], v_scale=c["v_scale"])
+    w0 = torch.rand((S, Hkv, table.shape[1] * page + 5), generator=g, device="cuda")
+    w1, w2, w3 = w0.clone(), w0.clone(), w0.clone()
+    o, lse = bd.sage_attn_paged_decode(q, *args, weights=w1, **kw)
+    torch.cuda.synchronize()
+    check_decode(q, c, table, lens, window, sinks, o, lse, "weights fp4 %s" % (case,), w0, w1)
+    o2, lse2 = bd.sage_attn_paged_decode(q, *args, weights=w2, **kw)
+    o3, lse3 = bd.sage_attn_paged_decode(q, *args, **kw)
+    assert torch.equal(w1, w2)
+    for x, y in ((o2, lse2), (o3, lse3)):
+        assert torch.equal(o, x) and torch.equal(lse, y)
+    bd.sage_attn_paged_decode(q, *args, lse=False, weights=w3, **kw)
+    assert torch.equal(w1, w3)
+
+
+EVICTS = [
+    # Hkv, page, D, lens, budget, first, last, layout
+    (1, 16, 64, [1], 1, 0, 0, "hnd"),
+    (2, 16, 64, [100, 40, 0, 41], 40, 4, 8, "hnd"),
+    (2, 24, 128, [2500, 999, 1000, 1001], 1000, 16, 300, "nhd"),
+    (3, 1, 64, [77, 30], 20, 20, 0, "nhd"),
+    (2, 64, 128, [700], 699, 0, 0, "hnd"),
+    (1, 128, 128, [20000], 1, 0, 0, "hnd"),
+    (1, 32, 64, [20000], 300, 100, 200, "hnd"),
+]
+
+
+@pytest.mark.parametrize("case", EVICTS)
+def test_evict_fp4(case):
+    """The kept tokens by their definition; their codes and scales bit for bit; nothing else of the cache changes."""
+    import torch
+    Hkv, page, D, lens, budget, first, last, layout = case
+    g = gen(sum(lens) + budget)
+    S, M2 = len(lens), -(-budget // page)
+    c, table, spare = fp4_cache(g, S, Hkv, page, D, lens, layout, spare=S * M2 + 2, wide=True)
+    new_table = spare[:S * M2].view(S, M2).contiguous()
+    w = torch.exp(3 * randn(g, S, Hkv, table.shape[1] * page + 7) - 6)
+    if D == 64:
+        w = torch.round(w * 4) / 4                       # ties
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want = {x: t.clone() for x, t in c.items()}
+    say("evict fp4 %s" % (case,))
+    nl, nw, kept = bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, ln, w, new_table, budget, first, last, k_scale=c["k_scale"],
+                                    v_scale=c["v_scale"])
+    torch.cuda.synchronize()
+    assert nl.tolist() == [min(n, budget) for n in lens]
+    wc, tc, ntc = w.cpu().numpy(), table.cpu().numpy(), new_table.cpu().numpy()
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).long().cuda()
+    for s, n in enumerate(lens):
+        for h in range(Hkv):
+            keep = _lm.kept_tokens(wc[s, h, :n], n, budget, first, last)
+            m = len(keep)
+            got, j = kept[s, h].cpu().numpy(), np.arange(m)
+            assert np.array_equal(got[:m], keep) and (got[m:] == -1).all(), (s, h)
+            assert torch.equal(nw[s, h, :m], w[s, h][dev(keep)]) and not bool(nw[s, h, m:].any())
+            for x in want:
+                want[x][dev(ntc[s, j // page]), h, dev(j % page)] = want[x][dev(tc[s, keep // page]), h, dev(keep % page)]
+    for x in c:
+        assert torch.equal(c[x], want[x]), x
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_tokens_weights_and_eviction_over_fp4(D):
+    """Prompts stored, tokens one at a time by a captured graph that adds up the weights, an eviction by these, and tokens
+    over what is left: every answer is the attention over the rows that the cache holds."""
+    import torch
+    g = gen(78)
+    S, Hq, Hkv, N, T, page = 3, 8, 2, 90, 8, 16
+    lens0 = [90, 41, 7]
+    M = -(-(N + T) // page)
+    c, table, spare = fp4_cache(g, S, Hkv, page, D, [M * page] * S, spare=3 * S)
+    kw = dict(k_scale=c["k_scale"], v_scale=c["v_scale"])
+    i32 = dict(dtype=torch.int32, device="cuda")
+    w = torch.full((S, Hkv, M * page), 9.0, device="cuda")
+    lens = torch.tensor(lens0, **i32)
+    k, v = (randn(g, S, Hkv, N, D).to(torch.bfloat16) for _ in "kv")
+    bd.sage_kv_append(k, v, c["k_cache"], c["v_cache"], table, torch.zeros(S, **i32), lens, weights=w, **kw)
+    assert all(bool((w[s, :, :n] == 0).all()) and bool((w[s, :, n:] == 9).all()) for s, n in enumerate(lens0))
+    q, kt, vt = torch.zeros((S, Hq, D), dtype=torch.bfloat16, device="cuda"), *(torch.zeros((S, Hkv, 1, D), dtype=torch.bfloat16, device="cuda") for _ in "kv")
+
+    def step(c, lens, w):
+        sc = dict(k_scale=c["k_scale"], v_scale=c["v_scale"])
+        bd.sage_kv_append(kt, vt, c["k_cache"], c["v_cache"], table, lens, weights=w, **sc)
+        lens += 1
+        return bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], table, lens, window=64, sinks=4, weights=w, **sc)
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step({x: t.clone() for x, t in c.items()}, lens.clone(), w.clone())
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = step(c, lens, w)
+    for t in range(T):
+        q.copy_(0.5 * randn(g, S, Hq, D)), kt.copy_(randn(g, S, Hkv, 1, D)), vt.copy_(randn(g, S, Hkv, 1, D))
+        eager = ({x: t.clone() for x, t in c.items()}, lens.clone(), w.clone())
+        w0 = w.clone()
+        for s in range(S):
+            w0[s, :, lens[s]] = 0                        # a new token begins with none
+        graph.replay()
+        want = step(*eager)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and torch.equal(w, eager[2]) and torch.equal(lens, eager[1])
+        assert all(torch.equal(c[x], eager[0][x]) for x in c)
+        check_decode(q, c, table, lens.tolist(), 64, 4, o, lse, "token %d" % t, w0, w)
+    new_table = spare[:3 * S].view(S, 3).contiguous()
+    nl, nw, kept = bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, lens, w, new_table, 40, 4, 16, **kw)
+    assert nl.tolist() == [min(n + T, 40) for n in lens0]
+    o, lse = bd.sage_attn_paged_decode(q, c["k_cache"], c["v_cache"], new_table, nl, **kw)
+    torch.cuda.synchronize()
+    check_decode(q, c, new_table, nl.tolist(), None, 0, o, lse, "after the eviction")
+    for s in range(S):
+        m = int(nl[s])
+        for h in range(Hkv):
+            i = kept[s, h, :m].long()
+            j = torch.arange(m, device="cuda")
+            for x in c:
+                assert torch.equal(c[x][new_table[s][j // page].long(), h, j % page], c[x][table[s][i // page].long(), h, i % page]), x
+            assert torch.equal(nw[s, h, :m], w[s, h][i])
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -571,10 +715,11 @@ def test_binding_refuses_mismatched_tensors():
         with pytest.raises(ValueError):
             put(**bad)
     one = q[:, :, 0]
-    for call in (lambda: bd.sage_attn_paged_decode(one, c["k_cache"], c["v_cache"], table, ln, weights=z((2, 2, 64), device="cuda"), **sc),
+    for call in (lambda: bd.sage_attn_paged_decode(one, c["k_cache"], c["v_cache"], table, ln, weights=z((2, 2, 47), device="cuda"), **sc),
                  lambda: bd.sage_attn_paged_decode(one[..., :32], c["k_cache"], c["v_cache"], table, ln, **sc),
                  lambda: bd.sage_attn_paged_decode(one, c["k_cache"], c["v_cache"], table, ln),
-                 lambda: bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, ln, z((2, 2, 64), device="cuda"), table.clone(), 16, **sc)):
+                 lambda: bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, ln, z((2, 1, 64), device="cuda"), table.clone(), 16, **sc),
+                 lambda: bd.sage_kv_evict(c["k_cache"], c["v_cache"], table, ln, z((2, 2, 64), device="cuda"), table.clone(), 16)):
         with pytest.raises(ValueError):
             call()
     counts, free, n = torch.ones(2, **i32), z(8, **i32), z(1, **i32)

@@ -10,7 +10,7 @@ from paper_2505_11594_amd import binding as bd
 import _more_lm as mo
 
 FAKE = 0x10000  # aligned, non-null; never dereferenced because validation fails first
-INVALID, UNSUPPORTED, WORKSPACE = bd.SAGE_ERR_INVALID_ARG, bd.SAGE_ERR_UNSUPPORTED, bd.SAGE_ERR_WORKSPACE
+INVALID, WORKSPACE = bd.SAGE_ERR_INVALID_ARG, bd.SAGE_ERR_WORKSPACE
 FP4 = bd.SAGE_KV_FP4
 
 
@@ -115,13 +115,39 @@ def test_append_slots_refusals(L, bad):
     assert append_slots(L, cache(), flags=4, B=0) == INVALID
 
 
-def test_decode_over_fp4_refuses_weights(L):
-    assert decode(L, weights=FAKE, wstride=64) == UNSUPPORTED
+def evict(L, c=None, f="sage_kv_evict_fp4", **kw):
+    a = dict(table=FAKE, M=4, lens=FAKE, weights=FAKE, wstride=64, new_table=FAKE, M2=2, budget=20, first=2, last=3, new_lens=FAKE + 4096,
+             new_weights=FAKE + 4096, kept=FAKE, S=2, ws=FAKE, size=1 << 30)
+    a.update(kw)
+    return getattr(L, f)(c or cache(), *a.values(), None)
+
+
+def test_decode_over_fp4_refusals(L):
+    wide = cache(page_size=64, ks=(8192, 4096, 64), vs=(8192, 4096, 64))
     assert decode(L, weights=FAKE, wstride=63) == INVALID
+    assert decode(L, weights=FAKE + 2, wstride=64) == INVALID
+    assert decode(L, weights=FAKE, wstride=64, ws=None) == INVALID
     assert decode(L, flags=FP4 | 8) == INVALID
     # the workspace is the one that the size function gives for any cache
-    need = bd.attn_paged_decode_workspace_size(3, 16, 2, 128, 100, 64)
-    assert decode(L, cache(page_size=64, ks=(8192, 4096, 64), vs=(8192, 4096, 64)), S=3, Hq=16, M=100, size=need - 1) == WORKSPACE
+    for w in (False, True):
+        need = bd.attn_paged_decode_workspace_size(3, 16, 2, 128, 100, 64, w)
+        kw = dict(weights=FAKE, wstride=6400) if w else {}
+        assert decode(L, wide, S=3, Hq=16, M=100, size=need - 1, **kw) == WORKSPACE
+
+
+@pytest.mark.parametrize("bad", [dict(k=0), dict(v=FAKE + 8), dict(k_scale=0), dict(k_scale=0, v_scale=0), dict(v_scale=FAKE + 2), dict(D=96),
+                                 dict(ks=(2048, 1024, 72)), dict(vs=(-16, 1024, 64)), dict(ks=(2048, 1024, 48)), dict(vs=(2048, 0, 64))])
+def test_evict_refuses_bad_fp4_caches(L, bad):
+    assert evict(L, cache(**bad)) == INVALID
+
+
+@pytest.mark.parametrize("bad", [dict(lens=None), dict(weights=None), dict(weights=FAKE + 2), dict(new_table=None), dict(budget=0), dict(budget=33),
+                                 dict(first=18), dict(last=-1), dict(M2=0), dict(wstride=63), dict(new_lens=FAKE), dict(new_weights=FAKE),
+                                 dict(kept=FAKE + 1), dict(S=70000), dict(ws=None, M=2000, wstride=32000), dict(ws=FAKE + 64, M=2000, wstride=32000)])
+def test_evict_over_fp4_refusals(L, bad):
+    assert evict(L, **bad) == INVALID
+    # rows of 64 bytes overlap as rows of 128 int8 values do
+    assert evict(L, f="sage_kv_evict") == INVALID
 
 
 def plan(L, **kw):
