@@ -69,7 +69,7 @@ __device__ __forceinline__ v2u tr_read(uint32_t at) {
 // instructions: a launch does not find its code in the caches.  5 KB more of it, for two tiles'
 // rows in flight, made every call 1 to 2.5 us longer.)
 // SCORES: they are kept for the weights, which another launch adds up (32 sequences of 857 to 6000 tokens, 32 / 8
-// heads, in a graph of calls: 43 us, 34 without: 13 MB written and read, and a launch).
+// heads, in a graph of calls: 43 us, 34 without: 14 MB written and read, and a launch).
 template <int D, bool BF16, int COPIES, bool WHOLE, bool SCORES>
 __global__ __launch_bounds__(64 * FW, 2) void paged_decode_fp4_kernel(const Decode a) {
   constexpr int ROW = D * 2, SB = D / 32;                // bytes of a V row in LDS; scale bytes of a cached row
