@@ -550,8 +550,10 @@ int sage_kv_evict_fp4(const sage_kv_cache* cache, const int32_t* table, int max_
  *             the rows' first tokens, from which they run on (below 2^31); or NULL (0)
  *  lens     : int32 [B] or NULL: tokens of each sequence of a padded batch.  What lies
  *             behind is not read, and zero in the outputs
- *  zq, zk   : shapes of q and k, any strides; may be q and k themselves (the same address
- *             and strides), rows may not overlap otherwise
+ *  zq, zk   : shapes of q and k, any strides; zq may be q and zk k itself (the same address
+ *             and strides).  Other rows in common, of an output with itself, the other one or an
+ *             input, are SAGE_ERR_INVALID_ARG (views of one buffer whose rows lie between one
+ *             another's have none)
  * flags: SAGE_IN_BF16, SAGE_ROPE_PAIRS.  No workspace.
  */
 int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
@@ -569,7 +571,7 @@ size_t sage_qk_norm_rope_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D
  *  q, k and all else as given to the forward
  *  dzq, dzk : gradients of zq, zk, any strides; not read behind a sequence's end
  *  dq, dk   : shapes of q and k, any strides; zero behind a sequence's end.  They may be
- *             dzq and dzk, or q and k, themselves
+ *             dzq and dzk, or q and k, themselves; as zq and zk otherwise
  *  dq_weight, dk_weight: fp32 [D] or NULL, written (not added to); the same call gives the
  *             same bits
  *  workspace: at least sage_qk_norm_rope_bwd_workspace_size() bytes, 256-byte aligned

@@ -783,7 +783,7 @@ def sage_qk_norm_rope_fwd(q, k, q_weight, k_weight, inv_freq, pos=None, lens=Non
     multiple of 4 entries.  ``pos``: int32 [B, N], or [B] for rows whose positions run on from these,
     or None (from 0 on).  ``lens``: int32 [B], the tokens of a padded batch's sequences; what lies
     behind is not read, and 0 in the outputs.  Returns both like q and k; ``out``: two tensors of any
-    strides, which may be q and k themselves."""
+    strides, which may be q and k themselves; other rows in common are refused."""
     head, tail, st = _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interleaved)
     zq, zk = _like(out, (q, k), ("out[0]", "out[1]"), st)
     _call("sage_qk_norm_rope_fwd", q.device, *head, zq.data_ptr(), zk.data_ptr(), *tail, *st)

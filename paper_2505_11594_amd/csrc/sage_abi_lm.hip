@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "lm_args.h"
+#include "rows.h"
 #include "sage_mi355x.h"
 
 namespace {
@@ -124,7 +125,7 @@ int check_norm_rope(sage::NormRope& a, const void* q, const void* k, const float
     if (!strides_ok(s, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
   return SAGE_OK;
 }
-// Its outputs: rows apart, and each either away from its input or the very same tensor.
+// Its outputs: rows apart.
 int check_norm_rope_out(sage::NormRope& a, void* zq, void* zk, int D, const sage_strides* zq_strides, const sage_strides* zk_strides) {
   if (!zq || !zk || !aligned(zq, 16) || !aligned(zk, 16)) return SAGE_ERR_INVALID_ARG;
   a.zq = zq; a.zk = zk;
@@ -133,6 +134,26 @@ int check_norm_rope_out(sage::NormRope& a, void* zq, void* zk, int D, const sage
     if (!strides_ok(s, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
   if (!distinct_rows(a.zqs, a.B, a.Hq, a.N, D) || !distinct_rows(a.zks, a.B, a.Hkv, a.N, D)) return SAGE_ERR_INVALID_ARG;
   return SAGE_OK;
+}
+// No output has memory in common with another tensor, but for that of its own heads (zq with q and gq, zk with k and
+// gk) where it is the very same: a wave stores a row when it has read it, and nobody else reads it.  Any other row
+// of an input may still be waiting for its wave.
+bool norm_rope_apart(const sage::NormRope& a, int D) {
+  struct View { const void* p; const Strides* s; int H; };
+  const View zq{a.zq, &a.zqs, a.Hq}, zk{a.zk, &a.zks, a.Hkv}, q[2] = {{a.q, &a.qs, a.Hq}, {a.gq, &a.gqs, a.Hq}},
+             k[2] = {{a.k, &a.ks, a.Hkv}, {a.gk, &a.gks, a.Hkv}};
+  auto meet = [&](const View& x, const View& y) {
+    const sage::RowSet rx(D, x.s->b, a.B, x.s->h, x.H, x.s->n, a.N), ry(D, y.s->b, a.B, y.s->h, y.H, y.s->n, a.N);
+    int steps = 4096;
+    return sage::rows_meet(rx, 0, ry, 0, ((long long)(intptr_t)y.p - (long long)(intptr_t)x.p) / 2, &steps);
+  };
+  auto same = [&](const View& x, const View& y) {
+    return x.p == y.p && (a.B == 1 || x.s->b == y.s->b) && (x.H == 1 || x.s->h == y.s->h) && (a.N == 1 || x.s->n == y.s->n);
+  };
+  if (meet(zq, zk)) return false;
+  for (int i = 0; i < 2 && q[i].p; ++i)
+    if ((!same(zq, q[i]) && meet(zq, q[i])) || (!same(zk, k[i]) && meet(zk, k[i])) || meet(zq, k[i]) || meet(zk, q[i])) return false;
+  return true;
 }
 
 struct BwdWs {
@@ -397,6 +418,7 @@ int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, c
                            q_strides, k_strides);
   if (rc == SAGE_OK) rc = check_norm_rope_out(a, zq, zk, D, zq_strides, zk_strides);
   if (rc != SAGE_OK) return rc;
+  if (!norm_rope_apart(a, D)) return SAGE_ERR_INVALID_ARG;
   return hip_status(sage::launch_norm_rope(a, D, (flags & SAGE_IN_BF16) != 0, (flags & SAGE_ROPE_PAIRS) != 0, false, stream));
 }
 
@@ -424,6 +446,7 @@ int sage_qk_norm_rope_bwd(const void* q, const void* k, const float* q_weight, c
     if (!strides_ok(s, 8, kMaxElems)) return SAGE_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, 256)) return SAGE_ERR_INVALID_ARG;
   if (workspace_bytes < sage_qk_norm_rope_bwd_workspace_size(B, Hq, Hkv, N, D)) return SAGE_ERR_WORKSPACE;
+  if (!norm_rope_apart(a, D) || (dq_weight && dq_weight == dk_weight)) return SAGE_ERR_INVALID_ARG;
   a.part = static_cast<float*>(workspace);
   return hip_status(sage::launch_norm_rope(a, D, (flags & SAGE_IN_BF16) != 0, (flags & SAGE_ROPE_PAIRS) != 0, true, stream));
 }
