@@ -171,6 +171,8 @@ def _check_qkv(q, k, v):
 def _check_tensor(t, what: str, shape, dtype, device):
     """A caller-supplied buffer must match what the kernels will write or read
     (the C ABI receives bare pointers and cannot check it)."""
+    if type(shape) is not tuple:                         # a caller's list never equals a torch.Size
+        shape = tuple(shape)
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device.index or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s, got %s %s on %s"
                          % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
