@@ -432,9 +432,9 @@ def _call(fn: str, device, *args):
     """The C call on ``device`` and its current stream."""
     f = _calls.get(fn)
     if f is None:
-        f = _calls[fn] = getattr(lib(), fn)
         import torch
-        _calls[""] = torch
+        _calls[""] = torch                               # first: who finds the function takes this too
+        f = _calls[fn] = getattr(lib(), fn)
     torch = _calls[""]
     index = device.index
     stream = torch._C._cuda_getCurrentRawStream(index)
@@ -735,7 +735,8 @@ def _check_norm_rope(q, k, q_weight, k_weight, inv_freq, pos, lens, eps, interle
     global _F32, _I32
     if _F32 is None:
         import torch
-        _F32, _I32 = torch.float32, torch.int32
+        _I32 = torch.int32                               # first: who finds _F32 takes this too
+        _F32 = torch.float32
     flags = _in_flag(q)
     if interleaved:
         flags |= SAGE_ROPE_PAIRS
