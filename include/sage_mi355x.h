@@ -602,7 +602,9 @@ int sage_qk_norm_rope_bwd(const void* q, const void* k, const float* q_weight, c
  *  granted    : int32 [S], counts[s] or 0;  starts: int32 [S + 1], their sums before each
  *  pos, slots : int32, int64 [max_tokens]: new token i's position in its sequence and slot,
  *               page * page_size + place in the page; behind the last 0 and -1.  Tokens of
- *               request s are starts[s] to starts[s + 1] - 1
+ *               request s are starts[s] to starts[s + 1] - 1.  (Tokens of all requests lie behind one
+ *               another; sage_attn_paged_decode takes a row per request: gather its q by
+ *               starts[s + 1] - 1.  The row of a request that was granted none says nothing.)
  * table, lens, free_pages and n_free are changed in place.  No two arguments overlap.  S is at
  * most 65535.  No workspace.
  */

@@ -835,7 +835,10 @@ def sage_kv_plan(table, lens, counts, free_pages, n_free, page_size: int, max_to
     place; requests are granted in order as far as pages and ``max_tokens`` go.  Returns (granted [S],
     starts [S + 1], pos [max_tokens], slots int64 [max_tokens]): the tokens granted, their sums before
     each request, and each new token's position and slot (0 and -1 behind the last), for
-    sage_qk_norm_rope_fwd and sage_kv_append_slots.  With ``out`` (these four) nothing is allocated."""
+    sage_qk_norm_rope_fwd and sage_kv_append_slots.  Tokens of all requests lie behind one another:
+    sage_attn_paged_decode, which takes a row per request, wants row starts[s + 1] - 1 for request s (and
+    what it gives for a request that was granted none says nothing).  With ``out`` (these four) nothing
+    is allocated."""
     import torch
     if table.dim() != 2 or table.numel() == 0 or not table.is_cuda:
         raise ValueError("table must be a non-empty [S, max_pages] device tensor")
