@@ -458,7 +458,8 @@ typedef struct {
  *  weights: fp32 [S, Hkv, weights_stride] or NULL: set to 0 for the new tokens
  * Where two tokens of one call go to the same slot, parts of both may be left there (of
  * an INT8 or MXFP4 cache also one's codes with the other's scale).  For an INT8 or MXFP4
- * cache k and v must be finite.
+ * cache k and v must be finite, and for MXFP4 below 1.75 * 2^127 in size (from there on they
+ * round to 2^128).
  */
 int sage_kv_append(const sage_kv_cache* cache, const void* k, const void* v, const sage_strides* k_strides,
                    const sage_strides* v_strides, const int32_t* table, int max_pages, const int32_t* pos,

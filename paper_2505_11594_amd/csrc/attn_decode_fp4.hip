@@ -65,7 +65,8 @@ __device__ __forceinline__ v2u tr_read(uint32_t at) {
 }
 
 // WHOLE: the 16 keys of a subtile lie on one page, K and V lie alike, and each has at most
-// 2^31 bytes: a subtile's place is found once for the wave, in scalar registers.  (Not only to save
+// 2^31 bytes: a subtile's place is found once for the wave, in scalar registers.  (17 to 35 of what else is
+// scalar lie in lanes of a vector register for it, read per sequence, not per tile.  Not only to save
 // instructions: a launch does not find its code in the caches.  5 KB more of it, for two tiles'
 // rows in flight, made every call 1 to 2.5 us longer.)
 // SCORES: they are kept for the weights, which another launch adds up (32 sequences of 857 to 6000 tokens, 32 / 8

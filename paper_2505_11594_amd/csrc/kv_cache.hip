@@ -38,6 +38,11 @@ __device__ __forceinline__ void quantize8(const v4i x, float* scale, v2u* codes)
 // sides are contiguous for one head.  4 sequences of up to 4096 tokens, 8 heads: 16-bit
 // 15-16 us, 5.8 TB/s; INT8 19-20 us, 3.5 TB/s, as the VALU is busy 95% of the time (65%
 // for 16 bits: the divisions that find a row's place).
+// kv_store_kernel below, whose divisions are multiplications, in its place (graphs of calls on four sets of
+// inputs, bf16, 8 heads, D = 128, pages of 32): 4 x up to 4096 tokens 16-bit 20.8 us for 20.7 here, INT8 16.3
+// for 18.3; 8 x up to 1500 13.9 for 13.7, 11.4 for 12.4; 32 x 512 28.5 for 28.3, 23.9 for 24.6; 128 x 1
+// 2.4 for 2.6, 3.0 for 3.1.  16-bit caches gain nothing; INT8 ones would gain 3 to 11% and are still
+// stored here.
 template <int D, bool BF16, bool I8>
 __global__ __launch_bounds__(256) void kv_append_kernel(const Append a) {
   constexpr int LPR = D / 8;
@@ -98,7 +103,8 @@ hipError_t launch_kv_append(const Append& a, int D, bool bf16, hipStream_t st) {
 }
 
 // The same for a cache in MXFP4, and for every kind of cache where the caller gives each
-// token's slot (page * page_size + its place in the page) in place of tables.  MXFP4 rows:
+// token's slot (page * page_size + its place in the page) in place of tables (the tokens above by slots,
+// in one row: 16-bit 20.1, 12.2, 27.9, 2.3 us; INT8 15.6, 10.8, 23.8, 2.9; MXFP4 11.1, 8.7, 19.0, 2.6).  MXFP4 rows:
 // per 32 channels the scale 2^e has the smallest e with 6 * 2^e >= max|x| (phi of the FP4
 // attention), codes are E2M1 of x / 2^e, nearest, ties to even; 4 lanes of 8 channels make
 // a block.  (4 sequences of up to 4096 tokens, 8 heads: 13.3 us, 4.3 TB/s, VALU busy 43%; 14.2 with

@@ -2,7 +2,7 @@
 // have ended go back on the stack of free pages, requests that bring tokens take theirs from
 // it, and every new token gets its position and its slot in the cache.  Whole numbers
 // only; what it takes is the way through memory and the launches: 7 us for the next step of 256
-// requests of 8000 cached tokens, 26 of them ended; 6 + 4 us for 64 prompts of up to 2000 tokens.
+// requests of up to 8000 cached tokens, a tenth of them ended; 6 + 4 us for 64 prompts of up to 2000 tokens.
 //
 // Requests are granted in their order: with A and C the sums of the pages and tokens asked
 // for up to a request, its own among them (by requests that cannot fit their row of the table:

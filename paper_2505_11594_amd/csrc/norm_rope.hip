@@ -9,7 +9,9 @@
 // sums.  A wave takes a token (or a part of its heads): its lanes find the token's angles
 // once, one each, for all of its rows.  The bytes bound it: 32768 tokens of 32 / 8 heads, D = 128,
 // take 133 us, 5.05 TB/s (a large copy: 5.27); 8192 tokens 34 us, their backward 51 and 4.8 for the
-// weights' sums (VALU busy half of the time in all three).
+// weights' sums (VALU busy half of the time in all three).  The scalar registers that do not do lie in
+// lanes of vector ones (4 in the forward, 23-25 in the backward): read per token, not in the loop over
+// its rows.
 //
 // Angles: p f in 64 bits (a position has up to 31 bits, f 24: 53 keep the product's
 // fraction of a turn to 2^-22 of one at the farthest), reduced there to an eighth of a turn
@@ -358,8 +360,11 @@ static int split_of(long long tokens, int Hq, int Hkv, int D) {
   while (split * 2 <= steps && tokens * split < 4096) split *= 2;
   return split;
 }
-// The backward's workgroups: each leaves a sum of its own, so no more than fill the GPU once (4
-// waves per SIMD).
+// The backward's workgroups: each leaves a sum of its own, so no more than fill the GPU once at 4
+// waves per SIMD.  That is what the kernel's 124 registers let run, but for fp16 in pairs: its 132 let 3,
+// and a quarter of the workgroups comes in a second round (8192 tokens of 32 / 8 heads, D = 128, graph of
+// calls: 61 us; fp16 in halves 53, bf16 in pairs 56 and in halves 53-54.  2 x 1000 of 12 / 4, D = 64: 15.3;
+// 12.8, 13.8 and 12.7).
 int norm_rope_bwd_blocks(long long tokens, int Hq, int Hkv, int D) {
   const long long want = (tokens * split_of(tokens, Hq, Hkv, D) + 3) / 4;
   return (int)(want < 1024 ? want : 1024);
