@@ -553,8 +553,8 @@ int sage_kv_evict_fp4(const sage_kv_cache* cache, const int32_t* table, int max_
  *             behind is not read, and zero in the outputs
  *  zq, zk   : shapes of q and k, any strides; zq may be q and zk k itself (the same address
  *             and strides).  Other rows in common, of an output with itself, the other one or an
- *             input, are SAGE_ERR_INVALID_ARG (views of one buffer whose rows lie between one
- *             another's have none)
+ *             input, may not be, and are SAGE_ERR_INVALID_ARG where the call sees them: always in
+ *             views of one buffer (which have none if their rows lie between one another's)
  * flags: SAGE_IN_BF16, SAGE_ROPE_PAIRS.  No workspace.
  */
 int sage_qk_norm_rope_fwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
@@ -573,8 +573,8 @@ size_t sage_qk_norm_rope_bwd_workspace_size(int B, int Hq, int Hkv, int N, int D
  *  dzq, dzk : gradients of zq, zk, any strides; not read behind a sequence's end
  *  dq, dk   : shapes of q and k, any strides; zero behind a sequence's end.  They may be
  *             dzq and dzk, or q and k, themselves; as zq and zk otherwise
- *  dq_weight, dk_weight: fp32 [D] or NULL, written (not added to); the same call gives the
- *             same bits
+ *  dq_weight, dk_weight: fp32 [D] or NULL, not the same array, written (not added to); the same
+ *             call gives the same bits
  *  workspace: at least sage_qk_norm_rope_bwd_workspace_size() bytes, 256-byte aligned
  */
 int sage_qk_norm_rope_bwd(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* inv_freq,
